@@ -15,7 +15,8 @@
  *     live in the library's own device globals and are filled on first use per device.)
  *   - Work is enqueued on `hip_stream` (a hipStream_t passed as void*, NULL = default
  *     stream).  Every call synchronises that stream before it returns, so the status and
- *     all outputs are final on return.
+ *     all outputs are final on return; the calls under "Fitting the laws" below do not, they
+ *     return once their kernels are enqueued.
  *   - Return value: 0 on success, a negative PILC_E_* code otherwise.  No exceptions.  Calls on
  *     different streams may run concurrently, from any threads, if they use different workspaces.
  *     The library's only process-wide state: the constant tables (filled once per device under a
@@ -311,6 +312,164 @@ int pilc_twar_forward(uint32_t n, uint32_t h, uint32_t w, const uint8_t *img_dev
  * Errors: PILC_E_ARG, PILC_E_TOO_LARGE, PILC_E_HIP, PILC_E_TIMEOUT (img_dev contents undefined). */
 int pilc_twar_inverse(uint32_t n, uint32_t h, uint32_t w, const uint8_t *res_dev,
                       const pilc_twar_params *params_host, uint8_t *img_dev, void *hip_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Fitting the laws.  The coder takes the laws of its symbols as given; what follows is for the
+ * program that learns them: what symbols cost under a model's logits and what else they might
+ * have been, the gradient of that cost, the norm before the layer that makes the logits, and the
+ * step that moves the weights.
+ *
+ * These entry points differ from the coder's in two ways.  They only ENQUEUE their kernels on
+ * `hip_stream` and return: nothing that happens on the device decides their status, and outputs
+ * are final when the stream gets there, as with a kernel of the caller's own (they may be
+ * captured into a graph).  And tensors need no more alignment than their elements have, except
+ * the workspace (256 bytes); what is aligned to 16 bytes, rows included, is read faster.
+ * pilc_last_timing reports nothing for them.  Inputs and outputs must not overlap unless a
+ * comment says that they may.  Sums, statistics and states are held in 32 bits; a value is
+ * rounded to its tensor's type once, to the nearest, ties to even.
+ * ------------------------------------------------------------------------------------------ */
+enum { PILC_F32 = 0, PILC_BF16 = 1, PILC_F16 = 2 }; /* types of values */
+enum { PILC_U8 = 0, PILC_I32 = 1, PILC_I64 = 2 };   /* types of symbols */
+
+/* rows x num_sym logits, row r at r * stride elements; what lies between rows is never used. */
+typedef struct {
+    uint32_t rows;        /* 0: the calls do nothing                                        */
+    uint32_t num_sym;     /* 1 .. 2^31 - 1                                                  */
+    uint64_t stride;      /* >= num_sym, in elements                                        */
+    uint32_t dtype;       /* PILC_F32, PILC_BF16, PILC_F16                                  */
+    uint32_t target_type; /* PILC_U8, PILC_I32, PILC_I64                                    */
+    uint32_t top;         /* alternatives a row, 0 .. 32                                    */
+} pilc_logits_shape;
+
+/* Device workspace of pilc_logprobs and pilc_logprobs_train for this shape (at least 256).
+ * Errors: PILC_E_ARG. */
+int pilc_logprobs_workspace_size(const pilc_logits_shape *shape, size_t *workspace_bytes_host);
+
+/* What symbols cost under the law that a row of logits x stands for, p_j = exp(x_j - lse),
+ * lse = ln sum_j exp(x_j).  Per row, in nats (a symbol's length in a container is about
+ * -logp / ln 2 bits):
+ *   logp_dev       f32 [rows]  x_t - lse of the target t; NULL: not wanted
+ *   entropy_dev    f32 [rows]  -sum_j p_j ln p_j; NULL: not wanted
+ *   lse_dev        f32 [rows]  NULL: not wanted
+ *   top_sym_dev    int32 [rows, top], top_logp_dev f32 [rows, top]: the `top` most likely symbols,
+ *                  most likely first, the lower symbol first among equals, and ln p of each;
+ *                  symbol -1 and -inf where fewer symbols have a probability above 0
+ *   target_dev     [rows]; NULL if logp_dev is NULL.  A negative target does not count: its logp
+ *                  is 0.  A target >= num_sym: NaN
+ * Logits of -inf are symbols that cannot occur.  A row that has no others has no law: lse and
+ * logp are -inf, the entropy 0, there are no alternatives.  A row with a NaN or +inf among its
+ * logits: lse, entropy, logp and top_logp are NaN, top_sym -1.
+ * Errors: PILC_E_ARG, PILC_E_WORKSPACE, PILC_E_HIP. */
+int pilc_logprobs(const pilc_logits_shape *shape, const void *logits_dev, const void *target_dev,
+                  float *logp_dev, float *entropy_dev, float *lse_dev, int32_t *top_sym_dev,
+                  float *top_logp_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* The gradient of sum_r up_logp[r] logp[r] + up_entropy[r] entropy[r] by the logits:
+ *   grad_j = a (1[j = t] - p_j) - b p_j (ln p_j + entropy),  a = up_logp[r] (0 where the target does
+ * not count), b = up_entropy[r].
+ *   lse_dev, entropy_dev   f32 [rows], from pilc_logprobs
+ *   up_logp_dev            f32 [rows]
+ *   up_entropy_dev         f32 [rows]; NULL: no such term, entropy_dev is then not read
+ *   grad_dev               [rows, num_sym] of the logits' type, row r at r * grad_stride; may be the
+ *                          logits themselves (same address and stride)
+ * A row whose a and b are both 0 gets zeros whatever its logits are, and so does a row without a
+ * law; a row with a NaN, a +inf or a target >= num_sym (a or b not 0) gets NaN throughout.
+ * `top` is not looked at.  Errors: PILC_E_ARG, PILC_E_HIP. */
+int pilc_logprobs_grad(const pilc_logits_shape *shape, const void *logits_dev, const void *target_dev,
+                       const float *lse_dev, const float *entropy_dev, const float *up_logp_dev,
+                       const float *up_entropy_dev, void *grad_dev, uint64_t grad_stride,
+                       void *hip_stream);
+
+/* Both in one call, for a loss whose weights are known beforehand: the logp, entropy and lse of
+ * pilc_logprobs (entropy_dev, lse_dev NULL: not wanted) and the gradient of pilc_logprobs_grad.
+ * `top` has to be 0.  Errors: PILC_E_ARG, PILC_E_WORKSPACE, PILC_E_HIP. */
+int pilc_logprobs_train(const pilc_logits_shape *shape, const void *logits_dev, const void *target_dev,
+                        const float *up_logp_dev, const float *up_entropy_dev, float *logp_dev,
+                        float *entropy_dev, float *lse_dev, void *grad_dev, uint64_t grad_stride,
+                        void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* rows x width values; strides between rows in elements, >= width. */
+typedef struct {
+    uint32_t rows;        /* 0: forward does nothing, backward's weight gradients are 0     */
+    uint32_t width;       /* 1 .. 2^31 - 1                                                  */
+    uint64_t x_stride;    /* of x                                                           */
+    uint64_t y_stride;    /* of y, in the backward pass of dy                               */
+    uint64_t dx_stride;   /* of dx; not looked at by the forward pass                       */
+    uint32_t dtype;       /* of x, y, dy, dx: PILC_F32, PILC_BF16, PILC_F16                 */
+    uint32_t weight_type; /* of weight, bias and their gradients: dtype or PILC_F32         */
+    float eps;            /* >= 0                                                           */
+} pilc_norm_shape;
+
+/* y = (x - mean) rstd weight + bias, rstd = 1 / sqrt(mean of (x - mean)^2 + eps), over each row.
+ * weight_dev, bias_dev [width], NULL: 1 and 0.  mean_dev, rstd_dev f32 [rows], NULL: not wanted.
+ * y_dev may be x_dev (same stride).  Errors: PILC_E_ARG, PILC_E_HIP. */
+int pilc_norm_forward(const pilc_norm_shape *shape, const void *x_dev, const void *weight_dev,
+                      const void *bias_dev, void *y_dev, float *mean_dev, float *rstd_dev,
+                      void *hip_stream);
+
+/* Device workspace of pilc_norm_backward (at least 256).  Errors: PILC_E_ARG. */
+int pilc_norm_workspace_size(const pilc_norm_shape *shape, size_t *workspace_bytes_host);
+
+/* With xh = (x - mean) rstd and q = dy weight:
+ *   dx = rstd (q - mean of q - xh mean of (q xh)) over each row, dweight = sum over rows of dy xh,
+ *   dbias = sum over rows of dy.
+ * mean_dev, rstd_dev f32 [rows] from the forward pass; weight_dev NULL: 1.  dx_dev, dweight_dev,
+ * dbias_dev: NULL: not wanted, one at least is.  dx_dev may be dy_dev (dx_stride = y_stride).  The
+ * sums over rows are taken in an order that the shape and the GPU's number of compute units fix.
+ * Errors: PILC_E_ARG, PILC_E_WORKSPACE, PILC_E_HIP. */
+int pilc_norm_backward(const pilc_norm_shape *shape, const void *dy_dev, const void *x_dev,
+                       const void *weight_dev, const float *mean_dev, const float *rstd_dev,
+                       void *dx_dev, void *dweight_dev, void *dbias_dev, void *workspace_dev,
+                       size_t workspace_bytes, void *hip_stream);
+
+/* One tensor of an AdamW step: `count` values, dense. */
+typedef struct {
+    void *param;       /* device, param_type; updated                                       */
+    const void *grad;  /* device, grad_type                                                 */
+    void *m, *v;       /* device, f32, or uint8 codes with state_bits 8; updated            */
+    uint8_t *m_scale;  /* device, a byte for each 256 values (the last ones maybe fewer);   */
+    uint8_t *v_scale;  /*   state_bits 8 only                                               */
+    uint64_t count;    /* 0: left out                                                       */
+    float lr_mult;     /* lr of this tensor = lr * lr_mult                                  */
+    float decay;       /* weight decay                                                      */
+} pilc_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps; /* 0 <= beta < 1, eps >= 0                                */
+    double grad_scale;            /* the gradients are multiplied by it                     */
+    uint64_t step;                /* of this step, from 1                                   */
+    uint32_t param_type, grad_type;
+    uint32_t state_bits;          /* 32 or 8                                                */
+    uint32_t dither;              /* state_bits 8: another number every step, say its own   */
+} pilc_adamw_params;
+
+/* One step over `num_tensors` tensors (tensors_host is read before the call returns):
+ *   g = grad grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   param = param (1 - lr decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * with the new m and v as they are before they are put into 8 bits.
+ *
+ * State in 8 bits: 256 values in a row share a scale 2^(e-126), e the exponent field of the
+ * largest of them (at least 1), held as a byte; e = 255 says that the block is not finite, its
+ * values are NaN.  A value is coded as a short floating number of its distance from zero plus a
+ * constant, y = |value| / scale + 2^-k (k = 15 for m, 31 for v), three bits behind the leading one:
+ *   code = ((bits(y) + r) >> 20) - ((127 - k) << 3),  value = sign (y(code) - 2^-k) scale
+ * m has its sign in bit 7, v none.  Even steps near zero (2^-18 of the scale for m, 2^-34 for v),
+ * an eighth of the value above.  r = 16 n + 8, n being 16 bits of a hash of the value's number in
+ * the list and `dither` (low half m, high half v), so that rounding up or down is as likely as it
+ * is near: an average that moves by less than a step at a time, as beta2 makes them, still moves.
+ * A v above 0 never gets code 0: a denominator does not vanish under an m that does not.
+ * A value's number is 256 times the whole or begun blocks of the tensors before its own, plus its
+ * place in it; hash, with 32-bit wrap-around: h = low * 0x9E3779B9 + high * 0x6A09E667 + dither *
+ * 0xBB67AE85; h ^= h >> 16; h *= 0x3C6EF373; h ^= h >> 15; h *= 0xA54FF53B; h ^= h >> 16.
+ * States start as zero bytes.
+ * Errors: PILC_E_ARG, PILC_E_HIP. */
+int pilc_adamw_step(const pilc_adamw_params *params_host, const pilc_adamw_tensor *tensors_host,
+                    uint32_t num_tensors, void *hip_stream);
+
+/* The values that `count` codes stand for, in 32 bits (for a checkpoint, or to look at them).
+ * is_signed: 1 for m, 0 for v.  Errors: PILC_E_ARG, PILC_E_HIP. */
+int pilc_adamw_values(const uint8_t *code_dev, const uint8_t *scale_dev, uint64_t count, int is_signed,
+                      float *values_dev, void *hip_stream);
 
 const char *pilc_strerror(int code);
 const char *pilc_last_hip_error(void); /* text of the last HIP failure on this thread */

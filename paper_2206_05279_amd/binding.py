@@ -33,6 +33,9 @@ EXPORTS = [
     "pilc_ansai_table_bytes", "pilc_ansai_build_tables", "pilc_ansai_workspace_size", "pilc_ansai_encode",
     "pilc_ansai_decode", "pilc_ansai_center", "pilc_twar_forward", "pilc_twar_inverse",
     "pilc_mix_encode", "pilc_mix_decode",
+    "pilc_logprobs_workspace_size", "pilc_logprobs", "pilc_logprobs_grad", "pilc_logprobs_train",
+    "pilc_norm_workspace_size", "pilc_norm_forward", "pilc_norm_backward",
+    "pilc_adamw_step", "pilc_adamw_values",
 ]
 
 
@@ -57,6 +60,28 @@ class pilc_ansai_shape(C.Structure):
 
 class pilc_twar_params(C.Structure):
     _fields_ = [("w", (C.c_int16 * 3) * 3), ("bias", C.c_int32 * 3)]
+
+
+class pilc_logits_shape(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("num_sym", C.c_uint32), ("stride", C.c_uint64), ("dtype", C.c_uint32),
+                ("target_type", C.c_uint32), ("top", C.c_uint32)]
+
+
+class pilc_norm_shape(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("width", C.c_uint32), ("x_stride", C.c_uint64), ("y_stride", C.c_uint64),
+                ("dx_stride", C.c_uint64), ("dtype", C.c_uint32), ("weight_type", C.c_uint32), ("eps", C.c_float)]
+
+
+class pilc_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("count", C.c_uint64), ("lr_mult", C.c_float),
+                ("decay", C.c_float)]
+
+
+class pilc_adamw_params(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("grad_scale", C.c_double), ("step", C.c_uint64), ("param_type", C.c_uint32), ("grad_type", C.c_uint32),
+                ("state_bits", C.c_uint32), ("dither", C.c_uint32)]
 
 
 class PilcError(RuntimeError):
@@ -143,6 +168,21 @@ def lib():
         L.pilc_mix_decode.restype = C.c_int
         L.pilc_mix_decode.argtypes = [gp, C.c_void_p, C.c_size_t, mp, C.c_void_p, C.c_size_t,
                                       C.c_void_p, C.c_void_p]
+        V, Z = C.c_void_p, C.c_size_t
+        lp, np_ = C.POINTER(pilc_logits_shape), C.POINTER(pilc_norm_shape)
+        L.pilc_logprobs_workspace_size.argtypes = [lp, C.POINTER(Z)]
+        L.pilc_logprobs.argtypes = [lp, V, V, V, V, V, V, V, V, Z, V]
+        L.pilc_logprobs_grad.argtypes = [lp, V, V, V, V, V, V, V, C.c_uint64, V]
+        L.pilc_logprobs_train.argtypes = [lp, V, V, V, V, V, V, V, V, C.c_uint64, V, Z, V]
+        L.pilc_norm_workspace_size.argtypes = [np_, C.POINTER(Z)]
+        L.pilc_norm_forward.argtypes = [np_, V, V, V, V, V, V, V]
+        L.pilc_norm_backward.argtypes = [np_, V, V, V, V, V, V, V, V, V, Z, V]
+        L.pilc_adamw_step.argtypes = [C.POINTER(pilc_adamw_params), C.POINTER(pilc_adamw_tensor), C.c_uint32, V]
+        L.pilc_adamw_values.argtypes = [V, V, C.c_uint64, C.c_int, V, V]
+        for f in (L.pilc_logprobs_workspace_size, L.pilc_logprobs, L.pilc_logprobs_grad, L.pilc_logprobs_train,
+                  L.pilc_norm_workspace_size, L.pilc_norm_forward, L.pilc_norm_backward, L.pilc_adamw_step,
+                  L.pilc_adamw_values):
+            f.restype = C.c_int
         _lib = L
     return _lib
 
@@ -395,4 +435,216 @@ def pilc_mix_decode(geom: pilc_geom, num_comp: int, coded, coded_bytes: int, mu,
                                _stream_handle(stream))
     if check and rc != PILC_OK:
         raise PilcError(rc, "pilc_mix_decode")
+    return rc
+
+
+# ---- fitting the laws ------------------------------------------------------------------------
+# These calls enqueue their kernels on the stream and return; see include/pilc.h for what each computes.
+_VALUES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_SYMBOLS = {torch.uint8: 0, torch.int32: 1, torch.int64: 2}
+
+
+def _on_device(t: torch.Tensor, what: str) -> None:
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise TypeError("%s must be on the current device" % what)
+
+
+def _vector(t: Optional[torch.Tensor], dtype, count: int, what: str) -> Optional[int]:
+    """The address of `count` dense values on the device, or None for None."""
+    if t is None:
+        return None
+    _on_device(t, what)
+    if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+        raise TypeError("%s must be %d contiguous values of %s" % (what, count, dtype))
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, dtype, shape, what: str) -> Tuple[int, int]:
+    """(address, elements from row to row) of a matrix whose rows are dense."""
+    _on_device(t, what)
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TypeError("%s must be %s rows of %s with dense rows" % (what, tuple(shape), dtype))
+    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if stride < t.shape[1]:
+        raise TypeError("%s: rows overlap" % what)
+    return t.data_ptr(), stride
+
+
+def _logits(logits: torch.Tensor, targets: Optional[torch.Tensor], top: int):
+    if logits.dim() != 2 or logits.dtype not in _VALUES:
+        raise TypeError("logits must be a matrix of float32, bfloat16 or float16")
+    ptr, stride = _rows(logits, logits.dtype, logits.shape, "logits")
+    if targets is not None and targets.dtype not in _SYMBOLS:
+        raise TypeError("targets must be uint8, int32 or int64")
+    rows, num_sym = logits.shape
+    shape = pilc_logits_shape(rows, num_sym, stride, _VALUES[logits.dtype], _SYMBOLS[targets.dtype] if targets is not None else 0, top)
+    return shape, ptr, _vector(targets, targets.dtype if targets is not None else None, rows, "targets")
+
+
+def pilc_logprobs_workspace_size(rows: int, num_sym: int, top: int = 0) -> int:
+    """Bytes of workspace that pilc_logprobs and pilc_logprobs_train need for any type of logits."""
+    n = C.c_size_t(0)
+    shape = pilc_logits_shape(int(rows), int(num_sym), int(num_sym), 0, 0, int(top))
+    rc = lib().pilc_logprobs_workspace_size(C.byref(shape), C.byref(n))
+    if rc != PILC_OK:
+        raise PilcError(rc, "pilc_logprobs_workspace_size")
+    return int(n.value)
+
+
+def _workspace(workspace: torch.Tensor) -> Tuple[int, int]:
+    return _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel()
+
+
+def pilc_logprobs(logits, targets=None, logp=None, entropy=None, lse=None, top_sym=None, top_logp=None, *, workspace,
+                  stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """ln p of the targets, entropy, ln of the sum and the most likely symbols of each row; what is None is not wanted.
+    logits [rows, num_sym], its rows dense; top_sym int32 and top_logp float32 [rows, top]; the rest [rows]."""
+    top = 0 if top_sym is None else top_sym.shape[-1]
+    shape, x, t = _logits(logits, targets, top)
+    rows = shape.rows
+    rc = lib().pilc_logprobs(C.byref(shape), x, t, _vector(logp, torch.float32, rows, "logp"),
+                             _vector(entropy, torch.float32, rows, "entropy"), _vector(lse, torch.float32, rows, "lse"),
+                             _vector(top_sym, torch.int32, rows * top, "top_sym"),
+                             _vector(top_logp, torch.float32, rows * top, "top_logp"), *_workspace(workspace), _stream_handle(stream))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_logprobs")
+    return rc
+
+
+def pilc_logprobs_grad(logits, targets, lse, up_logp, grad, entropy=None, up_entropy=None,
+                       stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """grad = gradient of sum(up_logp * logp) + sum(up_entropy * entropy) by the logits; grad may be the logits."""
+    shape, x, t = _logits(logits, targets, 0)
+    rows = shape.rows
+    g, g_stride = _rows(grad, logits.dtype, logits.shape, "grad")
+    rc = lib().pilc_logprobs_grad(C.byref(shape), x, t, _vector(lse, torch.float32, rows, "lse"),
+                                  _vector(entropy, torch.float32, rows, "entropy"), _vector(up_logp, torch.float32, rows, "up_logp"),
+                                  _vector(up_entropy, torch.float32, rows, "up_entropy"), g, g_stride, _stream_handle(stream))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_logprobs_grad")
+    return rc
+
+
+def pilc_logprobs_train(logits, targets, up_logp, logp, grad, entropy=None, lse=None, up_entropy=None, *, workspace,
+                        stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """pilc_logprobs (without alternatives) and pilc_logprobs_grad in one call."""
+    shape, x, t = _logits(logits, targets, 0)
+    rows = shape.rows
+    g, g_stride = _rows(grad, logits.dtype, logits.shape, "grad")
+    rc = lib().pilc_logprobs_train(C.byref(shape), x, t, _vector(up_logp, torch.float32, rows, "up_logp"),
+                                   _vector(up_entropy, torch.float32, rows, "up_entropy"), _vector(logp, torch.float32, rows, "logp"),
+                                   _vector(entropy, torch.float32, rows, "entropy"), _vector(lse, torch.float32, rows, "lse"),
+                                   g, g_stride, *_workspace(workspace), _stream_handle(stream))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_logprobs_train")
+    return rc
+
+
+def _norm_weights(x, *weights):
+    kinds = {w.dtype for w in weights if w is not None}
+    if x.dim() != 2 or x.dtype not in _VALUES or len(kinds) > 1 or not kinds <= {x.dtype, torch.float32}:
+        raise TypeError("x must be a matrix of float32, bfloat16 or float16, weight and bias of its type or float32")
+    return kinds.pop() if kinds else x.dtype
+
+
+def pilc_norm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5,
+                      stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """y = (x - mean) * rstd * weight + bias over each row of x [rows, width]; weight, bias None: 1 and 0."""
+    kind = _norm_weights(x, weight, bias)
+    rows, width = x.shape
+    xp, xs = _rows(x, x.dtype, x.shape, "x")
+    yp, ys = _rows(y, x.dtype, x.shape, "y")
+    shape = pilc_norm_shape(rows, width, xs, ys, 0, _VALUES[x.dtype], _VALUES[kind], eps)
+    rc = lib().pilc_norm_forward(C.byref(shape), xp, _vector(weight, kind, width, "weight"), _vector(bias, kind, width, "bias"), yp,
+                                 _vector(mean, torch.float32, rows, "mean"), _vector(rstd, torch.float32, rows, "rstd"),
+                                 _stream_handle(stream))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_norm_forward")
+    return rc
+
+
+def pilc_norm_workspace_size(rows: int, width: int) -> int:
+    """Bytes of workspace that pilc_norm_backward needs for any types."""
+    n = C.c_size_t(0)
+    shape = pilc_norm_shape(int(rows), int(width), int(width), int(width), int(width), 0, 0, 0.0)
+    rc = lib().pilc_norm_workspace_size(C.byref(shape), C.byref(n))
+    if rc != PILC_OK:
+        raise PilcError(rc, "pilc_norm_workspace_size")
+    return int(n.value)
+
+
+def pilc_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, *, workspace,
+                       stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """Gradients of pilc_norm_forward by x, weight and bias; what is None is not wanted.  dx may be dy."""
+    kind = _norm_weights(x, weight, dweight, dbias)
+    rows, width = x.shape
+    xp, xs = _rows(x, x.dtype, x.shape, "x")
+    dyp, dys = _rows(dy, x.dtype, x.shape, "dy")
+    dxp, dxs = _rows(dx, x.dtype, x.shape, "dx") if dx is not None else (None, width)
+    shape = pilc_norm_shape(rows, width, xs, dys, dxs, _VALUES[x.dtype], _VALUES[kind], 0.0)
+    rc = lib().pilc_norm_backward(C.byref(shape), dyp, xp, _vector(weight, kind, width, "weight"),
+                                  _vector(mean, torch.float32, rows, "mean"), _vector(rstd, torch.float32, rows, "rstd"), dxp,
+                                  _vector(dweight, kind, width, "dweight"), _vector(dbias, kind, width, "dbias"),
+                                  *_workspace(workspace), _stream_handle(stream))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_norm_backward")
+    return rc
+
+
+class AdamwTensors:
+    """The tensors of an AdamW step as pilc_adamw_step takes them; holds them, so that they stay where they are."""
+
+    def __init__(self, records, param_type: int, grad_type: int, state_bits: int, device: int, held):
+        self.records, self.held = records, held
+        self.param_type, self.grad_type, self.state_bits, self.device = param_type, grad_type, state_bits, device
+
+
+def make_adamw_tensors(params, grads, ms, vs, m_scales=None, v_scales=None, lr_mults=None, decay=0.0) -> AdamwTensors:
+    """Lists of dense device tensors, one entry a tensor.  Parameters share a type, gradients too.  ms and vs are float32,
+    or uint8 codes with m_scales and v_scales (uint8, one for each 256 values, the last ones maybe fewer).  decay: one
+    number or one a tensor.  Made once and used for every step as long as the tensors stay the same ones."""
+    n = len(params)
+    state = torch.float32 if m_scales is None else torch.uint8
+    lists = [params, grads, ms, vs] + ([] if m_scales is None and v_scales is None else [m_scales, v_scales])
+    if n == 0 or any(k is None or len(k) != n for k in lists):
+        raise TypeError("as many gradients and states as parameters, one at least")
+    p_type, g_type = params[0].dtype, grads[0].dtype
+    if p_type not in _VALUES or g_type not in _VALUES:
+        raise TypeError("parameters and gradients must be float32, bfloat16 or float16")
+    decays = [float(decay)] * n if isinstance(decay, (int, float)) else [float(d) for d in decay]
+    mults = [1.0] * n if lr_mults is None else [float(m) for m in lr_mults]
+    if len(decays) != n or len(mults) != n:
+        raise TypeError("one decay and one lr_mult a tensor")
+    records = (pilc_adamw_tensor * n)()
+    for i in range(n):
+        count = params[i].numel()
+        scales = [None, None] if m_scales is None else [
+            _vector(s[i], torch.uint8, -(-count // 256), "scales") for s in (m_scales, v_scales)]
+        records[i] = pilc_adamw_tensor(_vector(params[i], p_type, count, "params"), _vector(grads[i], g_type, count, "grads"),
+                                       _vector(ms[i], state, count, "ms"), _vector(vs[i], state, count, "vs"), *scales, count,
+                                       mults[i], decays[i])
+    return AdamwTensors(records, _VALUES[p_type], _VALUES[g_type], 32 if m_scales is None else 8, params[0].device.index,
+                        [list(k) for k in lists])
+
+
+def pilc_adamw_step(tensors: AdamwTensors, lr: float, beta1: float, beta2: float, eps: float, step: int,
+                    grad_scale: float = 1.0, dither: int = 0, stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """One AdamW step, in place.  dither: with states in 8 bits another number every step, say the step's own."""
+    if tensors.device != torch.cuda.current_device():
+        raise TypeError("tensors must be on the current device")
+    par = pilc_adamw_params(lr, beta1, beta2, eps, grad_scale, step, tensors.param_type, tensors.grad_type, tensors.state_bits,
+                            dither & 0xFFFFFFFF)
+    rc = lib().pilc_adamw_step(C.byref(par), tensors.records, len(tensors.records), _stream_handle(stream))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_adamw_step")
+    return rc
+
+
+def pilc_adamw_values(codes, scales, values, signed: bool, stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """values (float32) = what the codes of an 8-bit state stand for; signed for m, not for v."""
+    n = codes.numel()
+    rc = lib().pilc_adamw_values(_vector(codes, torch.uint8, n, "codes"), _vector(scales, torch.uint8, -(-n // 256), "scales"), n,
+                                 1 if signed else 0, _vector(values, torch.float32, n, "values"), _stream_handle(stream))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_adamw_values")
     return rc

@@ -9,7 +9,7 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libpilc.so")
-SOURCES = [os.path.join(CSRC, "pilc.hip")]
+SOURCES = [os.path.join(CSRC, "pilc.hip"), os.path.join(CSRC, "pilc_fit.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",

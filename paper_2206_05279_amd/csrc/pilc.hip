@@ -22,6 +22,7 @@
 
 #include "../../include/pilc.h"
 #include "pilc_device.hpp"
+#include "pilc_host.hpp"
 
 namespace pilc {
 
@@ -614,7 +615,7 @@ static std::atomic<int> g_ansai_decode_waves{0};  // 0: chosen per call
 static std::atomic<unsigned long long> g_one_pass_wait{0};
 static std::atomic<int> g_one_pass_withhold{0};
 
-static uint32_t compute_units()
+uint32_t compute_units()
 {
     int dev = 0, cus = 0;
     if (hipGetDevice(&dev) != hipSuccess ||
@@ -629,17 +630,11 @@ thread_local const char *t_timing_name[16];
 thread_local int t_timing_count = 0;
 static std::atomic<int> g_timing_enabled{0};
 
-static int hip_fail(hipError_t e, const char *what)
+int hip_fail(hipError_t e, const char *what)
 {
     snprintf(t_hip_error, sizeof(t_hip_error), "%s: %s", what, hipGetErrorString(e));
     return PILC_E_HIP;
 }
-
-#define HIP_TRY(expr)                                   \
-    do {                                                \
-        hipError_t e_ = (expr);                         \
-        if (e_ != hipSuccess) return hip_fail(e_, #expr); \
-    } while (0)
 
 static std::mutex g_table_mutex;
 static bool g_table_ready[64] = {false};
