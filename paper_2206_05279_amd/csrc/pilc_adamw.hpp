@@ -5,16 +5,28 @@ namespace pilc {
 
 constexpr uint32_t kStateBlock = 256;  // values that share a scale
 
-struct AdamwArgs {
+// What a launch works on goes to the kernel by value, so that nothing has to be copied to the GPU beforehand and
+// nothing kept: up to 56 tensors, near 4 KB.
+constexpr int kAdamwTensors = 56;
+
+struct AdamwTensor {
     void *param;
     const void *grad;
     void *m, *v;
     uint8_t *m_scale, *v_scale;
-    uint64_t count, first_block;  // blocks of 256 of the tensors before this one
-    float keep, rate;             // 1 - lr decay, lr / (1 - beta1^t)
-    float b1, b1_rest, b2, b2_rest, grad_scale, root_scale, eps;
-    uint32_t dither;
+    uint64_t count;
+    float keep, rate;  // 1 - lr decay, lr / (1 - beta1^t)
 };
+
+struct AdamwArgs {
+    AdamwTensor tensor[kAdamwTensors];
+    uint32_t chunk_end[kAdamwTensors];  // chunks of the launch's tensors up to and with this one
+    uint32_t block[kAdamwTensors];      // blocks of 256 of the launch's tensors before this one
+    uint64_t first_block;               // and of those before the launch's
+    float b1, b1_rest, b2, b2_rest, grad_scale, root_scale, eps;
+    uint32_t dither, num;
+};
+static_assert(sizeof(AdamwArgs) <= 4096, "what a launch may carry");
 
 struct Moments {
     float m, v;
@@ -30,9 +42,9 @@ __device__ __forceinline__ Moments move_moments(const AdamwArgs &a, Moments s, f
     return {m0 + m1, v0 + v1};
 }
 
-__device__ __forceinline__ float move_param(const AdamwArgs &a, float p, Moments s)
+__device__ __forceinline__ float move_param(const AdamwArgs &a, const AdamwTensor &t, float p, Moments s)
 {
-    return p * a.keep - a.rate * s.m / (sqrtf(s.v) * a.root_scale + a.eps);
+    return p * t.keep - t.rate * s.m / (sqrtf(s.v) * a.root_scale + a.eps);
 }
 
 template <bool kSigned>
@@ -71,47 +83,122 @@ __device__ __forceinline__ uint32_t hash_of(uint64_t number, uint32_t dither)
     return h ^ (h >> 16);
 }
 
-template <class P, class G>
-__global__ __launch_bounds__(256) void k_adamw(AdamwArgs a)
+// Which tensor a workgroup's chunk is of: every lane compares with one tensor's end, and how many ends lie before
+// the chunk is counted over the wavefront.
+__device__ __forceinline__ uint32_t tensor_of(const AdamwArgs &a, uint32_t chunk)
 {
-    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < a.count; i += gridDim.x * 256ull) {
-        float *m = (float *)a.m + i, *v = (float *)a.v + i;
-        const Moments s = move_moments(a, {*m, *v}, widen(((const G *)a.grad)[i]));
-        P *p = (P *)a.param + i;
-        *p = (P)move_param(a, widen(*p), s);
-        *m = s.m;
-        *v = s.v;
+    const uint32_t lane = threadIdx.x & 63;
+    const bool before = lane < a.num && a.chunk_end[lane < kAdamwTensors ? lane : 0] <= chunk;
+    return (uint32_t)__builtin_popcountll(__ballot(before));
+}
+
+constexpr int kAdamwThreads = 256;
+constexpr uint32_t kAdamwChunk = 4096;  // values a workgroup takes
+
+// States in 32 bits: four values a thread at a time.
+template <class P, class G>
+__global__ __launch_bounds__(kAdamwThreads) void k_adamw(AdamwArgs a)
+{
+    constexpr int kEach = 4;
+    const uint32_t k = __builtin_amdgcn_readfirstlane(tensor_of(a, blockIdx.x));
+    const AdamwTensor &t = a.tensor[k];
+    const uint64_t begin = (uint64_t)(blockIdx.x - (k ? a.chunk_end[k - 1] : 0)) * kAdamwChunk;
+    P *param = (P *)t.param + begin;
+    const G *grad = (const G *)t.grad + begin;
+    float *ms = (float *)t.m + begin, *vs = (float *)t.v + begin;
+    const uint32_t left = (uint32_t)min((uint64_t)kAdamwChunk, t.count - begin);
+    const bool aligned = (((uintptr_t)param & (sizeof(P) * kEach - 1)) | ((uintptr_t)grad & (sizeof(G) * kEach - 1)) |
+                          (((uintptr_t)ms | (uintptr_t)vs) & 15)) == 0;
+#pragma unroll 2
+    for (uint32_t i = threadIdx.x * kEach; i < left; i += kAdamwThreads * kEach) {
+        const int valid = (int)min((uint32_t)kEach, left - i);
+        const bool whole = aligned && valid == kEach;
+        float p[kEach], g[kEach], m[kEach], v[kEach];
+        load_pack<kEach>(param + i, whole, valid, p);
+        load_pack<kEach>(grad + i, whole, valid, g);
+        load_pack<kEach>(ms + i, whole, valid, m);
+        load_pack<kEach>(vs + i, whole, valid, v);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const Moments s = move_moments(a, {m[j], v[j]}, g[j]);
+            p[j] = move_param(a, t, p[j], s);
+            m[j] = s.m, v[j] = s.v;
+        }
+        store_pack<kEach>(param + i, whole, valid, p);
+        store_pack<kEach>(ms + i, whole, valid, m);
+        store_pack<kEach>(vs + i, whole, valid, v);
     }
 }
 
-// A block of 256 values a workgroup at a time.
+// States in 8 bits: eight values a thread, half a wavefront a block of 256.
 template <class P, class G>
-__global__ __launch_bounds__(256) void k_adamw_bytes(AdamwArgs a)
+__global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
 {
-    __shared__ int room[4];
-    const uint64_t blocks = (a.count + kStateBlock - 1) / kStateBlock;
-    for (uint64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
-        const uint64_t i = b * kStateBlock + threadIdx.x;
-        const bool in = i < a.count;
-        uint8_t *m = (uint8_t *)a.m + i, *v = (uint8_t *)a.v + i;
-        Moments s = {0.0f, 0.0f};
-        if (in) {
-            s = {Coding<true>::decode(*m, a.m_scale[b]), Coding<false>::decode(*v, a.v_scale[b])};
-            s = move_moments(a, s, widen(((const G *)a.grad)[i]));
-            P *p = (P *)a.param + i;
-            *p = (P)move_param(a, widen(*p), s);
+    constexpr int kEach = 8;
+    const uint32_t k = __builtin_amdgcn_readfirstlane(tensor_of(a, blockIdx.x));
+    const AdamwTensor &t = a.tensor[k];
+    const uint32_t chunk = blockIdx.x - (k ? a.chunk_end[k - 1] : 0);
+    const uint64_t begin = (uint64_t)chunk * kAdamwChunk;
+    P *param = (P *)t.param + begin;
+    const G *grad = (const G *)t.grad + begin;
+    uint8_t *ms = (uint8_t *)t.m + begin, *vs = (uint8_t *)t.v + begin;
+    constexpr uint32_t kBlocks = kAdamwChunk / kStateBlock;
+    uint8_t *m_scale = t.m_scale + (uint64_t)chunk * kBlocks, *v_scale = t.v_scale + (uint64_t)chunk * kBlocks;
+    // the number of the chunk's first value
+    const uint64_t number = (a.first_block + a.block[k] + (uint64_t)chunk * kBlocks) * kStateBlock;
+    const uint32_t left = (uint32_t)min((uint64_t)kAdamwChunk, t.count - begin);
+    const bool aligned = (((uintptr_t)param | (uintptr_t)grad) & 15) == 0 && (((uintptr_t)ms | (uintptr_t)vs) & 7) == 0;
+    for (uint32_t i = threadIdx.x * kEach; i < left + kStateBlock - 1 - (left - 1) % kStateBlock; i += kAdamwThreads * kEach) {
+        const int valid = i < left ? (int)min((uint32_t)kEach, left - i) : 0;
+        const bool whole = aligned && valid == kEach;
+        const uint32_t b = i / kStateBlock;
+        float p[kEach], g[kEach], m[kEach], v[kEach];
+        Pack<uint8_t, kEach> mc = {}, vc = {};
+        load_pack<kEach>(param + i, whole, valid, p);
+        load_pack<kEach>(grad + i, whole, valid, g);
+        if (whole) {
+            mc = *(const Pack<uint8_t, kEach> *)(ms + i);
+            vc = *(const Pack<uint8_t, kEach> *)(vs + i);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (j < valid) mc.v[j] = ms[i + j], vc.v[j] = vs[i + j];
         }
-        const int em = max(1, block_reduce<4>((int)(__float_as_uint(s.m) >> 23 & 255), Max(), room));
-        const int ev = max(1, block_reduce<4>((int)(__float_as_uint(s.v) >> 23 & 255), Max(), room));
-        if (in) {
-            const uint32_t h = hash_of((a.first_block + b) * kStateBlock + threadIdx.x, a.dither);
-            *m = (uint8_t)Coding<true>::encode(s.m, em, h & 0xFFFF);
-            *v = (uint8_t)Coding<false>::encode(s.v, ev, h >> 16);
+        int em = m_scale[b], ev = v_scale[b];
+        uint32_t m_most = 0, v_most = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            Moments s = {Coding<true>::decode(mc.v[j], em), Coding<false>::decode(vc.v[j], ev)};
+            s = move_moments(a, s, g[j]);
+            if (j >= valid) s = {0.0f, 0.0f};
+            p[j] = move_param(a, t, p[j], s);
+            m[j] = s.m, v[j] = s.v;
+            m_most = max(m_most, __float_as_uint(s.m) & 0x7FFFFFFFu);
+            v_most = max(v_most, __float_as_uint(s.v) & 0x7FFFFFFFu);
         }
-        if (threadIdx.x == 0) {
-            a.m_scale[b] = (uint8_t)em;
-            a.v_scale[b] = (uint8_t)ev;
+        store_pack<kEach>(param + i, whole, valid, p);
+        // the block is half a wavefront's; the other half may be in another block, but not outside the loop
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) {
+            m_most = max(m_most, (uint32_t)__shfl_xor((int)m_most, d, 64));
+            v_most = max(v_most, (uint32_t)__shfl_xor((int)v_most, d, 64));
         }
+        em = max(1, (int)(m_most >> 23)), ev = max(1, (int)(v_most >> 23));
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const uint32_t h = hash_of(number + i + j, a.dither);
+            mc.v[j] = (uint8_t)Coding<true>::encode(m[j], em, h & 0xFFFF);
+            vc.v[j] = (uint8_t)Coding<false>::encode(v[j], ev, h >> 16);
+        }
+        if (whole) {
+            *(Pack<uint8_t, kEach> *)(ms + i) = mc;
+            *(Pack<uint8_t, kEach> *)(vs + i) = vc;
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (j < valid) ms[i + j] = mc.v[j], vs[i + j] = vc.v[j];
+        }
+        if (i % kStateBlock == 0) m_scale[b] = (uint8_t)em, v_scale[b] = (uint8_t)ev;
     }
 }
 
@@ -121,6 +208,9 @@ __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *code, const
     for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < count; i += gridDim.x * 256ull)
         values[i] = Coding<kSigned>::decode(code[i], scale[i / kStateBlock]);
 }
+
+constexpr uint32_t kAdamwMostChunks = 1u << 20;  // a launch has fewer than 2^32 threads
+static uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
 static bool adamw_ok(const pilc_adamw_params *h, const pilc_adamw_tensor *t, uint32_t num)
 {
@@ -156,28 +246,44 @@ int pilc_adamw_step(const pilc_adamw_params *params_host, const pilc_adamw_tenso
     a.grad_scale = (float)h.grad_scale, a.eps = (float)h.eps, a.dither = h.dither;
     const double c1 = 1.0 - std::pow(h.beta1, (double)h.step), c2 = 1.0 - std::pow(h.beta2, (double)h.step);
     a.root_scale = (float)(1.0 / std::sqrt(c2));
-    for (uint32_t k = 0; k < num_tensors; ++k) {
-        const pilc_adamw_tensor &x = tensors_host[k];
-        if (x.count == 0) continue;
-        a.param = x.param, a.grad = x.grad, a.m = x.m, a.v = x.v, a.m_scale = x.m_scale, a.v_scale = x.v_scale, a.count = x.count;
-        const double lr = h.lr * x.lr_mult;
-        a.keep = (float)(1.0 - lr * x.decay), a.rate = (float)(lr / c1);
-        const uint64_t blocks = (x.count + 255) / 256;
-        const uint32_t grid = (uint32_t)std::min<uint64_t>(blocks, 1u << 20);
+    uint64_t blocks = 0;
+    uint32_t chunks = 0;
+    const auto launch = [&]() -> int {
+        if (a.num == 0) return PILC_OK;
         const int rc = by_type(h.param_type, [&](auto *p) {
-            by_type(h.grad_type, [&](auto *g) {
+            by_value_type(h.grad_type, [&](auto *g) {
                 using P = std::remove_pointer_t<decltype(p)>;
                 using G = std::remove_pointer_t<decltype(g)>;
                 if (h.state_bits == 32)
-                    k_adamw<P, G><<<grid, 256, 0, (hipStream_t)hip_stream>>>(a);
+                    k_adamw<P, G><<<chunks, kAdamwThreads, 0, (hipStream_t)hip_stream>>>(a);
                 else
-                    k_adamw_bytes<P, G><<<grid, 256, 0, (hipStream_t)hip_stream>>>(a);
+                    k_adamw_bytes<P, G><<<chunks, kAdamwThreads, 0, (hipStream_t)hip_stream>>>(a);
             });
         });
-        if (rc != PILC_OK) return rc;
-        a.first_block += blocks;
+        a.num = 0, chunks = 0, a.first_block = blocks;
+        return rc;
+    };
+    for (uint32_t k = 0; k < num_tensors; ++k) {
+        pilc_adamw_tensor x = tensors_host[k];
+        const double lr = h.lr * x.lr_mult;
+        while (x.count) {  // a tensor of more chunks than a launch has room for goes on in the next
+            const uint64_t room = kAdamwMostChunks - chunks, wanted = ceil_div(x.count, kAdamwChunk);
+            const uint64_t here = std::min(room, wanted), count = here < wanted ? here * kAdamwChunk : x.count;
+            AdamwTensor &t = a.tensor[a.num];
+            t = {x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, count, (float)(1.0 - lr * x.decay), (float)(lr / c1)};
+            a.block[a.num] = (uint32_t)(blocks - a.first_block);
+            chunks += (uint32_t)here, blocks += ceil_div(count, kStateBlock);
+            a.chunk_end[a.num++] = chunks;
+            x.count -= count;
+            x.param = (char *)x.param + count * value_bytes(h.param_type);
+            x.grad = (const char *)x.grad + count * value_bytes(h.grad_type);
+            x.m = (char *)x.m + count * h.state_bits / 8, x.v = (char *)x.v + count * h.state_bits / 8;
+            if (h.state_bits == 8) x.m_scale += count / kStateBlock, x.v_scale += count / kStateBlock;
+            if (a.num == kAdamwTensors || chunks == kAdamwMostChunks)
+                if (const int rc = launch(); rc != PILC_OK) return rc;
+        }
     }
-    return PILC_OK;
+    return launch();
 }
 
 int pilc_adamw_values(const uint8_t *code_dev, const uint8_t *scale_dev, uint64_t count, int is_signed, float *values_dev, void *hip_stream)

@@ -10,14 +10,42 @@ namespace pilc {
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
 
-// kBytes of T from an address that is a multiple of kBytes, as one access.
+// kCount of T as one access; the address is a multiple of its size, or of 16 bytes if that is less.
 template <class T, int kCount>
-struct alignas(sizeof(T) * kCount) Pack {
+struct alignas(sizeof(T) * kCount < 16 ? sizeof(T) * kCount : 16) Pack {
     T v[kCount];
 };
 
 template <class T>
 __device__ __forceinline__ float widen(T v) { return (float)v; }
+
+// `valid` of kCount values from p, 0 behind them.  whole: all are there and p is aligned for a Pack.
+template <int kCount, class T>
+__device__ __forceinline__ void load_pack(const T *p, bool whole, int valid, float (&out)[kCount])
+{
+    if (whole) {
+        const Pack<T, kCount> t = *(const Pack<T, kCount> *)p;
+#pragma unroll
+        for (int k = 0; k < kCount; ++k) out[k] = widen(t.v[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < kCount; ++k) out[k] = k < valid ? widen(p[k]) : 0.0f;
+    }
+}
+template <int kCount, class T>
+__device__ __forceinline__ void store_pack(T *p, bool whole, int valid, const float (&in)[kCount])
+{
+    if (whole) {
+        Pack<T, kCount> t;
+#pragma unroll
+        for (int k = 0; k < kCount; ++k) t.v[k] = (T)in[k];
+        *(Pack<T, kCount> *)p = t;
+    } else {
+#pragma unroll
+        for (int k = 0; k < kCount; ++k)
+            if (k < valid) p[k] = (T)in[k];
+    }
+}
 
 constexpr float kInf = __builtin_inff();
 constexpr float kLog2e = 1.44269504088896340736f;

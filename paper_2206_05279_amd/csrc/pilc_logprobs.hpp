@@ -157,13 +157,18 @@ static bool logits_in_ok(const pilc_logits_shape *s, const void *logits, const v
 static size_t logits_workspace(const pilc_logits_shape &s) { return 256; }
 
 template <class Launch>
-static int by_type(uint32_t type, Launch launch)
+static void by_value_type(uint32_t type, Launch launch)
 {
     switch (type) {
     case PILC_F32: launch((float *)nullptr); break;
     case PILC_BF16: launch((bf16_t *)nullptr); break;
     default: launch((f16_t *)nullptr); break;
     }
+}
+template <class Launch>
+static int by_type(uint32_t type, Launch launch)
+{
+    by_value_type(type, launch);
     HIP_TRY(hipGetLastError());
     return PILC_OK;
 }
