@@ -205,8 +205,25 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
 template <bool kSigned>
 __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *code, const uint8_t *scale, uint64_t count, float *values)
 {
-    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < count; i += gridDim.x * 256ull)
-        values[i] = Coding<kSigned>::decode(code[i], scale[i / kStateBlock]);
+    constexpr int kEach = 4;
+    const bool aligned = ((uintptr_t)code & 3) == 0 && ((uintptr_t)values & 15) == 0;
+    for (uint64_t i = (blockIdx.x * 256ull + threadIdx.x) * kEach; i < count; i += gridDim.x * 256ull * kEach) {
+        const int valid = (int)min((uint64_t)kEach, count - i);
+        const bool whole = aligned && valid == kEach;
+        Pack<uint8_t, kEach> c = {};
+        if (whole) {
+            c = *(const Pack<uint8_t, kEach> *)(code + i);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j)
+                if (j < valid) c.v[j] = code[i + j];
+        }
+        const int e = scale[i / kStateBlock];  // of all four: 4 divides a block
+        float x[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) x[j] = Coding<kSigned>::decode(c.v[j], e);
+        store_pack<kEach>(values + i, whole, valid, x);
+    }
 }
 
 constexpr uint32_t kAdamwMostChunks = 1u << 20;  // a launch has fewer than 2^32 threads
@@ -290,7 +307,7 @@ int pilc_adamw_values(const uint8_t *code_dev, const uint8_t *scale_dev, uint64_
 {
     if (count == 0) return PILC_OK;
     if (!code_dev || !scale_dev || !values_dev || !aligned_to(values_dev, 4) || count > (1ull << 48)) return PILC_E_ARG;
-    const uint32_t grid = (uint32_t)std::min<uint64_t>((count + 255) / 256, 1u << 20);
+    const uint32_t grid = (uint32_t)std::min<uint64_t>(ceil_div(count, 1024), 1u << 20);
     if (is_signed)
         k_adamw_values<true><<<grid, 256, 0, (hipStream_t)hip_stream>>>(code_dev, scale_dev, count, values_dev);
     else
