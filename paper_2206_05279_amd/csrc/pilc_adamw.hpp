@@ -42,34 +42,45 @@ __device__ __forceinline__ Moments move_moments(const AdamwArgs &a, Moments s, f
     return {m0 + m1, v0 + v1};
 }
 
+// The weight's move needs no last bit: the root and the quotient are the hardware's, one unit off each.  Its root
+// takes no denormal numbers, so small ones are brought up.
 __device__ __forceinline__ float move_param(const AdamwArgs &a, const AdamwTensor &t, float p, Moments s)
 {
-    return p * t.keep - t.rate * s.m / (sqrtf(s.v) * a.root_scale + a.eps);
+    const bool small = s.v < 0x1p-96f;
+    float root = __builtin_amdgcn_sqrtf(small ? s.v * 0x1p64f : s.v);
+    root = small ? root * 0x1p-32f : root;
+    return p * t.keep - t.rate * s.m * __builtin_amdgcn_rcpf(root * a.root_scale + a.eps);
 }
 
+// States in 8 bits.  Everything but the last rounding is exact: scales are powers of two, and where scaling a value
+// would lose bits of it the constant that is added leaves nothing of those.
 template <bool kSigned>
 struct Coding {
     static constexpr int kOctaves = kSigned ? 15 : 31;
     static constexpr uint32_t kBase = (127 - kOctaves) << 3;
-    __device__ static float step() { return __uint_as_float((127 - kOctaves) << 23); }
 
-    __device__ static uint32_t encode(float x, int exponent, uint32_t noise)
+    // 2^(e-127) for decode, NaN for a block that is not finite
+    __device__ static float scale_of(uint32_t e) { return __uint_as_float(e == 255 ? 0x7FC00000u : e == 0 ? 0x00400000u : e << 23); }
+    // 2^(126-e) for encode
+    __device__ static float inverse_of(uint32_t e) { return ldexpf(1.0f, 126 - (int)e); }
+
+    // byte k of a word of codes
+    __device__ static float decode(uint32_t word, int k, float scale)
     {
 #pragma clang fp contract(off)
-        const float y = ldexpf(fabsf(x), 126 - exponent) + step();
-        const uint32_t code = ((__float_as_uint(y) + (noise << 4) + 8) >> 20) - kBase;
-        if constexpr (kSigned)
-            return code | (x < 0.0f ? 128u : 0u);
-        else
-            return x > 0.0f && code == 0 ? 1u : code;
+        const uint32_t size = word >> (8 * k) & (kSigned ? 127 : 255);
+        // twice the number that is coded, less twice the constant
+        const float x = (__uint_as_float((size + kBase + 8) << 20) - __uint_as_float((128 - kOctaves) << 23)) * scale;
+        return kSigned ? __uint_as_float(__float_as_uint(x) ^ (word << (24 - 8 * k) & 0x80000000u)) : x;
     }
-    __device__ static float decode(uint32_t code, int exponent)
+    __device__ static uint32_t encode(float x, float inverse, uint32_t noise)
     {
-#pragma clang fp contract(off)
-        if (exponent == 255) return __builtin_nanf("");
-        const uint32_t size = kSigned ? code & 127 : code;
-        const float x = ldexpf(__uint_as_float((size + kBase) << 20) - step(), exponent - 126);
-        return kSigned && code > 127 ? -x : x;
+        const float y = __builtin_fmaf(fabsf(x), inverse, __uint_as_float((127 - kOctaves) << 23));
+        const uint32_t code = (__float_as_uint(y) + (noise << 4) + (8u - (kBase << 20))) >> 20;
+        if constexpr (kSigned)
+            return code | (__float_as_uint(x) >> 24 & 128u);
+        else
+            return max(code, min(__float_as_uint(x), 1u));
     }
 };
 
@@ -153,28 +164,28 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
         const bool whole = aligned && valid == kEach;
         const uint32_t b = i / kStateBlock;
         float p[kEach], g[kEach], m[kEach], v[kEach];
-        Pack<uint8_t, kEach> mc = {}, vc = {};
+        Pack<uint32_t, kEach / 4> mc = {}, vc = {};
         load_pack<kEach>(param + i, whole, valid, p);
         load_pack<kEach>(grad + i, whole, valid, g);
         if (whole) {
-            mc = *(const Pack<uint8_t, kEach> *)(ms + i);
-            vc = *(const Pack<uint8_t, kEach> *)(vs + i);
+            mc = *(const Pack<uint32_t, kEach / 4> *)(ms + i);
+            vc = *(const Pack<uint32_t, kEach / 4> *)(vs + i);
         } else {
 #pragma unroll
             for (int j = 0; j < kEach; ++j)
-                if (j < valid) mc.v[j] = ms[i + j], vc.v[j] = vs[i + j];
+                if (j < valid) mc.v[j / 4] |= (uint32_t)ms[i + j] << (8 * (j & 3)), vc.v[j / 4] |= (uint32_t)vs[i + j] << (8 * (j & 3));
         }
-        int em = m_scale[b], ev = v_scale[b];
+        const float m_unit = Coding<true>::scale_of(m_scale[b]), v_unit = Coding<false>::scale_of(v_scale[b]);
         uint32_t m_most = 0, v_most = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            Moments s = {Coding<true>::decode(mc.v[j], em), Coding<false>::decode(vc.v[j], ev)};
+            Moments s = {Coding<true>::decode(mc.v[j / 4], j & 3, m_unit), Coding<false>::decode(vc.v[j / 4], j & 3, v_unit)};
             s = move_moments(a, s, g[j]);
-            if (j >= valid) s = {0.0f, 0.0f};
+            if (!whole && j >= valid) s = {0.0f, 0.0f};
             p[j] = move_param(a, t, p[j], s);
             m[j] = s.m, v[j] = s.v;
             m_most = max(m_most, __float_as_uint(s.m) & 0x7FFFFFFFu);
-            v_most = max(v_most, __float_as_uint(s.v) & 0x7FFFFFFFu);
+            v_most = max(v_most, __float_as_uint(s.v));
         }
         store_pack<kEach>(param + i, whole, valid, p);
         // the block is half a wavefront's; the other half may be in another block, but not outside the loop
@@ -183,46 +194,56 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
             m_most = max(m_most, (uint32_t)__shfl_xor((int)m_most, d, 64));
             v_most = max(v_most, (uint32_t)__shfl_xor((int)v_most, d, 64));
         }
-        em = max(1, (int)(m_most >> 23)), ev = max(1, (int)(v_most >> 23));
+        const uint32_t em = max(1u, m_most >> 23), ev = max(1u, v_most >> 23 & 255);  // a NaN may have its sign set
+        const float m_inverse = Coding<true>::inverse_of(em), v_inverse = Coding<false>::inverse_of(ev);
+        mc = {}, vc = {};
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             const uint32_t h = hash_of(number + i + j, a.dither);
-            mc.v[j] = (uint8_t)Coding<true>::encode(m[j], em, h & 0xFFFF);
-            vc.v[j] = (uint8_t)Coding<false>::encode(v[j], ev, h >> 16);
+            mc.v[j / 4] |= (Coding<true>::encode(m[j], m_inverse, h & 0xFFFF) & 255) << (8 * (j & 3));
+            vc.v[j / 4] |= (Coding<false>::encode(v[j], v_inverse, h >> 16) & 255) << (8 * (j & 3));
         }
         if (whole) {
-            *(Pack<uint8_t, kEach> *)(ms + i) = mc;
-            *(Pack<uint8_t, kEach> *)(vs + i) = vc;
+            *(Pack<uint32_t, kEach / 4> *)(ms + i) = mc;
+            *(Pack<uint32_t, kEach / 4> *)(vs + i) = vc;
         } else {
 #pragma unroll
             for (int j = 0; j < kEach; ++j)
-                if (j < valid) ms[i + j] = mc.v[j], vs[i + j] = vc.v[j];
+                if (j < valid) ms[i + j] = (uint8_t)(mc.v[j / 4] >> (8 * (j & 3))), vs[i + j] = (uint8_t)(vc.v[j / 4] >> (8 * (j & 3)));
         }
         if (i % kStateBlock == 0) m_scale[b] = (uint8_t)em, v_scale[b] = (uint8_t)ev;
     }
 }
 
+// Sixteen values a thread, four at a time: a thread that took four only would be done before the next ones could
+// be started (300 million values: 370 us, 4.0 TB/s).
+constexpr uint32_t kValuesChunk = 256 * 16;
 template <bool kSigned>
 __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *code, const uint8_t *scale, uint64_t count, float *values)
 {
     constexpr int kEach = 4;
     const bool aligned = ((uintptr_t)code & 3) == 0 && ((uintptr_t)values & 15) == 0;
-    for (uint64_t i = (blockIdx.x * 256ull + threadIdx.x) * kEach; i < count; i += gridDim.x * 256ull * kEach) {
-        const int valid = (int)min((uint64_t)kEach, count - i);
-        const bool whole = aligned && valid == kEach;
-        Pack<uint8_t, kEach> c = {};
-        if (whole) {
-            c = *(const Pack<uint8_t, kEach> *)(code + i);
-        } else {
+    for (uint64_t begin = (uint64_t)blockIdx.x * kValuesChunk; begin < count; begin += (uint64_t)gridDim.x * kValuesChunk) {
 #pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (j < valid) c.v[j] = code[i + j];
+        for (uint32_t part = 0; part < kValuesChunk; part += 256 * kEach) {
+            const uint64_t i = begin + part + threadIdx.x * kEach;
+            if (i >= count) break;
+            const int valid = (int)min((uint64_t)kEach, count - i);
+            const bool whole = aligned && valid == kEach;
+            uint32_t c = 0;
+            if (whole) {
+                c = *(const uint32_t *)(code + i);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kEach; ++j)
+                    if (j < valid) c |= (uint32_t)code[i + j] << (8 * j);
+            }
+            const float unit = Coding<kSigned>::scale_of(scale[i / kStateBlock]);  // of all four: 4 divides a block
+            float x[kEach];
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) x[j] = Coding<kSigned>::decode(c, j, unit);
+            store_pack<kEach>(values + i, whole, valid, x);
         }
-        const int e = scale[i / kStateBlock];  // of all four: 4 divides a block
-        float x[kEach];
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) x[j] = Coding<kSigned>::decode(c.v[j], e);
-        store_pack<kEach>(values + i, whole, valid, x);
     }
 }
 
@@ -307,7 +328,7 @@ int pilc_adamw_values(const uint8_t *code_dev, const uint8_t *scale_dev, uint64_
 {
     if (count == 0) return PILC_OK;
     if (!code_dev || !scale_dev || !values_dev || !aligned_to(values_dev, 4) || count > (1ull << 48)) return PILC_E_ARG;
-    const uint32_t grid = (uint32_t)std::min<uint64_t>(ceil_div(count, 1024), 1u << 20);
+    const uint32_t grid = (uint32_t)std::min<uint64_t>(ceil_div(count, kValuesChunk), 1u << 20);
     if (is_signed)
         k_adamw_values<true><<<grid, 256, 0, (hipStream_t)hip_stream>>>(code_dev, scale_dev, count, values_dev);
     else
