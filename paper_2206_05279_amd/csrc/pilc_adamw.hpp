@@ -120,10 +120,7 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw(AdamwArgs a)
     const uint32_t left = (uint32_t)min((uint64_t)kAdamwChunk, t.count - begin);
     const bool aligned = (((uintptr_t)param & (sizeof(P) * kEach - 1)) | ((uintptr_t)grad & (sizeof(G) * kEach - 1)) |
                           (((uintptr_t)ms | (uintptr_t)vs) & 15)) == 0;
-#pragma unroll 2
-    for (uint32_t i = threadIdx.x * kEach; i < left; i += kAdamwThreads * kEach) {
-        const int valid = (int)min((uint32_t)kEach, left - i);
-        const bool whole = aligned && valid == kEach;
+    const auto some = [&](uint32_t i, bool whole, int valid) {
         float p[kEach], g[kEach], m[kEach], v[kEach];
         load_pack<kEach>(param + i, whole, valid, p);
         load_pack<kEach>(grad + i, whole, valid, g);
@@ -138,6 +135,14 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw(AdamwArgs a)
         store_pack<kEach>(param + i, whole, valid, p);
         store_pack<kEach>(ms + i, whole, valid, m);
         store_pack<kEach>(vs + i, whole, valid, v);
+    };
+    if (aligned && left == kAdamwChunk) {
+        for (uint32_t i = threadIdx.x * kEach; i < kAdamwChunk; i += kAdamwThreads * kEach) some(i, true, kEach);
+    } else {
+        for (uint32_t i = threadIdx.x * kEach; i < left; i += kAdamwThreads * kEach) {
+            const int valid = (int)min((uint32_t)kEach, left - i);
+            some(i, aligned && valid == kEach, valid);
+        }
     }
 }
 
@@ -146,6 +151,7 @@ template <class P, class G>
 __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
 {
     constexpr int kEach = 8;
+    using Codes = Pack<uint32_t, kEach / 4>;
     const uint32_t k = __builtin_amdgcn_readfirstlane(tensor_of(a, blockIdx.x));
     const AdamwTensor &t = a.tensor[k];
     const uint32_t chunk = blockIdx.x - (k ? a.chunk_end[k - 1] : 0);
@@ -158,18 +164,18 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
     // the number of the chunk's first value
     const uint64_t number = (a.first_block + a.block[k] + (uint64_t)chunk * kBlocks) * kStateBlock;
     const uint32_t left = (uint32_t)min((uint64_t)kAdamwChunk, t.count - begin);
-    const bool aligned = (((uintptr_t)param | (uintptr_t)grad) & 15) == 0 && (((uintptr_t)ms | (uintptr_t)vs) & 7) == 0;
-    for (uint32_t i = threadIdx.x * kEach; i < left + kStateBlock - 1 - (left - 1) % kStateBlock; i += kAdamwThreads * kEach) {
-        const int valid = i < left ? (int)min((uint32_t)kEach, left - i) : 0;
-        const bool whole = aligned && valid == kEach;
+    const bool aligned = (((uintptr_t)param & (sizeof(P) * kEach < 16 ? sizeof(P) * kEach - 1 : 15)) |
+                          ((uintptr_t)grad & (sizeof(G) * kEach < 16 ? sizeof(G) * kEach - 1 : 15)) |
+                          (((uintptr_t)ms | (uintptr_t)vs) & 7)) == 0;
+    const auto some = [&](uint32_t i, bool whole, int valid) {
         const uint32_t b = i / kStateBlock;
         float p[kEach], g[kEach], m[kEach], v[kEach];
-        Pack<uint32_t, kEach / 4> mc = {}, vc = {};
+        Codes mc = {}, vc = {};
         load_pack<kEach>(param + i, whole, valid, p);
         load_pack<kEach>(grad + i, whole, valid, g);
         if (whole) {
-            mc = *(const Pack<uint32_t, kEach / 4> *)(ms + i);
-            vc = *(const Pack<uint32_t, kEach / 4> *)(vs + i);
+            mc = *(const Codes *)(ms + i);
+            vc = *(const Codes *)(vs + i);
         } else {
 #pragma unroll
             for (int j = 0; j < kEach; ++j)
@@ -204,45 +210,56 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
             vc.v[j / 4] |= (Coding<false>::encode(v[j], v_inverse, h >> 16) & 255) << (8 * (j & 3));
         }
         if (whole) {
-            *(Pack<uint32_t, kEach / 4> *)(ms + i) = mc;
-            *(Pack<uint32_t, kEach / 4> *)(vs + i) = vc;
+            *(Codes *)(ms + i) = mc;
+            *(Codes *)(vs + i) = vc;
         } else {
 #pragma unroll
             for (int j = 0; j < kEach; ++j)
                 if (j < valid) ms[i + j] = (uint8_t)(mc.v[j / 4] >> (8 * (j & 3))), vs[i + j] = (uint8_t)(vc.v[j / 4] >> (8 * (j & 3)));
         }
         if (i % kStateBlock == 0) m_scale[b] = (uint8_t)em, v_scale[b] = (uint8_t)ev;
+    };
+    if (aligned && left == kAdamwChunk) {
+        for (uint32_t i = threadIdx.x * kEach; i < kAdamwChunk; i += kAdamwThreads * kEach) some(i, true, kEach);
+    } else {
+        const uint32_t end = (left + kStateBlock - 1) / kStateBlock * kStateBlock;  // whole halves of wavefronts
+        for (uint32_t i = threadIdx.x * kEach; i < end; i += kAdamwThreads * kEach) {
+            const int valid = i < left ? (int)min((uint32_t)kEach, left - i) : 0;
+            some(i, aligned && valid == kEach, valid);
+        }
     }
 }
 
-// Sixteen values a thread, four at a time: a thread that took four only would be done before the next ones could
-// be started (300 million values: 370 us, 4.0 TB/s).
-constexpr uint32_t kValuesChunk = 256 * 16;
+// Thirty-two values a thread, four at a time, all codes asked for before the first value is written: a byte read
+// makes four written, so that reads of four bytes a lane leave too few bytes on their way if one waits for the other.
+constexpr int kValuesParts = 8;
+constexpr uint32_t kValuesChunk = 256 * 4 * kValuesParts;
 template <bool kSigned>
-__global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *code, const uint8_t *scale, uint64_t count, float *values)
+__global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *__restrict__ code, const uint8_t *__restrict__ scale, uint64_t count,
+                                                      float *__restrict__ values)
 {
-    constexpr int kEach = 4;
     const bool aligned = ((uintptr_t)code & 3) == 0 && ((uintptr_t)values & 15) == 0;
     for (uint64_t begin = (uint64_t)blockIdx.x * kValuesChunk; begin < count; begin += (uint64_t)gridDim.x * kValuesChunk) {
+        if (aligned && count - begin >= kValuesChunk) {
+            const uint64_t first = begin + threadIdx.x * 4;
+            uint32_t c[kValuesParts], e[kValuesParts];
 #pragma unroll
-        for (uint32_t part = 0; part < kValuesChunk; part += 256 * kEach) {
-            const uint64_t i = begin + part + threadIdx.x * kEach;
-            if (i >= count) break;
-            const int valid = (int)min((uint64_t)kEach, count - i);
-            const bool whole = aligned && valid == kEach;
-            uint32_t c = 0;
-            if (whole) {
-                c = *(const uint32_t *)(code + i);
-            } else {
-#pragma unroll
-                for (int j = 0; j < kEach; ++j)
-                    if (j < valid) c |= (uint32_t)code[i + j] << (8 * j);
+            for (int part = 0; part < kValuesParts; ++part) {
+                c[part] = *(const uint32_t *)(code + first + part * 1024);
+                e[part] = scale[(first + part * 1024) / kStateBlock];  // of all four: 4 divides a block
             }
-            const float unit = Coding<kSigned>::scale_of(scale[i / kStateBlock]);  // of all four: 4 divides a block
-            float x[kEach];
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) x[j] = Coding<kSigned>::decode(c, j, unit);
-            store_pack<kEach>(values + i, whole, valid, x);
+            for (int part = 0; part < kValuesParts; ++part) {
+                const float unit = Coding<kSigned>::scale_of(e[part]);
+                Pack<float, 4> x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x.v[j] = Coding<kSigned>::decode(c[part], j, unit);
+                *(Pack<float, 4> *)(values + first + part * 1024) = x;
+            }
+        } else {
+            const uint64_t end = min(count, begin + kValuesChunk);
+            for (uint64_t i = begin + threadIdx.x; i < end; i += 256)
+                values[i] = Coding<kSigned>::decode(code[i], 0, Coding<kSigned>::scale_of(scale[i / kStateBlock]));
         }
     }
 }
