@@ -44,12 +44,29 @@ def built_digest() -> str:
 
 
 def build_lib(verbose: bool = False) -> str:
+    """Compiles every source by itself, side by side, and links them."""
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [HIPCC] + FLAGS + ["-o", tmp] + SOURCES
-    if verbose:
-        print(" ".join(cmd), flush=True)
+    parts = ["%s.%d.o" % (tmp, i) for i in range(len(SOURCES))]
+    compiles = [[HIPCC] + [f for f in FLAGS if f != "-shared"] + ["-c", "-o", o, src] for o, src in zip(parts, SOURCES)]
+    link = [HIPCC, "--offload-arch=gfx950", "-shared", "-o", tmp] + parts
     digest = source_digest()
-    subprocess.check_call(cmd)
+    try:
+        running = []
+        for cmd in compiles:
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            running.append(subprocess.Popen(cmd))
+        codes = [p.wait() for p in running]
+        for cmd, code in zip(compiles, codes):
+            if code:
+                raise subprocess.CalledProcessError(code, cmd)
+        if verbose:
+            print(" ".join(link), flush=True)
+        subprocess.check_call(link)
+    finally:
+        for o in parts:
+            if os.path.exists(o):
+                os.remove(o)
     os.replace(tmp, LIB)
     with open(DIGEST, "w") as fh:
         fh.write(digest + "\n")

@@ -121,32 +121,40 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw(AdamwArgs a)
     const G *grad = (const G *)t.grad + begin;
     float *ms = (float *)t.m + begin, *vs = (float *)t.v + begin;
     const uint32_t left = (uint32_t)min((uint64_t)a.chunk, t.count - begin);
-    const bool aligned = (((uintptr_t)param & (sizeof(P) * kEach - 1)) | ((uintptr_t)grad & (sizeof(G) * kEach - 1)) |
-                          (((uintptr_t)ms | (uintptr_t)vs) & 15)) == 0;
-    const auto some = [&](uint32_t i, bool whole, int valid) {
-        float p[kEach], g[kEach], m[kEach], v[kEach];
-        load_pack<kEach>(param + i, whole, valid, p);
-        load_pack<kEach>(grad + i, whole, valid, g);
-        load_pack<kEach>(ms + i, whole, valid, m);
-        load_pack<kEach>(vs + i, whole, valid, v);
+    const auto some = [&](uint32_t i, int valid) {
+        auto p = load_pack<kEach>(param + i, valid);
+        const auto g = load_pack<kEach>(grad + i, valid);
+        auto m = load_pack<kEach>(ms + i, valid), v = load_pack<kEach>(vs + i, valid);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const Moments s = move_moments(a, {m[j], v[j]}, g[j]);
-            p[j] = move_param(a, t, p[j], s);
-            m[j] = s.m, v[j] = s.v;
+            const Moments s = move_moments(a, {m.v[j], v.v[j]}, widen(g.v[j]));
+            p.v[j] = (P)move_param(a, t, widen(p.v[j]), s);
+            m.v[j] = s.m, v.v[j] = s.v;
         }
-        store_pack<kEach>(param + i, whole, valid, p);
-        store_pack<kEach>(ms + i, whole, valid, m);
-        store_pack<kEach>(vs + i, whole, valid, v);
+        store_pack(param + i, valid, p);
+        store_pack(ms + i, valid, m);
+        store_pack(vs + i, valid, v);
     };
-    if (aligned && left == a.chunk) {
-        for (uint32_t i = threadIdx.x * kEach; i < a.chunk; i += kAdamwThreads * kEach) some(i, true, kEach);
+    if (left == a.chunk) {
+        for (uint32_t i = threadIdx.x * kEach; i < a.chunk; i += kAdamwThreads * kEach) some(i, kEach);
     } else {
-        for (uint32_t i = threadIdx.x * kEach; i < left; i += kAdamwThreads * kEach) {
-            const int valid = (int)min((uint32_t)kEach, left - i);
-            some(i, aligned && valid == kEach, valid);
-        }
+        for (uint32_t i = threadIdx.x * kEach; i < left; i += kAdamwThreads * kEach) some(i, (int)(left - i));
     }
+}
+
+// `valid` codes, four a word; 0 behind them.
+template <int kWords>
+__device__ __forceinline__ void load_codes(const uint8_t *p, int valid, uint32_t (&out)[kWords])
+{
+    const auto t = load_pack<4 * kWords>(p, valid);
+    __builtin_memcpy(out, &t, sizeof(out));
+}
+template <int kWords>
+__device__ __forceinline__ void store_codes(uint8_t *p, int valid, const uint32_t (&in)[kWords])
+{
+    Pack<uint8_t, 4 * kWords> t;
+    __builtin_memcpy(&t, in, sizeof(t));
+    store_pack(p, valid, t);
 }
 
 // States in 8 bits: eight values a thread, half a wavefront a block of 256.
@@ -154,7 +162,6 @@ template <class P, class G>
 __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
 {
     constexpr int kEach = 8;
-    using Codes = Pack<uint32_t, kEach / 4>;
     const uint32_t k = __builtin_amdgcn_readfirstlane(tensor_of(a, blockIdx.x));
     const AdamwTensor &t = a.tensor[k];
     const uint32_t chunk = blockIdx.x - (k ? a.chunk_end[k - 1] : 0);
@@ -166,36 +173,27 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
     // the number of the chunk's first value
     const uint64_t number = (a.first_block + a.block[k]) * kStateBlock + begin;
     const uint32_t left = (uint32_t)min((uint64_t)a.chunk, t.count - begin);
-    const bool aligned = (((uintptr_t)param & (sizeof(P) * kEach < 16 ? sizeof(P) * kEach - 1 : 15)) |
-                          ((uintptr_t)grad & (sizeof(G) * kEach < 16 ? sizeof(G) * kEach - 1 : 15)) |
-                          (((uintptr_t)ms | (uintptr_t)vs) & 7)) == 0;
-    const auto some = [&](uint32_t i, bool whole, int valid) {
+    const auto some = [&](uint32_t i, int valid) {
         const uint32_t b = i / kStateBlock;
-        float p[kEach], g[kEach], m[kEach], v[kEach];
-        Codes mc = {}, vc = {};
-        load_pack<kEach>(param + i, whole, valid, p);
-        load_pack<kEach>(grad + i, whole, valid, g);
-        if (whole) {
-            mc = *(const Codes *)(ms + i);
-            vc = *(const Codes *)(vs + i);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (j < valid) mc.v[j / 4] |= (uint32_t)ms[i + j] << (8 * (j & 3)), vc.v[j / 4] |= (uint32_t)vs[i + j] << (8 * (j & 3));
-        }
+        auto p = load_pack<kEach>(param + i, valid);
+        const auto g = load_pack<kEach>(grad + i, valid);
+        uint32_t mc[kEach / 4], vc[kEach / 4];
+        load_codes(ms + i, valid, mc);
+        load_codes(vs + i, valid, vc);
+        float m[kEach], v[kEach];
         const float m_unit = Coding<true>::scale_of(m_scale[b]), v_unit = Coding<false>::scale_of(v_scale[b]);
         uint32_t m_most = 0, v_most = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            Moments s = {Coding<true>::decode(mc.v[j / 4], j & 3, m_unit), Coding<false>::decode(vc.v[j / 4], j & 3, v_unit)};
-            s = move_moments(a, s, g[j]);
-            if (!whole && j >= valid) s = {0.0f, 0.0f};
-            p[j] = move_param(a, t, p[j], s);
+            Moments s = {Coding<true>::decode(mc[j / 4], j & 3, m_unit), Coding<false>::decode(vc[j / 4], j & 3, v_unit)};
+            s = move_moments(a, s, widen(g.v[j]));
+            if (j >= valid) s = {0.0f, 0.0f};
+            p.v[j] = (P)move_param(a, t, widen(p.v[j]), s);
             m[j] = s.m, v[j] = s.v;
             m_most = max(m_most, __float_as_uint(s.m) & 0x7FFFFFFFu);
             v_most = max(v_most, __float_as_uint(s.v));
         }
-        store_pack<kEach>(param + i, whole, valid, p);
+        store_pack(param + i, valid, p);
         // the block is half a wavefront's; the other half may be in another block, but not outside the loop
 #pragma unroll
         for (int d = 16; d >= 1; d >>= 1) {
@@ -204,31 +202,22 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
         }
         const uint32_t em = max(1u, m_most >> 23), ev = max(1u, v_most >> 23 & 255);  // a NaN may have its sign set
         const float m_inverse = Coding<true>::inverse_of(em), v_inverse = Coding<false>::inverse_of(ev);
-        mc = {}, vc = {};
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
+            if (j % 4 == 0) mc[j / 4] = vc[j / 4] = 0;
             const uint32_t h = hash_of(number + i + j, a.dither);
-            mc.v[j / 4] |= (Coding<true>::encode(m[j], m_inverse, h & 0xFFFF) & 255) << (8 * (j & 3));
-            vc.v[j / 4] |= (Coding<false>::encode(v[j], v_inverse, h >> 16) & 255) << (8 * (j & 3));
+            mc[j / 4] |= (Coding<true>::encode(m[j], m_inverse, h & 0xFFFF) & 255) << (8 * (j & 3));
+            vc[j / 4] |= (Coding<false>::encode(v[j], v_inverse, h >> 16) & 255) << (8 * (j & 3));
         }
-        if (whole) {
-            *(Codes *)(ms + i) = mc;
-            *(Codes *)(vs + i) = vc;
-        } else {
-#pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (j < valid) ms[i + j] = (uint8_t)(mc.v[j / 4] >> (8 * (j & 3))), vs[i + j] = (uint8_t)(vc.v[j / 4] >> (8 * (j & 3)));
-        }
+        store_codes(ms + i, valid, mc);
+        store_codes(vs + i, valid, vc);
         if (i % kStateBlock == 0) m_scale[b] = (uint8_t)em, v_scale[b] = (uint8_t)ev;
     };
-    if (aligned && left == a.chunk) {
-        for (uint32_t i = threadIdx.x * kEach; i < a.chunk; i += kAdamwThreads * kEach) some(i, true, kEach);
+    if (left == a.chunk) {
+        for (uint32_t i = threadIdx.x * kEach; i < a.chunk; i += kAdamwThreads * kEach) some(i, kEach);
     } else {
         const uint32_t end = (left + kStateBlock - 1) / kStateBlock * kStateBlock;  // whole halves of wavefronts
-        for (uint32_t i = threadIdx.x * kEach; i < end; i += kAdamwThreads * kEach) {
-            const int valid = i < left ? (int)min((uint32_t)kEach, left - i) : 0;
-            some(i, aligned && valid == kEach, valid);
-        }
+        for (uint32_t i = threadIdx.x * kEach; i < end; i += kAdamwThreads * kEach) some(i, (int)left - (int)i);
     }
 }
 
@@ -240,14 +229,13 @@ template <bool kSigned>
 __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *__restrict__ code, const uint8_t *__restrict__ scale, uint64_t count,
                                                       float *__restrict__ values)
 {
-    const bool aligned = ((uintptr_t)code & 3) == 0 && ((uintptr_t)values & 15) == 0;
     for (uint64_t begin = (uint64_t)blockIdx.x * kValuesChunk; begin < count; begin += (uint64_t)gridDim.x * kValuesChunk) {
-        if (aligned && count - begin >= kValuesChunk) {
+        if (count - begin >= kValuesChunk) {
             const uint64_t first = begin + threadIdx.x * 4;
-            uint32_t c[kValuesParts], e[kValuesParts];
+            uint32_t c[kValuesParts][1], e[kValuesParts];
 #pragma unroll
             for (int part = 0; part < kValuesParts; ++part) {
-                c[part] = *(const uint32_t *)(code + first + part * 1024);
+                load_codes(code + first + part * 1024, 4, c[part]);
                 e[part] = scale[(first + part * 1024) / kStateBlock];  // of all four: 4 divides a block
             }
 #pragma unroll
@@ -255,7 +243,7 @@ __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *__restrict_
                 const float unit = Coding<kSigned>::scale_of(e[part]);
                 Pack<float, 4> x;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x.v[j] = Coding<kSigned>::decode(c[part], j, unit);
+                for (int j = 0; j < 4; ++j) x.v[j] = Coding<kSigned>::decode(c[part][0], j, unit);
                 *(Pack<float, 4> *)(values + first + part * 1024) = x;
             }
         } else {

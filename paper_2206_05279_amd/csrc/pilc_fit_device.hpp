@@ -10,40 +10,34 @@ namespace pilc {
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
 
-// kCount of T as one access; the address is a multiple of its size, or of 16 bytes if that is less.
-template <class T, int kCount>
-struct alignas(sizeof(T) * kCount < 16 ? sizeof(T) * kCount : 16) Pack {
-    T v[kCount];
-};
-
 template <class T>
 __device__ __forceinline__ float widen(T v) { return (float)v; }
 
-// `valid` of kCount values from p, 0 behind them.  whole: all are there and p is aligned for a Pack.
+// kCount of T as one access wherever they lie: this GPU's global memory takes accesses of 16 bytes at any address.
+template <class T, int kCount>
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
+    T v[kCount];
+};
+
+// `valid` of kCount values from p, 0 behind them.
 template <int kCount, class T>
-__device__ __forceinline__ void load_pack(const T *p, bool whole, int valid, float (&out)[kCount])
+__device__ __forceinline__ Pack<T, kCount> load_pack(const T *p, int valid)
 {
-    if (whole) {
-        const Pack<T, kCount> t = *(const Pack<T, kCount> *)p;
+    if (valid >= kCount) return *(const Pack<T, kCount> *)p;
+    Pack<T, kCount> t;
 #pragma unroll
-        for (int k = 0; k < kCount; ++k) out[k] = widen(t.v[k]);
-    } else {
-#pragma unroll
-        for (int k = 0; k < kCount; ++k) out[k] = k < valid ? widen(p[k]) : 0.0f;
-    }
+    for (int k = 0; k < kCount; ++k) t.v[k] = k < valid ? p[k] : (T)0;
+    return t;
 }
 template <int kCount, class T>
-__device__ __forceinline__ void store_pack(T *p, bool whole, int valid, const float (&in)[kCount])
+__device__ __forceinline__ void store_pack(T *p, int valid, const Pack<T, kCount> &t)
 {
-    if (whole) {
-        Pack<T, kCount> t;
-#pragma unroll
-        for (int k = 0; k < kCount; ++k) t.v[k] = (T)in[k];
+    if (valid >= kCount) {
         *(Pack<T, kCount> *)p = t;
     } else {
 #pragma unroll
         for (int k = 0; k < kCount; ++k)
-            if (k < valid) p[k] = (T)in[k];
+            if (k < valid) p[k] = t.v[k];
     }
 }
 
@@ -53,11 +47,56 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // 2^x by the hardware's instruction, one unit in the last place off at most; results below 2^-126 are 0.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// What a lane's partner has, the partner being 1, 2, 4, 8 lanes away within groups of 2, 4, 8, 16: the first two by
+// their numbers, the others as mirror images, which is the same once the smaller groups are of one value.
+template <int kDpp>
+__device__ __forceinline__ float from_partner(float v)
+{
+    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), kDpp, 15, 15, true));
+}
+template <int kDpp>
+__device__ __forceinline__ uint32_t from_partner(uint32_t v)
+{
+    return __builtin_amdgcn_mov_dpp(v, kDpp, 15, 15, true);
+}
+__device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ uint32_t bits_of(uint32_t v) { return v; }
+__device__ __forceinline__ void from_bits(uint32_t b, float &v) { v = __uint_as_float(b); }
+__device__ __forceinline__ void from_bits(uint32_t b, uint32_t &v) { v = b; }
+
+// Over groups of kLanes neighbouring lanes, without LDS; every lane gets the result, the same bits in all.
+template <int kLanes, class V, class Op>
+__device__ __forceinline__ V lanes_reduce(V v, Op op)
+{
+    static_assert(kLanes >= 1 && kLanes <= 64 && (kLanes & (kLanes - 1)) == 0, "");
+    if constexpr (kLanes >= 2) v = op(v, from_partner<0xB1>(v));   // quads 1 0 3 2
+    if constexpr (kLanes >= 4) v = op(v, from_partner<0x4E>(v));   // quads 2 3 0 1
+    if constexpr (kLanes >= 8) v = op(v, from_partner<0x141>(v));  // eights the other way round
+    if constexpr (kLanes >= 16) v = op(v, from_partner<0x140>(v)); // sixteens the other way round
+    if constexpr (kLanes >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(bits_of(v), bits_of(v), false, false);
+        V p, q;
+        from_bits(r[0], p), from_bits(r[1], q);
+        v = op(p, q);
+    }
+    if constexpr (kLanes >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(bits_of(v), bits_of(v), false, false);
+        V p, q;
+        from_bits(r[0], p), from_bits(r[1], q);
+        v = op(p, q);
+    }
+    return v;
+}
+
 template <class V, class Op>
 __device__ __forceinline__ V wave_reduce(V v, Op op)
 {
-    for (int d = 32; d >= 1; d >>= 1) v = op(v, __shfl_xor(v, d, 64));
-    return v;
+    if constexpr (sizeof(V) == 4) {
+        return lanes_reduce<64>(v, op);
+    } else {
+        for (int d = 32; d >= 1; d >>= 1) v = op(v, __shfl_xor(v, d, 64));
+        return v;
+    }
 }
 
 // Over a workgroup of kWaves wavefronts; every thread gets the result.  `room` holds kWaves values; the

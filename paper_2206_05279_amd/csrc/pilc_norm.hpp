@@ -16,6 +16,211 @@ struct NormArgs {
 
 constexpr int kNormThreads = 256;
 
+// Rows held in registers: kLanes lanes of a wavefront, or a whole workgroup of kLanes threads, hold kEach values of a
+// row each, as packs of 16 bytes, and go from row to row with the weights in registers.
+template <class T, class W, int kLanes, int kEach>
+struct NormRow {
+    static constexpr int kVec = 16 / sizeof(T), kPer = kEach / kVec;
+    static constexpr bool kAhead = kLanes < 1024;  // the next row is asked for early; the largest workgroups lack the registers
+    static constexpr int kThreads = kLanes > 256 ? kLanes : 256;
+    static constexpr int kRows = kThreads / kLanes;  // that a workgroup has in hand
+    static constexpr int kWaves = kLanes / 64;       // that share a row
+    using Values = Pack<T, kVec>;
+
+    uint32_t width, lane, row_in_block;
+
+    __device__ explicit NormRow(uint32_t w) : width(w), lane(threadIdx.x % kLanes), row_in_block(threadIdx.x / kLanes) {}
+    __device__ uint32_t column(int q) const { return (q * kLanes + lane) * kVec; }
+    // of a pack's values, how many are the row's: kVec, or fewer at its end
+    __device__ int valid(int q) const { return min(max((int)(width - column(q)), 0), kVec); }
+
+    __device__ void load(const T *p, Values (&out)[kPer]) const
+    {
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) out[q] = load_pack<kVec>(p + column(q), valid(q));
+    }
+    __device__ void load_weights(const W *p, float none, float (&out)[kPer][kVec]) const
+    {
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) {
+            const auto t = p ? load_pack<kVec>(p + column(q), valid(q)) : Pack<W, kVec>{};
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) out[q][k] = p ? widen(t.v[k]) : none;
+        }
+    }
+
+    // Sums over the row of two numbers a lane.  `room` is used in turn: two halves, so that the workgroup meets
+    // once a sum.
+    __device__ float2 sum(float2 v, float2 *room, int half) const
+    {
+        constexpr int kWithin = kLanes < 64 ? kLanes : 64;
+        v.x = lanes_reduce<kWithin>(v.x, Sum());
+        v.y = lanes_reduce<kWithin>(v.y, Sum());
+        if constexpr (kWaves > 1) {
+            room += half * kWaves;
+            if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+            __syncthreads();
+            v = room[0];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) v.x += room[w].x, v.y += room[w].y;
+        }
+        return v;
+    }
+    __device__ float sum(float v, float2 *room, int half) const { return sum(make_float2(v, 0.0f), room, half).x; }
+};
+
+template <class T, class W, int kLanes, int kEach>
+__global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads)) void k_norm_forward_rows(NormArgs a)
+{
+    using Row = NormRow<T, W, kLanes, kEach>;
+    constexpr int kVec = Row::kVec, kPer = Row::kPer;
+    __shared__ float2 room[2 * (Row::kWaves > 1 ? Row::kWaves : 1)];
+    const Row r(a.width);
+    const float per_value = 1.0f / (float)a.width;
+    float weight[kPer][kVec], bias[kPer][kVec];
+    r.load_weights((const W *)a.weight, 1.0f, weight);
+    r.load_weights((const W *)a.bias, 0.0f, bias);
+    typename Row::Values x[kPer], next[kPer];
+    uint32_t row = blockIdx.x * Row::kRows + r.row_in_block;
+    const uint32_t step = gridDim.x * Row::kRows;
+    if (Row::kAhead && row < a.rows) r.load((const T *)a.x + row * a.x_stride, x);
+    for (; row < a.rows; row += step) {
+        if (!Row::kAhead)
+            r.load((const T *)a.x + row * a.x_stride, x);
+        else if (a.rows - row > step)
+            r.load((const T *)a.x + (row + step) * a.x_stride, next);
+        float sum = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kPer; ++q)
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) sum += widen(x[q].v[k]);
+        const float mean = r.sum(sum, room, 0) * per_value;
+        float square = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) {
+            const int valid = r.valid(q);
+            if (valid == kVec) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    const float d = widen(x[q].v[k]) - mean;
+                    square += d * d;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    const float d = k < valid ? widen(x[q].v[k]) - mean : 0.0f;
+                    square += d * d;
+                }
+            }
+        }
+        const float rstd = 1.0f / sqrtf(r.sum(square, room, 1) * per_value + a.eps);
+        if (r.lane == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        T *y = (T *)a.y + row * a.y_stride;
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) {
+            typename Row::Values out;
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) out.v[k] = (T)((widen(x[q].v[k]) - mean) * rstd * weight[q][k] + bias[q][k]);
+            store_pack(y + r.column(q), r.valid(q), out);
+            if (Row::kAhead) x[q] = next[q];
+        }
+    }
+}
+
+// dx row by row as above, and what the rows a workgroup meets add to the weights' gradients, in registers; at the end
+// the workgroup's rows are added up and put down as one part.
+template <class T, class W, int kLanes, int kEach>
+__global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads)) void k_norm_backward_rows(NormArgs a)
+{
+    using Row = NormRow<T, W, kLanes, kEach>;
+    constexpr int kVec = Row::kVec, kPer = Row::kPer;
+    __shared__ float2 room[2 * (Row::kWaves > 1 ? Row::kWaves : 1)];
+    __shared__ float added[Row::kRows > 1 ? Row::kThreads * kEach : 1];
+    const Row r(a.width);
+    const float per_value = 1.0f / (float)a.width;
+    float weight[kPer][kVec], dw[kPer][kVec] = {}, db[kPer][kVec] = {};
+    r.load_weights((const W *)a.weight, 1.0f, weight);
+    typename Row::Values x[kPer], dy[kPer], next_x[kPer], next_dy[kPer];
+    uint32_t row = blockIdx.x * Row::kRows + r.row_in_block;
+    const uint32_t step = gridDim.x * Row::kRows;
+    int half = 0;
+    if (Row::kAhead && row < a.rows) {
+        r.load((const T *)a.x + row * a.x_stride, x);
+        r.load((const T *)a.dy + row * a.y_stride, dy);
+    }
+    for (; row < a.rows; row += step) {
+        if (!Row::kAhead) {
+            r.load((const T *)a.x + row * a.x_stride, x);
+            r.load((const T *)a.dy + row * a.y_stride, dy);
+        } else if (a.rows - row > step) {
+            r.load((const T *)a.x + (row + step) * a.x_stride, next_x);
+            r.load((const T *)a.dy + (row + step) * a.y_stride, next_dy);
+        }
+        const float mean = a.mean_in[row], rstd = a.rstd_in[row];
+        float2 sums = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int q = 0; q < kPer; ++q)
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) {
+                const float d = widen(dy[q].v[k]), xh = (widen(x[q].v[k]) - mean) * rstd, g = d * weight[q][k];
+                sums.x += g;
+                sums.y += g * xh;
+                dw[q][k] += d * xh;
+                db[q][k] += d;
+            }
+        if (a.dx) {
+            sums = r.sum(sums, room, half);
+            half ^= 1;
+            const float c1 = sums.x * per_value, c2 = sums.y * per_value;
+            T *dx = (T *)a.dx + row * a.dx_stride;
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) {
+                typename Row::Values out;
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    const float xh = (widen(x[q].v[k]) - mean) * rstd;
+                    out.v[k] = (T)(rstd * (widen(dy[q].v[k]) * weight[q][k] - c1 - xh * c2));
+                }
+                store_pack(dx + r.column(q), r.valid(q), out);
+            }
+        }
+        if (Row::kAhead)
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) x[q] = next_x[q], dy[q] = next_dy[q];
+    }
+    if (!a.parts) return;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float *part = a.parts + ((size_t)which * gridDim.x + blockIdx.x) * a.width;
+        float(&own)[kPer][kVec] = which ? db : dw;
+        if constexpr (Row::kRows > 1) {
+            // value v of lane l of row g at (g * kEach + v) * kLanes + l
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < kEach; ++v) added[(r.row_in_block * kEach + v) * kLanes + r.lane] = own[v / kVec][v % kVec];
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < (uint32_t)(kEach * kLanes); i += Row::kThreads) {
+                const uint32_t v = i / kLanes, l = i % kLanes, j = (v / kVec * kLanes + l) * kVec + v % kVec;
+                float sum = 0.0f;
+                for (int g = 0; g < Row::kRows; ++g) sum += added[g * kEach * kLanes + i];
+                if (j < a.width) part[j] = sum;
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) {
+                Pack<float, kVec> out;
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) out.v[k] = own[q][k];
+                store_pack(part + r.column(q), r.valid(q), out);
+            }
+        }
+    }
+}
+
+// Rows too long for registers.
 template <class T, class W>
 __global__ __launch_bounds__(kNormThreads) void k_norm_forward(NormArgs a)
 {
@@ -85,22 +290,51 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_parts(NormArgs a)
     a.parts[(size_t)(a.num_parts + blockIdx.y) * a.width + j] = db;
 }
 
+// The parts added up: 64 columns a workgroup, each by sixteen threads that take every sixteenth part.
 template <class W>
-__global__ __launch_bounds__(kNormThreads) void k_norm_join(NormArgs a)
+__global__ __launch_bounds__(1024) void k_norm_join(NormArgs a)
 {
-    const uint32_t j = blockIdx.x * kNormThreads + threadIdx.x;
-    if (j >= a.width) return;
-    float dw = 0.0f, db = 0.0f;
-    for (uint32_t p = 0; p < a.num_parts; ++p) {
-        dw += a.parts[(size_t)p * a.width + j];
-        db += a.parts[(size_t)(a.num_parts + p) * a.width + j];
+    __shared__ float room[16][64];
+    const uint32_t column = threadIdx.x & 63, run = threadIdx.x >> 6, j = blockIdx.x * 64 + column;
+    W *out = (W *)(blockIdx.y ? a.dbias : a.dweight);
+    if (!out) return;
+    const float *part = a.parts + (size_t)blockIdx.y * a.num_parts * a.width + j;
+    float sum = 0.0f;
+    if (j < a.width) {
+#pragma unroll 8
+        for (uint32_t p = run; p < a.num_parts; p += 16) sum += part[(size_t)p * a.width];
     }
-    if (a.dweight) ((W *)a.dweight)[j] = (W)dw;
-    if (a.dbias) ((W *)a.dbias)[j] = (W)db;
+    room[run][column] = sum;
+    __syncthreads();
+    if (run == 0 && j < a.width) {
+        for (int i = 1; i < 16; ++i) sum += room[i][column];
+        out[j] = (W)sum;
+    }
 }
 
-static uint32_t norm_parts(const pilc_norm_shape &) { return 64; }
-static size_t norm_workspace(const pilc_norm_shape &s) { return std::max<size_t>(256, 2 * sizeof(float) * (size_t)norm_parts(s) * s.width); }
+// Calls `go` with the lanes and values a lane that a row of `width` values goes into, or returns false where it is too long.
+template <class Go>
+static bool norm_row(uint32_t width, Go go)
+{
+    using std::integral_constant;
+    const auto with = [&](auto lanes, auto each) {
+        if (width > (uint32_t)(lanes.value * each.value)) return false;
+        go(lanes, each);
+        return true;
+    };
+    return with(integral_constant<int, 8>(), integral_constant<int, 8>()) || with(integral_constant<int, 32>(), integral_constant<int, 8>()) ||
+           with(integral_constant<int, 64>(), integral_constant<int, 16>()) || with(integral_constant<int, 256>(), integral_constant<int, 8>()) ||
+           with(integral_constant<int, 256>(), integral_constant<int, 16>()) || with(integral_constant<int, 512>(), integral_constant<int, 16>()) ||
+           with(integral_constant<int, 1024>(), integral_constant<int, 16>());
+}
+
+constexpr uint32_t kNormBlocksPerUnit = 4;
+constexpr uint32_t kNormLongParts = 64;
+static uint32_t norm_most_parts(uint32_t rows) { return std::max(1u, std::min(rows, std::max(kNormLongParts, kNormBlocksPerUnit * compute_units()))); }
+static size_t norm_workspace(const pilc_norm_shape &s)
+{
+    return std::max<size_t>(256, 2 * sizeof(float) * (size_t)norm_most_parts(s.rows) * s.width);
+}
 
 static bool norm_shape_ok(const pilc_norm_shape *s, bool backward)
 {
@@ -139,9 +373,16 @@ int pilc_norm_forward(const pilc_norm_shape *shape, const void *x_dev, const voi
     NormArgs a = {};
     a.x = x_dev, a.weight = weight_dev, a.bias = bias_dev, a.y = y_dev, a.mean = mean_dev, a.rstd = rstd_dev;
     a.x_stride = shape->x_stride, a.y_stride = shape->y_stride, a.rows = shape->rows, a.width = shape->width, a.eps = shape->eps;
+    const uint32_t most = kNormBlocksPerUnit * compute_units();
     return by_types(shape->dtype, shape->weight_type, [&](auto *t, auto *w) {
-        k_norm_forward<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(w)>>
-            <<<row_blocks(a.rows), kNormThreads, 0, (hipStream_t)hip_stream>>>(a);
+        using T = std::remove_pointer_t<decltype(t)>;
+        using W = std::remove_pointer_t<decltype(w)>;
+        const bool done = norm_row(a.width, [&](auto lanes, auto each) {
+            using Row = NormRow<T, W, decltype(lanes)::value, decltype(each)::value>;
+            const uint32_t blocks = std::min((a.rows + Row::kRows - 1) / Row::kRows, most);
+            k_norm_forward_rows<T, W, decltype(lanes)::value, decltype(each)::value><<<blocks, Row::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+        });
+        if (!done) k_norm_forward<T, W><<<row_blocks(a.rows), kNormThreads, 0, (hipStream_t)hip_stream>>>(a);
     });
 }
 
@@ -167,18 +408,27 @@ int pilc_norm_backward(const pilc_norm_shape *shape, const void *dy_dev, const v
     if (workspace_bytes < norm_workspace(*shape)) return PILC_E_WORKSPACE;
     NormArgs a = {};
     a.dy = dy_dev, a.x = x_dev, a.weight = weight_dev, a.mean_in = mean_dev, a.rstd_in = rstd_dev, a.dx = dx_dev, a.dweight = dweight_dev;
-    a.dbias = dbias_dev, a.parts = (float *)workspace_dev, a.x_stride = shape->x_stride, a.y_stride = shape->y_stride;
-    a.dx_stride = shape->dx_stride, a.rows = shape->rows, a.width = shape->width, a.num_parts = norm_parts(*shape);
+    a.dbias = dbias_dev, a.x_stride = shape->x_stride, a.y_stride = shape->y_stride, a.dx_stride = shape->dx_stride;
+    a.rows = shape->rows, a.width = shape->width;
+    if (dweight_dev || dbias_dev) a.parts = (float *)workspace_dev;
+    const uint32_t most = kNormBlocksPerUnit * compute_units();
     const hipStream_t stream = (hipStream_t)hip_stream;
     return by_types(shape->dtype, shape->weight_type, [&](auto *t, auto *w) {
         using T = std::remove_pointer_t<decltype(t)>;
         using W = std::remove_pointer_t<decltype(w)>;
-        const uint32_t columns = (a.width + kNormThreads - 1) / kNormThreads;
-        if (a.dweight || a.dbias) {
-            k_norm_parts<T><<<dim3(columns, a.num_parts), kNormThreads, 0, stream>>>(a);
-            k_norm_join<W><<<columns, kNormThreads, 0, stream>>>(a);
+        const bool done = norm_row(a.width, [&](auto lanes, auto each) {
+            using Row = NormRow<T, W, decltype(lanes)::value, decltype(each)::value>;
+            a.num_parts = std::min((a.rows + Row::kRows - 1) / Row::kRows, most);
+            if (a.rows)
+                k_norm_backward_rows<T, W, decltype(lanes)::value, decltype(each)::value><<<a.num_parts, Row::kThreads, 0, stream>>>(a);
+        });
+        if (!done) {
+            a.num_parts = std::min(a.rows, kNormLongParts);
+            // before dx, which may take dy's place
+            if (a.parts && a.rows) k_norm_parts<T><<<dim3((a.width + kNormThreads - 1) / kNormThreads, a.num_parts), kNormThreads, 0, stream>>>(a);
+            if (a.dx && a.rows) k_norm_dx<T, W><<<row_blocks(a.rows), kNormThreads, 0, stream>>>(a);
         }
-        if (a.dx && a.rows) k_norm_dx<T, W><<<row_blocks(a.rows), kNormThreads, 0, stream>>>(a);
+        if (a.parts) k_norm_join<W><<<dim3((a.width + 63) / 64, 2), 1024, 0, stream>>>(a);
     });
 }
 
