@@ -47,6 +47,34 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // 2^x by the hardware's instruction, one unit in the last place off at most; results below 2^-126 are 0.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Sixteen bytes of T as they lie in memory.  They stay four registers until they are looked into: taken apart where they
+// are loaded, they would have to be waited for there.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+template <class T>
+struct Raw {
+    static constexpr int kVec = 16 / sizeof(T);
+    u32x4_t bits;
+
+    __device__ static Raw load(const T *p)
+    {
+        struct __attribute__((packed, aligned(sizeof(T)))) At { u32x4_t v; };
+        return {((const At *)p)->v};
+    }
+    __device__ void store(T *p) const
+    {
+        struct __attribute__((packed, aligned(sizeof(T)))) At { u32x4_t v; };
+        ((At *)p)->v = bits;
+    }
+    __device__ float operator[](int k) const { return widen(__builtin_bit_cast(Pack<T, kVec>, bits).v[k]); }
+    __device__ static Raw of(const float (&v)[kVec])
+    {
+        Pack<T, kVec> t;
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) t.v[k] = (T)v[k];
+        return {__builtin_bit_cast(u32x4_t, t)};
+    }
+};
+
 // What a lane's partner has, the partner being 1, 2, 4, 8 lanes away within groups of 2, 4, 8, 16: the first two by
 // their numbers, the others as mirror images, which is the same once the smaller groups are of one value.
 template <int kDpp>

@@ -15,9 +15,13 @@ struct NormArgs {
 };
 
 constexpr int kNormThreads = 256;
+// Wavefronts a SIMD that the kernels' registers are kept down to, and that are launched: all at once, each going from row to row.
+constexpr int kNormForwardWaves = 5, kNormBackwardWaves = 3;
 
 // Rows held in registers: kLanes lanes of a wavefront, or a whole workgroup of kLanes threads, hold kEach values of a
-// row each, as packs of 16 bytes, and go from row to row with the weights in registers.
+// row each, as packs of 16 bytes, and go from row to row with the weights in registers.  A pack that would reach over
+// the row's end begins earlier: some values are then held twice, worked out twice to the same bits and stored twice,
+// and left out of the row's sums the second time.
 template <class T, class W, int kLanes, int kEach>
 struct NormRow {
     static constexpr int kVec = 16 / sizeof(T), kPer = kEach / kVec;
@@ -25,30 +29,61 @@ struct NormRow {
     static constexpr int kThreads = kLanes > 256 ? kLanes : 256;
     static constexpr int kRows = kThreads / kLanes;  // that a workgroup has in hand
     static constexpr int kWaves = kLanes / 64;       // that share a row
-    using Values = Pack<T, kVec>;
+    // of `most` wavefronts a SIMD, the whole workgroups' that fit
+    static constexpr int waves(int most) { return kThreads == 1024 ? 4 : most * 256 / kThreads * kThreads / 256; }
 
     uint32_t width, lane, row_in_block;
+    bool ragged;
 
-    __device__ explicit NormRow(uint32_t w) : width(w), lane(threadIdx.x % kLanes), row_in_block(threadIdx.x / kLanes) {}
-    __device__ uint32_t column(int q) const { return (q * kLanes + lane) * kVec; }
-    // of a pack's values, how many are the row's: kVec, or fewer at its end
-    __device__ int valid(int q) const { return min(max((int)(width - column(q)), 0), kVec); }
-
-    __device__ void load(const T *p, Values (&out)[kPer]) const
+    __device__ explicit NormRow(uint32_t w)
+        : width(w), lane(threadIdx.x % kLanes), row_in_block(kRows > 1 ? threadIdx.x / kLanes : 0), ragged(w != (uint32_t)(kLanes * kEach))
     {
-#pragma unroll
-        for (int q = 0; q < kPer; ++q) out[q] = load_pack<kVec>(p + column(q), valid(q));
     }
-    __device__ void load_weights(const W *p, float none, float (&out)[kPer][kVec]) const
+    __device__ uint32_t place(int q) const { return (q * kLanes + lane) * kVec; }
+    __device__ uint32_t column(int q) const { return min(place(q), width - kVec); }
+    __device__ int twice(int q) const { return (int)min(place(q) - column(q), (uint32_t)kVec); }  // values at a pack's begin that another has
+
+    __device__ void load(const T *p, Raw<T> (&out)[kPer]) const
     {
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) {
-            const auto t = p ? load_pack<kVec>(p + column(q), valid(q)) : Pack<W, kVec>{};
+        for (int q = 0; q < kPer; ++q) out[q] = Raw<T>::load(p + column(q));
+    }
+    // weights as they lie in memory, `none` where there are none
+    __device__ void load_weights(const W *p, float none, Pack<W, kVec> (&out)[kPer]) const
+    {
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) out[q][k] = p ? widen(t.v[k]) : none;
+        for (int q = 0; q < kPer; ++q)
+            if (p) {
+                out[q] = *(const Pack<W, kVec> *)(p + column(q));
+            } else {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) out[q].v[k] = (W)none;
+            }
+    }
+
+    // The sum over a lane's values of f(pack, value)
+    template <class V, class F>
+    __device__ V own_sum(V sum, F f) const
+    {
+        if (!ragged) {
+#pragma unroll
+            for (int q = 0; q < kPer; ++q)
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) f(sum, q, k);
+        } else {
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) {
+                const int from = twice(q);
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    V with = sum;
+                    f(with, q, k);
+                    sum = k >= from ? with : sum;
+                }
+            }
         }
+        return sum;
     }
-
     // Sums over the row of two numbers a lane.  `room` is used in turn: two halves, so that the workgroup meets
     // once a sum.
     __device__ float2 sum(float2 v, float2 *room, int half) const
@@ -70,49 +105,32 @@ struct NormRow {
 };
 
 template <class T, class W, int kLanes, int kEach>
-__global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads)) void k_norm_forward_rows(NormArgs a)
+__global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads), (NormRow<T, W, kLanes, kEach>::waves(kNormForwardWaves))) void
+k_norm_forward_rows(NormArgs a)
 {
     using Row = NormRow<T, W, kLanes, kEach>;
     constexpr int kVec = Row::kVec, kPer = Row::kPer;
     __shared__ float2 room[2 * (Row::kWaves > 1 ? Row::kWaves : 1)];
     const Row r(a.width);
     const float per_value = 1.0f / (float)a.width;
-    float weight[kPer][kVec], bias[kPer][kVec];
+    Pack<W, kVec> weight[kPer], bias[kPer];
     r.load_weights((const W *)a.weight, 1.0f, weight);
     r.load_weights((const W *)a.bias, 0.0f, bias);
-    typename Row::Values x[kPer], next[kPer];
+    Raw<T> x[kPer], next[kPer];
     uint32_t row = blockIdx.x * Row::kRows + r.row_in_block;
-    const uint32_t step = gridDim.x * Row::kRows;
-    if (Row::kAhead && row < a.rows) r.load((const T *)a.x + row * a.x_stride, x);
+    const uint32_t step = gridDim.x * Row::kRows, last = a.rows - 1;
+    if (Row::kAhead) r.load((const T *)a.x + min(row, last) * a.x_stride, x);
     for (; row < a.rows; row += step) {
-        if (!Row::kAhead)
+        if (Row::kAhead)
+            r.load((const T *)a.x + (last - row > step ? row + step : last) * a.x_stride, next);
+        else
             r.load((const T *)a.x + row * a.x_stride, x);
-        else if (a.rows - row > step)
-            r.load((const T *)a.x + (row + step) * a.x_stride, next);
-        float sum = 0.0f;
-#pragma unroll
-        for (int q = 0; q < kPer; ++q)
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) sum += widen(x[q].v[k]);
-        const float mean = r.sum(sum, room, 0) * per_value;
-        float square = 0.0f;
-#pragma unroll
-        for (int q = 0; q < kPer; ++q) {
-            const int valid = r.valid(q);
-            if (valid == kVec) {
-#pragma unroll
-                for (int k = 0; k < kVec; ++k) {
-                    const float d = widen(x[q].v[k]) - mean;
-                    square += d * d;
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < kVec; ++k) {
-                    const float d = k < valid ? widen(x[q].v[k]) - mean : 0.0f;
-                    square += d * d;
-                }
-            }
-        }
+        const float own = r.own_sum(0.0f, [&](float &s, int q, int k) { s += x[q][k]; });
+        const float mean = r.sum(own, room, 0) * per_value;
+        const float square = r.own_sum(0.0f, [&](float &s, int q, int k) {
+            const float d = x[q][k] - mean;
+            s += d * d;
+        });
         const float rstd = 1.0f / sqrtf(r.sum(square, room, 1) * per_value + a.eps);
         if (r.lane == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -121,10 +139,10 @@ __global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads)) void k_no
         T *y = (T *)a.y + row * a.y_stride;
 #pragma unroll
         for (int q = 0; q < kPer; ++q) {
-            typename Row::Values out;
+            float out[kVec];
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) out.v[k] = (T)((widen(x[q].v[k]) - mean) * rstd * weight[q][k] + bias[q][k]);
-            store_pack(y + r.column(q), r.valid(q), out);
+            for (int k = 0; k < kVec; ++k) out[k] = (x[q][k] - mean) * rstd * widen(weight[q].v[k]) + widen(bias[q].v[k]);
+            Raw<T>::of(out).store(y + r.column(q));
             if (Row::kAhead) x[q] = next[q];
         }
     }
@@ -133,7 +151,8 @@ __global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads)) void k_no
 // dx row by row as above, and what the rows a workgroup meets add to the weights' gradients, in registers; at the end
 // the workgroup's rows are added up and put down as one part.
 template <class T, class W, int kLanes, int kEach>
-__global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads)) void k_norm_backward_rows(NormArgs a)
+__global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads), (NormRow<T, W, kLanes, kEach>::waves(kNormBackwardWaves))) void
+k_norm_backward_rows(NormArgs a)
 {
     using Row = NormRow<T, W, kLanes, kEach>;
     constexpr int kVec = Row::kVec, kPer = Row::kPer;
@@ -141,35 +160,38 @@ __global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads)) void k_no
     __shared__ float added[Row::kRows > 1 ? Row::kThreads * kEach : 1];
     const Row r(a.width);
     const float per_value = 1.0f / (float)a.width;
-    float weight[kPer][kVec], dw[kPer][kVec] = {}, db[kPer][kVec] = {};
+    Pack<W, kVec> weight[kPer];
+    float dw[kPer][kVec] = {}, db[kPer][kVec] = {};
     r.load_weights((const W *)a.weight, 1.0f, weight);
-    typename Row::Values x[kPer], dy[kPer], next_x[kPer], next_dy[kPer];
+    Raw<T> x[kPer], dy[kPer], next_x[kPer], next_dy[kPer];
     uint32_t row = blockIdx.x * Row::kRows + r.row_in_block;
-    const uint32_t step = gridDim.x * Row::kRows;
+    const uint32_t step = gridDim.x * Row::kRows, last = a.rows - 1;
     int half = 0;
-    if (Row::kAhead && row < a.rows) {
-        r.load((const T *)a.x + row * a.x_stride, x);
-        r.load((const T *)a.dy + row * a.y_stride, dy);
-    }
+    // a row's mean and rstd are asked for before its values: loads come back in order, and what was asked for late would
+    // make the values of the next row be waited for with it
+    float mean = 0.0f, rstd = 0.0f, next_mean = 0.0f, next_rstd = 0.0f;
+    const auto fetch = [&](uint32_t of, float &m, float &s, Raw<T>(&to_x)[kPer], Raw<T>(&to_dy)[kPer]) {
+        m = a.mean_in[of], s = a.rstd_in[of];
+        r.load((const T *)a.x + of * a.x_stride, to_x);
+        r.load((const T *)a.dy + of * a.y_stride, to_dy);
+    };
+    if (Row::kAhead) fetch(min(row, last), mean, rstd, x, dy);
     for (; row < a.rows; row += step) {
-        if (!Row::kAhead) {
-            r.load((const T *)a.x + row * a.x_stride, x);
-            r.load((const T *)a.dy + row * a.y_stride, dy);
-        } else if (a.rows - row > step) {
-            r.load((const T *)a.x + (row + step) * a.x_stride, next_x);
-            r.load((const T *)a.dy + (row + step) * a.y_stride, next_dy);
-        }
-        const float mean = a.mean_in[row], rstd = a.rstd_in[row];
-        float2 sums = make_float2(0.0f, 0.0f);
+        if (Row::kAhead)
+            fetch(last - row > step ? row + step : last, next_mean, next_rstd, next_x, next_dy);
+        else
+            fetch(row, mean, rstd, x, dy);
+        float2 sums = r.own_sum(make_float2(0.0f, 0.0f), [&](float2 &s, int q, int k) {
+            const float g = dy[q][k] * widen(weight[q].v[k]);
+            s.x += g;
+            s.y += g * ((x[q][k] - mean) * rstd);
+        });
 #pragma unroll
         for (int q = 0; q < kPer; ++q)
 #pragma unroll
             for (int k = 0; k < kVec; ++k) {
-                const float d = widen(dy[q].v[k]), xh = (widen(x[q].v[k]) - mean) * rstd, g = d * weight[q][k];
-                sums.x += g;
-                sums.y += g * xh;
-                dw[q][k] += d * xh;
-                db[q][k] += d;
+                dw[q][k] += dy[q][k] * ((x[q][k] - mean) * rstd);
+                db[q][k] += dy[q][k];
             }
         if (a.dx) {
             sums = r.sum(sums, room, half);
@@ -178,18 +200,17 @@ __global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads)) void k_no
             T *dx = (T *)a.dx + row * a.dx_stride;
 #pragma unroll
             for (int q = 0; q < kPer; ++q) {
-                typename Row::Values out;
+                float out[kVec];
 #pragma unroll
-                for (int k = 0; k < kVec; ++k) {
-                    const float xh = (widen(x[q].v[k]) - mean) * rstd;
-                    out.v[k] = (T)(rstd * (widen(dy[q].v[k]) * weight[q][k] - c1 - xh * c2));
-                }
-                store_pack(dx + r.column(q), r.valid(q), out);
+                for (int k = 0; k < kVec; ++k) out[k] = rstd * (dy[q][k] * widen(weight[q].v[k]) - c1 - (x[q][k] - mean) * rstd * c2);
+                Raw<T>::of(out).store(dx + r.column(q));
             }
         }
-        if (Row::kAhead)
+        if (Row::kAhead) {
+            mean = next_mean, rstd = next_rstd;
 #pragma unroll
             for (int q = 0; q < kPer; ++q) x[q] = next_x[q], dy[q] = next_dy[q];
+        }
     }
     if (!a.parts) return;
 #pragma unroll
@@ -203,10 +224,10 @@ __global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads)) void k_no
             for (int v = 0; v < kEach; ++v) added[(r.row_in_block * kEach + v) * kLanes + r.lane] = own[v / kVec][v % kVec];
             __syncthreads();
             for (uint32_t i = threadIdx.x; i < (uint32_t)(kEach * kLanes); i += Row::kThreads) {
-                const uint32_t v = i / kLanes, l = i % kLanes, j = (v / kVec * kLanes + l) * kVec + v % kVec;
+                const uint32_t v = i / kLanes, l = i % kLanes, j = min((v / kVec * kLanes + l) * kVec, a.width - kVec) + v % kVec;
                 float sum = 0.0f;
                 for (int g = 0; g < Row::kRows; ++g) sum += added[g * kEach * kLanes + i];
-                if (j < a.width) part[j] = sum;
+                part[j] = sum;
             }
         } else {
 #pragma unroll
@@ -214,13 +235,13 @@ __global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads)) void k_no
                 Pack<float, kVec> out;
 #pragma unroll
                 for (int k = 0; k < kVec; ++k) out.v[k] = own[q][k];
-                store_pack(part + r.column(q), r.valid(q), out);
+                *(Pack<float, kVec> *)(part + r.column(q)) = out;
             }
         }
     }
 }
 
-// Rows too long for registers.
+// Rows too long for registers, or shorter than a pack.
 template <class T, class W>
 __global__ __launch_bounds__(kNormThreads) void k_norm_forward(NormArgs a)
 {
@@ -317,6 +338,7 @@ template <class Go>
 static bool norm_row(uint32_t width, Go go)
 {
     using std::integral_constant;
+    if (width < 8) return false;  // less than a pack
     const auto with = [&](auto lanes, auto each) {
         if (width > (uint32_t)(lanes.value * each.value)) return false;
         go(lanes, each);
@@ -328,9 +350,13 @@ static bool norm_row(uint32_t width, Go go)
            with(integral_constant<int, 1024>(), integral_constant<int, 16>());
 }
 
-constexpr uint32_t kNormBlocksPerUnit = 4;
 constexpr uint32_t kNormLongParts = 64;
-static uint32_t norm_most_parts(uint32_t rows) { return std::max(1u, std::min(rows, std::max(kNormLongParts, kNormBlocksPerUnit * compute_units()))); }
+template <class Row>
+static uint32_t norm_blocks(uint32_t rows, int most_waves)
+{
+    return std::min((rows + Row::kRows - 1) / Row::kRows, compute_units() * (uint32_t)(Row::waves(most_waves) * 256 / Row::kThreads));
+}
+static uint32_t norm_most_parts(uint32_t rows) { return std::max(1u, std::min(rows, std::max(kNormLongParts, 4 * compute_units()))); }
 static size_t norm_workspace(const pilc_norm_shape &s)
 {
     return std::max<size_t>(256, 2 * sizeof(float) * (size_t)norm_most_parts(s.rows) * s.width);
@@ -373,13 +399,12 @@ int pilc_norm_forward(const pilc_norm_shape *shape, const void *x_dev, const voi
     NormArgs a = {};
     a.x = x_dev, a.weight = weight_dev, a.bias = bias_dev, a.y = y_dev, a.mean = mean_dev, a.rstd = rstd_dev;
     a.x_stride = shape->x_stride, a.y_stride = shape->y_stride, a.rows = shape->rows, a.width = shape->width, a.eps = shape->eps;
-    const uint32_t most = kNormBlocksPerUnit * compute_units();
     return by_types(shape->dtype, shape->weight_type, [&](auto *t, auto *w) {
         using T = std::remove_pointer_t<decltype(t)>;
         using W = std::remove_pointer_t<decltype(w)>;
         const bool done = norm_row(a.width, [&](auto lanes, auto each) {
             using Row = NormRow<T, W, decltype(lanes)::value, decltype(each)::value>;
-            const uint32_t blocks = std::min((a.rows + Row::kRows - 1) / Row::kRows, most);
+            const uint32_t blocks = norm_blocks<Row>(a.rows, kNormForwardWaves);
             k_norm_forward_rows<T, W, decltype(lanes)::value, decltype(each)::value><<<blocks, Row::kThreads, 0, (hipStream_t)hip_stream>>>(a);
         });
         if (!done) k_norm_forward<T, W><<<row_blocks(a.rows), kNormThreads, 0, (hipStream_t)hip_stream>>>(a);
@@ -411,14 +436,13 @@ int pilc_norm_backward(const pilc_norm_shape *shape, const void *dy_dev, const v
     a.dbias = dbias_dev, a.x_stride = shape->x_stride, a.y_stride = shape->y_stride, a.dx_stride = shape->dx_stride;
     a.rows = shape->rows, a.width = shape->width;
     if (dweight_dev || dbias_dev) a.parts = (float *)workspace_dev;
-    const uint32_t most = kNormBlocksPerUnit * compute_units();
     const hipStream_t stream = (hipStream_t)hip_stream;
     return by_types(shape->dtype, shape->weight_type, [&](auto *t, auto *w) {
         using T = std::remove_pointer_t<decltype(t)>;
         using W = std::remove_pointer_t<decltype(w)>;
         const bool done = norm_row(a.width, [&](auto lanes, auto each) {
             using Row = NormRow<T, W, decltype(lanes)::value, decltype(each)::value>;
-            a.num_parts = std::min((a.rows + Row::kRows - 1) / Row::kRows, most);
+            a.num_parts = norm_blocks<Row>(a.rows, kNormBackwardWaves);
             if (a.rows)
                 k_norm_backward_rows<T, W, decltype(lanes)::value, decltype(each)::value><<<a.num_parts, Row::kThreads, 0, stream>>>(a);
         });
