@@ -65,6 +65,23 @@ struct Raw {
         struct __attribute__((packed, aligned(sizeof(T)))) At { u32x4_t v; };
         ((At *)p)->v = bits;
     }
+    // Nothing worked out from the values before is kept for after: widened, they would take twice the registers.
+    __device__ void forget() { asm volatile("" : "+v"(bits)); }
+    // -inf in place of the first `count` values
+    __device__ void rule_out(int count)
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) bits[k] = k < count ? 0xFF800000u : bits[k];
+        } else {
+            constexpr uint32_t kNone = __is_same(T, __bf16) ? 0xFF80u : 0xFC00u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t low = (bits[i] & 0xFFFF0000u) | kNone;
+                bits[i] = 2 * i + 1 < count ? kNone << 16 | kNone : 2 * i < count ? low : bits[i];
+            }
+        }
+    }
     __device__ float operator[](int k) const { return widen(__builtin_bit_cast(Pack<T, kVec>, bits).v[k]); }
     __device__ static Raw of(const float (&v)[kVec])
     {
@@ -143,6 +160,10 @@ __device__ __forceinline__ V block_reduce(V v, Op op, V *room)
     return v;
 }
 
+// What is not a number is passed over.
+struct MaxFloat {
+    __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
 struct Max {
     template <class V>
     __device__ __forceinline__ V operator()(V a, V b) const { return a > b ? a : b; }

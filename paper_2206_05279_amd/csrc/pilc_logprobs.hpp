@@ -4,7 +4,7 @@
 namespace pilc {
 
 constexpr int kMaxTop = 32;
-constexpr int kLogitsThreads = 256;
+
 
 struct LogitsArgs {
     const void *x;
@@ -16,6 +16,9 @@ struct LogitsArgs {
     void *grad;
     uint64_t stride, grad_stride;
     uint32_t rows, num_sym, top, target_type;
+    uint32_t splits, span;  // a row goes into `splits` runs of `span` values, the last one maybe shorter
+    float4 *part;           // of each run: its largest, sum, sum of products (see Law)
+    uint64_t *part_top;     // and its `top` keys, best first, 0 where there are fewer
 };
 
 __device__ __forceinline__ int64_t target_of(const LogitsArgs &a, uint32_t row)
@@ -25,118 +28,530 @@ __device__ __forceinline__ int64_t target_of(const LogitsArgs &a, uint32_t row)
                                        : ((const int64_t *)a.target)[row];
 }
 
-// Integers in the order of the values they are made of, and the lower symbol first among equals.
-__device__ __forceinline__ uint64_t key_of(float x, uint32_t sym)
+// Integers in the order of the values they are made of; of a key, the lower symbol's is the higher among equals.
+__device__ __forceinline__ uint32_t order_of(float x)
 {
     const uint32_t b = __float_as_uint(x + 0.0f);  // no -0
-    const uint32_t order = b & 0x80000000u ? ~b : b | 0x80000000u;
-    return (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+constexpr uint32_t kOrderNone = 0x007FFFFFu;  // of -inf
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t sym) { return (uint64_t)order_of(x) << 32 | (0xFFFFFFFFu - sym); }
 __device__ __forceinline__ float value_of(uint64_t key)
 {
     const uint32_t order = (uint32_t)(key >> 32);
     return __uint_as_float(order & 0x80000000u ? order & 0x7FFFFFFFu : ~order);
 }
 
-struct Law {
-    float max, log_total, entropy;  // lse = max + log_total
+// How exponentials of a row's values are taken: 2^(x rate - shift), one fused multiply-add and one power a value.  shift
+// is the largest value times rate, rounded, so that all powers are the same factor 2^off too large; it cancels in
+// probabilities and is taken out of logarithms.  Where the product would overflow, values that differ at all differ by
+// so much that any rate does.
+struct Scale {
+    float max, rate, shift, off;
+
+    __device__ explicit Scale(float m) : max(m)
+    {
+        const bool plain = fabsf(m) < 1e38f;
+        rate = plain ? kLog2e : 0x1p-60f;
+        shift = m == -kInf ? 0.0f : m * rate;
+        off = plain ? __builtin_fmaf(m, rate, -shift) : 0.0f;
+    }
+    __device__ float power(float x) const { return __builtin_fmaf(x, rate, -shift); }
+};
+constexpr float kLn2 = 0.693147180559945309f;
+// No 32-bit power of two is left here: what a power is multiplied with need not go on falling, and may not be -inf.
+constexpr float kLeast = -200.0f;
+
+// What is known of a row or of a part of it: its largest value, the sum of the powers of its values and the sum of their
+// products with the exponents.
+struct Tally {
+    float max, total, inside;
 };
 
-// max, sum e^(x - max) and sum (x - max) e^(x - max) of a row as what is told of it.
-__device__ __forceinline__ Law law_of(float max, float total, float inside)
+// Both tallies' values together.
+__device__ __forceinline__ Tally both(Tally a, Tally b)
 {
-    if (max == -kInf && total == 0.0f) return {-kInf, 0.0f, 0.0f};
-    const float log_total = logf(total);
-    if (!(log_total == log_total)) max = log_total;  // a NaN, or +inf less itself
-    return {max, log_total, log_total - inside / total};
+    const float max = fmaxf(a.max, b.max);
+    // the exponents' difference as the powers were taken, each with its own rounding of the shift
+    const Scale of(max), sa(a.max), sb(b.max);
+    const float da = a.max == -kInf ? kLeast : fmaxf(sa.shift - of.shift, kLeast), db = b.max == -kInf ? kLeast : fmaxf(sb.shift - of.shift, kLeast);
+    const float fa = exp2_fast(da), fb = exp2_fast(db);
+    return {max, a.total * fa + b.total * fb, (a.inside + da * a.total) * fa + (b.inside + db * b.total) * fb};
 }
 
-__device__ __forceinline__ float target_logp(const LogitsArgs &a, const Law &law, int64_t t, float at)
-{
-    if (t < 0) return 0.0f;
-    if (t >= (int64_t)a.num_sym) return __builtin_nanf("");
-    return law.max == -kInf ? -kInf : (at - law.max) - law.log_total;
-}
+struct Law {
+    float max, log_total, entropy, total;  // lse = max + log_total
 
-template <class T>
-__device__ void gradient_row(const T *x, T *grad, uint32_t num_sym, int64_t t, float lse, float entropy, float up, float up_entropy)
-{
-    const float a = t < 0 ? 0.0f : up, b = up_entropy;
-    const bool zeros = (a == 0.0f && b == 0.0f) || lse == -kInf;
-    const bool nothing = t >= (int64_t)num_sym;
-    for (uint32_t j = threadIdx.x; j < num_sym; j += blockDim.x) {
-        float d = 0.0f;
-        if (!zeros) {
-            const float lp = widen(x[j]) - lse;
-            const float p = exp2_fast(lp * kLog2e);  // 0 below -88: what it is multiplied with need not go on falling
-            d = -p * (a + b * (fmaxf(lp, -100.0f) + entropy));
-            if ((int64_t)j == t) d += a;
-            if (nothing) d = __builtin_nanf("");
+    // An empty row: max -inf.  A NaN, or +inf less itself, in the sum: all NaN.
+    __device__ explicit Law(Tally t) : max(t.max), total(t.total)
+    {
+        if (t.max == -kInf && t.total == 0.0f) {
+            log_total = entropy = 0.0f;
+            return;
         }
-        grad[j] = (T)d;
+        const float log = logf(t.total);
+        entropy = log - kLn2 * t.inside / t.total;
+        log_total = log - kLn2 * Scale(t.max).off;
+        if (!(log == log)) max = log_total = entropy = log;
+    }
+    __device__ float lse() const { return max + log_total; }
+    __device__ float logp(float x) const { return max == -kInf ? -kInf : (x - max) - log_total; }
+};
+
+// A row, or a run of it, in registers: kLanes lanes hold kPer packs of 16 bytes each.  A pack that would reach over the
+// end begins earlier, and what another holds of it already is ruled out.  Rows need a pack's values at least.
+template <class T, int kLanes, int kPer>
+struct LogitsRow {
+    static constexpr int kVec = 16 / sizeof(T);
+    static constexpr int kThreads = kLanes > 256 ? kLanes : 256;
+    static constexpr int kRows = kThreads / kLanes;  // that a workgroup has in hand
+    static constexpr int kWithin = kLanes < 64 ? kLanes : 64, kWaves = kLanes > 64 ? kLanes / 64 : 1;
+    static constexpr bool kAhead = kPer <= 2;  // the next run is asked for early; larger ones have the other workgroups beside them
+    static constexpr uint32_t kValues = kLanes * kPer * kVec;
+
+    uint32_t lane, row_in_block;
+
+    __device__ LogitsRow() : lane(threadIdx.x % kLanes), row_in_block(kRows > 1 ? threadIdx.x / kLanes : 0) {}
+    __device__ uint32_t place(int q, uint32_t begin) const { return begin + (q * kLanes + lane) * kVec; }
+    __device__ uint32_t column(int q, uint32_t begin, uint32_t end) const { return min(place(q, begin), end - kVec); }
+    __device__ int twice(int q, uint32_t begin, uint32_t end) const
+    {
+        return (int)min(place(q, begin) - column(q, begin, end), (uint32_t)kVec);
+    }
+    __device__ void load(const T *p, uint32_t begin, uint32_t end, Raw<T> (&x)[kPer]) const
+    {
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) x[q] = Raw<T>::load(p + column(q, begin, end));
+    }
+    __device__ void rule_out(uint32_t begin, uint32_t end, Raw<T> (&x)[kPer]) const
+    {
+        if (end - begin < kValues)
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) x[q].rule_out(twice(q, begin, end));
+    }
+    __device__ static void forget(Raw<T> (&x)[kPer])
+    {
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) x[q].forget();
+    }
+    __device__ float largest(const Raw<T> (&x)[kPer]) const
+    {
+        float m[2] = {-kInf, -kInf};
+#pragma unroll
+        for (int q = 0; q < kPer; ++q)
+#pragma unroll
+            for (int k = 0; k < kVec; k += 2) m[0] = fmaxf(m[0], x[q][k]), m[1] = fmaxf(m[1], x[q][k + 1]);
+        return fmaxf(m[0], m[1]);
+    }
+    // f(order, symbol) for each of the lane's values
+    template <class F>
+    __device__ void each(Raw<T> (&x)[kPer], uint32_t begin, uint32_t end, F f) const
+    {
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) {
+            x[q].forget();
+            const uint32_t column_q = column(q, begin, end);
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) f(order_of(x[q][k]), column_q + k);
+        }
+    }
+    // The same from memory, in little code
+    template <class F>
+    __device__ void again(const T *p, uint32_t begin, uint32_t end, F f) const
+    {
+#pragma unroll 1
+        for (int q = 0; q < kPer; ++q)
+#pragma unroll 1
+            for (uint32_t j = place(q, begin); j < min(place(q, begin) + kVec, end); ++j) f(order_of(widen(p[j])), j);
+    }
+    // The row's tally in all its lanes; `room` holds 2 * kWaves, its halves are used in turn.
+    __device__ Tally tally(const Raw<T> (&x)[kPer], float own, Tally *room, int half) const
+    {
+        const float max = lanes_reduce<kWithin>(own, MaxFloat());
+        const Scale scale(max);
+        float total[2] = {0.0f, 0.0f}, inside[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int q = 0; q < kPer; ++q)
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) {
+                const float z = scale.power(x[q][k]), e = exp2_fast(z);
+                total[k & 1] += e;
+                inside[k & 1] = __builtin_fmaf(e, fmaxf(z, kLeast), inside[k & 1]);
+            }
+        Tally t = {max, lanes_reduce<kWithin>(total[0] + total[1], Sum()), lanes_reduce<kWithin>(inside[0] + inside[1], Sum())};
+        if constexpr (kWaves > 1) {
+            room += half * kWaves;
+            if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = t;
+            __syncthreads();
+            t = room[threadIdx.x & (kWaves - 1)];
+#pragma unroll
+            for (int d = 1; d < kWaves; d *= 2) {
+                const Tally o = {__shfl_xor(t.max, d, 64), __shfl_xor(t.total, d, 64), __shfl_xor(t.inside, d, 64)};
+                t = both(t, o);
+            }
+        }
+        return t;
+    }
+};
+
+// The `top` best of what the threads of a workgroup hold.  `each` calls its argument with the order (see order_of) and
+// symbol of every value of the calling thread, `again` does the same for the rare way below, `best` is the highest order among them; `put` is called, once for each
+// place in 0 .. top-1 and by some thread, with the place and the key that belongs there, or 0.
+//
+// The top-th best of the threads' best values has `top` values at least that are as good, and few more in what a model
+// answers with; those are put side by side, and each one's place is the number of better ones.  Rows with many equal
+// values may have too many of them: then the best that is worse than the last is looked for `top` times.
+constexpr int kMostPicked = 256;
+template <int kThreads>
+struct PickRoom {
+    uint32_t best[kThreads];
+    uint64_t picked[kMostPicked], rounds[kThreads / 64];
+    uint32_t count;
+};
+template <int kThreads, int kBits, class Each, class Again, class Put>
+__device__ void pick_top(uint32_t top, uint32_t best, Each each, Again again, Put put, PickRoom<kThreads> &room)
+{
+    constexpr int kEach = kThreads / 64;
+    __syncthreads();  // `room` may be in use from a row before
+    room.best[threadIdx.x] = best;
+    if (threadIdx.x == 0) room.count = 0;
+    __syncthreads();
+    // the highest order that `top` threads' best reach, bit by bit from the top; kBits is what the type's values differ in
+    uint32_t b[kEach], line = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) b[i] = room.best[i * 64 + (threadIdx.x & 63)];
+    for (int bit = 31; bit >= 32 - kBits; --bit) {
+        const uint32_t next = line | 1u << bit;
+        uint32_t reach = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) reach += (uint32_t)__builtin_popcountll(__ballot(b[i] >= next));
+        if (reach >= top) line = next;
+    }
+    line = max(line, kOrderNone + 1);  // -inf is no alternative
+    if (best >= line)
+        each([&](uint32_t order, uint32_t sym) {
+            if (order < line) return;
+            const uint32_t at = atomicAdd(&room.count, 1u);
+            if (at < kMostPicked) room.picked[at] = (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
+        });
+    __syncthreads();
+    const uint32_t count = room.count;
+    if (count <= (uint32_t)kMostPicked) {
+        for (uint32_t i = threadIdx.x; i < count; i += kThreads) {
+            const uint64_t key = room.picked[i];
+            uint32_t better = 0;
+            for (uint32_t j = 0; j < count; ++j) better += room.picked[j] > key;
+            if (better < top) put(better, key);
+        }
+        for (uint32_t i = count + threadIdx.x; i < top; i += kThreads) put(i, (uint64_t)0);
+        return;
+    }
+    uint64_t below = ~0ull;
+    for (uint32_t i = 0; i < top; ++i) {
+        uint64_t next = 0;
+        if (best >= line)
+            again([&](uint32_t order, uint32_t sym) {
+                const uint64_t key = (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
+                if (order >= line && key < below && key > next) next = key;
+            });
+        below = block_reduce<kThreads / 64>(next, Max(), room.rounds);
+        if (threadIdx.x == 0) put(i, below);
+    }
+}
+template <class T>
+constexpr int kOrderBits = sizeof(T) == 4 ? 32 : __is_same(T, __bf16) ? 16 : 19;
+
+__device__ __forceinline__ void put_alternative(const LogitsArgs &a, const Law &law, uint32_t row, uint32_t place, uint64_t key)
+{
+    const size_t at = (size_t)row * a.top + place;
+    const bool none = !(law.max == law.max);  // NaN or +inf in the row
+    a.top_sym[at] = key && !none ? (int32_t)(0xFFFFFFFFu - (uint32_t)key) : -1;
+    a.top_logp[at] = none ? __builtin_nanf("") : key ? law.logp(value_of(key)) : -kInf;
+}
+
+// The gradient of one pack's values: 2^z (from + slope z), and `up` more at the target.
+template <class T>
+__device__ __forceinline__ void put_gradient(const Raw<T> &x, T *grad, uint32_t column, int twice, const Scale &scale, float from, float slope,
+                                             bool in, int64_t t, float up, bool zeros)
+{
+    constexpr int kVec = 16 / sizeof(T);
+    float d[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        const float z = fmaxf(scale.power(x[i]), kLeast);
+        d[i] = exp2_fast(z) * __builtin_fmaf(slope, z, from);
+    }
+    const uint32_t k = (uint32_t)t - column;
+    if (in && k < (uint32_t)kVec)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) d[i] += i == (int)k ? up : 0.0f;
+    if (zeros)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) d[i] = 0.0f;
+    if (twice == 0) {
+        Raw<T>::of(d).store(grad + column);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (i >= twice) grad[column + i] = (T)d[i];
     }
 }
 
-template <class T, bool kTrain>
-__global__ __launch_bounds__(kLogitsThreads) void k_logprobs(LogitsArgs a)
+// Rows, or runs of rows, one after another; a row that is one run is finished here.  kTrain: whole rows, and their
+// gradient from the same registers.
+template <class T, int kLanes, int kPer, bool kTrain>
+__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logits(LogitsArgs a)
 {
-    constexpr int kWaves = kLogitsThreads / 64;
-    __shared__ float room[kWaves];
-    __shared__ uint64_t key_room[kWaves];
-    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const T *x = (const T *)a.x + row * a.stride;
-        float max = -kInf;
-        for (uint32_t j = threadIdx.x; j < a.num_sym; j += kLogitsThreads) max = fmaxf(max, widen(x[j]));
-        max = block_reduce<kWaves>(max, Max(), room);
-        const float from = max == -kInf ? 0.0f : max;
-        float total = 0.0f, inside = 0.0f;
-        for (uint32_t j = threadIdx.x; j < a.num_sym; j += kLogitsThreads) {
-            const float z = widen(x[j]) - from, e = exp2_fast(z * kLog2e);
-            total += e;
-            inside += e * fmaxf(z, -3e38f);
+    using Row = LogitsRow<T, kLanes, kPer>;
+    constexpr int kVec = Row::kVec;
+    __shared__ Tally room[2 * Row::kWaves];
+    const Row r;
+    const uint64_t items = (uint64_t)a.rows * a.splits, step = (uint64_t)gridDim.x * Row::kRows;
+    uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block;
+    Raw<T> x[kPer], next[kPer];
+    // what comes with a row is asked for before its values: loads come back in order
+    struct Given {
+        int64_t t;
+        float up, up_entropy;
+    } given = {-1, 0.0f, 0.0f}, next_given = given;
+    int half = 0;
+    const auto fetch = [&](uint64_t i, Given &to, Raw<T>(&to_x)[kPer]) {
+        i = min(i, items - 1);
+        const uint32_t row = (uint32_t)(a.splits == 1 ? i : i / a.splits), begin = (uint32_t)(i - (uint64_t)row * a.splits) * a.span;
+        if (a.target && (kTrain || a.splits == 1)) to.t = target_of(a, row);
+        if (kTrain) {
+            to.up = a.up_logp[row];
+            if (a.up_entropy) to.up_entropy = a.up_entropy[row];
         }
-        total = block_reduce<kWaves>(total, Sum(), room);
-        inside = block_reduce<kWaves>(inside, Sum(), room);
-        const Law law = law_of(max, total, inside);
-        const int64_t t = a.target ? target_of(a, row) : -1;
-        if (threadIdx.x == 0) {
-            const bool in = t >= 0 && t < (int64_t)a.num_sym;
-            if (a.logp) a.logp[row] = target_logp(a, law, t, in ? widen(x[t]) : 0.0f);
-            if (a.entropy) a.entropy[row] = law.entropy;
-            if (a.lse) a.lse[row] = law.max + law.log_total;
-        }
-        if constexpr (kTrain) {
-            __syncthreads();  // the gradient may lie where the logits are: the target's is read above
-            gradient_row<T>(x, (T *)a.grad + row * a.grad_stride, a.num_sym, t, law.max + law.log_total, law.entropy, a.up_logp[row],
-                            a.up_entropy ? a.up_entropy[row] : 0.0f);
-        } else {
-            uint64_t below = ~0ull;
-            const bool none = !(law.max == law.max);  // NaN or +inf in the row
-            for (uint32_t k = 0; k < a.top; ++k) {
-                uint64_t best = 0;
-                for (uint32_t j = threadIdx.x; j < a.num_sym; j += kLogitsThreads) {
-                    const uint64_t key = key_of(widen(x[j]), j);
-                    if (key < below && key > best) best = key;
+        r.load((const T *)a.x + row * a.stride, begin, min(begin + a.span, a.num_sym), to_x);
+    };
+    if (Row::kAhead) fetch(item, given, x);
+    for (; item < items; item += step) {
+        if (Row::kAhead)
+            fetch(item + step, next_given, next);
+        else
+            fetch(item, given, x);
+        const uint32_t row = (uint32_t)(a.splits == 1 ? item : item / a.splits), begin = (uint32_t)(item - (uint64_t)row * a.splits) * a.span;
+        const uint32_t end = min(begin + a.span, a.num_sym);
+        const int64_t t = given.t;
+        r.rule_out(begin, end, x);
+        const float own = r.largest(x);
+        r.forget(x);
+        const Tally tally = r.tally(x, own, room, half);
+        r.forget(x);
+        half ^= 1;
+        if (!kTrain && a.splits > 1) {
+            if (r.lane == 0) a.part[item] = make_float4(tally.max, tally.total, tally.inside, 0.0f);
+            if constexpr (kLanes == 256)
+                if (a.top) {
+                    __shared__ PickRoom<256> pick;
+                    pick_top<256, kOrderBits<T>>(
+                        a.top, order_of(own),
+                        [&](auto f) { r.each(x, begin, end, f); },
+                        [&](auto f) { r.again((const T *)a.x + row * a.stride, begin, end, f); },
+                        [&](uint32_t place, uint64_t key) { a.part_top[item * a.top + place] = key; }, pick);
                 }
-                below = block_reduce<kWaves>(best, Max(), key_room);
-                if (threadIdx.x == 0) {
-                    const float v = below ? value_of(below) : -kInf;
-                    const size_t at = (size_t)row * a.top + k;
-                    const bool there = !none && v > -kInf;
-                    a.top_sym[at] = there ? (int32_t)(0xFFFFFFFFu - (uint32_t)below) : -1;
-                    a.top_logp[at] = none ? __builtin_nanf("") : there ? (v - law.max) - law.log_total : -kInf;
+        } else {
+            const Law law(tally);
+            if (r.lane == 0) {
+                if (a.entropy) a.entropy[row] = law.entropy;
+                if (a.lse) a.lse[row] = law.lse();
+                if (a.logp && (t < 0 || t >= (int64_t)a.num_sym)) a.logp[row] = t < 0 ? 0.0f : __builtin_nanf("");
+            }
+            const bool in = t >= 0 && t < (int64_t)a.num_sym;
+            if (a.logp && in)
+#pragma unroll
+                for (int q = 0; q < kPer; ++q) {
+                    const uint32_t k = (uint32_t)t - r.column(q, begin, end);
+                    if (k < (uint32_t)kVec && (int)k >= r.twice(q, begin, end)) {
+                        float at = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < kVec; ++i) at = i == (int)k ? x[q][i] : at;
+                        a.logp[row] = law.logp(at);
+                    }
+                }
+            if constexpr (kTrain) {
+                const float up = t < 0 ? 0.0f : given.up, up_entropy = given.up_entropy;
+                // grad = e (from + slope z), ln p being ln 2 z - ln total
+                const Scale scale(tally.max);
+                float from = -(up + up_entropy * (law.entropy - logf(law.total))) / law.total, slope = -up_entropy * kLn2 / law.total;
+                const bool zeros = (up == 0.0f && up_entropy == 0.0f) || law.max == -kInf;
+                if (t >= (int64_t)a.num_sym || !(law.max == law.max)) from = __builtin_nanf("");
+                T *grad = (T *)a.grad + row * a.grad_stride;
+#pragma unroll
+                for (int q = 0; q < kPer; ++q)
+                    put_gradient(x[q], grad, r.column(q, begin, end), r.twice(q, begin, end), scale, from, slope, in, t, up, zeros);
+            } else if (a.top) {
+                const auto each = [&](auto f) { r.each(x, begin, end, f); };
+                if constexpr (kLanes == 256) {
+                    __shared__ PickRoom<256> pick;
+                    pick_top<256, kOrderBits<T>>(
+                        a.top, order_of(own), each, [&](auto f) { r.again((const T *)a.x + row * a.stride, begin, end, f); },
+                        [&](uint32_t place, uint64_t key) { put_alternative(a, law, row, place, key); }, pick);
+                } else {
+                    // few values a lane: the best that is worse than the last, `top` times
+                    uint64_t below = ~0ull;
+                    for (uint32_t i = 0; i < a.top; ++i) {
+                        uint64_t best = 0;
+                        each([&](uint32_t order, uint32_t sym) {
+                            const uint64_t key = (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
+                            if (order > kOrderNone && key < below && key > best) best = key;
+                        });
+                        const uint32_t high = lanes_reduce<Row::kWithin>((uint32_t)(best >> 32), Max());
+                        const uint32_t low = lanes_reduce<Row::kWithin>(best >> 32 == high ? (uint32_t)best : 0u, Max());
+                        below = (uint64_t)high << 32 | low;
+                        if (r.lane == 0) put_alternative(a, law, row, i, below);
+                    }
                 }
             }
         }
+        if (Row::kAhead) {
+            given = next_given;
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) x[q] = next[q];
+        }
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(kLogitsThreads) void k_logprobs_grad(LogitsArgs a)
+// The runs of a row put together, a workgroup a row.
+__global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type)
 {
-    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x)
-        gradient_row<T>((const T *)a.x + row * a.stride, (T *)a.grad + row * a.grad_stride, a.num_sym, target_of(a, row), a.lse_in[row],
-                        a.up_entropy ? a.entropy_in[row] : 0.0f, a.up_logp[row], a.up_entropy ? a.up_entropy[row] : 0.0f);
+    __shared__ Tally room[4];
+    __shared__ PickRoom<256> pick;
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        Tally t = {-kInf, 0.0f, 0.0f};
+        for (uint32_t s = threadIdx.x; s < a.splits; s += 256) {
+            const float4 p = a.part[(uint64_t)row * a.splits + s];
+            t = both(t, {p.x, p.y, p.z});
+        }
+        const auto over = [&](int lanes) {
+            for (int d = 1; d < lanes; d *= 2) t = both(t, {__shfl_xor(t.max, d, 64), __shfl_xor(t.total, d, 64), __shfl_xor(t.inside, d, 64)});
+        };
+        over(64);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = t;
+        __syncthreads();
+        t = room[threadIdx.x & 3];
+        over(4);
+        const Law law(t);
+        if (threadIdx.x == 0) {
+            if (a.entropy) a.entropy[row] = law.entropy;
+            if (a.lse) a.lse[row] = law.lse();
+            if (a.logp) {
+                const int64_t target = target_of(a, row);
+                float at = 0.0f;
+                if (target >= 0 && target < (int64_t)a.num_sym) {
+                    const uint64_t i = row * a.stride + (uint64_t)target;
+                    at = type == PILC_F32 ? ((const float *)a.x)[i] : type == PILC_BF16 ? widen(((const bf16_t *)a.x)[i]) : widen(((const f16_t *)a.x)[i]);
+                }
+                a.logp[row] = target < 0 ? 0.0f : target >= (int64_t)a.num_sym ? __builtin_nanf("") : law.logp(at);
+            }
+        }
+        if (a.top) {
+            const uint64_t *keys = a.part_top + (uint64_t)row * a.splits * a.top;
+            const uint32_t count = a.splits * a.top;
+            uint32_t best = 0;
+            for (uint32_t i = threadIdx.x; i < count; i += 256) best = max(best, (uint32_t)(keys[i] >> 32));
+            const auto each = [&](auto f) {
+                for (uint32_t i = threadIdx.x; i < count; i += 256) f((uint32_t)(keys[i] >> 32), 0xFFFFFFFFu - (uint32_t)keys[i]);
+            };
+            pick_top<256, 32>(
+                a.top, best, each, each,
+                [&](uint32_t place, uint64_t key) { put_alternative(a, law, row, place, key); }, pick);
+        }
+    }
+}
+
+// The gradient where a row's law is known: run by run.
+template <class T, int kLanes, int kPer>
+__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logits_grad(LogitsArgs a)
+{
+    using Row = LogitsRow<T, kLanes, kPer>;
+    const Row r;
+    const uint64_t items = (uint64_t)a.rows * a.splits, step = (uint64_t)gridDim.x * Row::kRows;
+    for (uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block; item < items; item += step) {
+        const uint32_t row = (uint32_t)(a.splits == 1 ? item : item / a.splits), begin = (uint32_t)(item - (uint64_t)row * a.splits) * a.span;
+        const uint32_t end = min(begin + a.span, a.num_sym);
+        const int64_t t = target_of(a, row);
+        const float up = t < 0 ? 0.0f : a.up_logp[row], up_entropy = a.up_entropy ? a.up_entropy[row] : 0.0f;
+        const float lse = a.lse_in[row], entropy = a.up_entropy ? a.entropy_in[row] : 0.0f;
+        const bool zeros = (up == 0.0f && up_entropy == 0.0f) || lse == -kInf;
+        // p = 2^z 2^-off, ln p = ln 2 (z - off)
+        const Scale scale(lse);
+        const float less = exp2_fast(-scale.off);
+        float from = -(up + up_entropy * (entropy - kLn2 * scale.off)) * less, slope = -up_entropy * kLn2 * less;
+        if (t >= (int64_t)a.num_sym || !(lse == lse)) from = __builtin_nanf("");
+        Raw<T> x[kPer];
+        r.load((const T *)a.x + row * a.stride, begin, end, x);
+        T *grad = (T *)a.grad + row * a.grad_stride;
+        const bool in = t >= 0 && t < (int64_t)a.num_sym;
+#pragma unroll
+        for (int q = 0; q < kPer; ++q)
+            put_gradient(x[q], grad, r.column(q, begin, end), r.twice(q, begin, end), scale, from, slope, in, t, up, zeros);
+    }
+}
+
+// Rows shorter than a pack: a thread a row.  kTrain: with the gradient; kGrad: the gradient by a law that is known.
+template <class T, bool kTrain, bool kGrad>
+__global__ __launch_bounds__(256) void k_logits_short(LogitsArgs a)
+{
+    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < a.rows; i += gridDim.x * 256ull) {
+        const uint32_t row = (uint32_t)i;
+        const T *x = (const T *)a.x + row * a.stride;
+        const int64_t t = a.target ? target_of(a, row) : -1;
+        const bool in = t >= 0 && t < (int64_t)a.num_sym;
+        float largest = -kInf;
+        for (uint32_t j = 0; j < a.num_sym; ++j) largest = fmaxf(largest, widen(x[j]));
+        const Scale scale(kGrad ? a.lse_in[row] : largest);
+        float up = 0.0f, up_entropy = 0.0f, from, slope;
+        if (kTrain || kGrad) {
+            up = t < 0 ? 0.0f : a.up_logp[row];
+            up_entropy = a.up_entropy ? a.up_entropy[row] : 0.0f;
+        }
+        bool zeros = up == 0.0f && up_entropy == 0.0f, spoilt = t >= (int64_t)a.num_sym;
+        if constexpr (kGrad) {
+            const float less = exp2_fast(-scale.off), entropy = a.up_entropy ? a.entropy_in[row] : 0.0f;
+            from = -(up + up_entropy * (entropy - kLn2 * scale.off)) * less;
+            slope = -up_entropy * kLn2 * less;
+            zeros |= scale.max == -kInf;
+            spoilt |= !(scale.max == scale.max);
+        } else {
+            Tally tally = {largest, 0.0f, 0.0f};
+            for (uint32_t j = 0; j < a.num_sym; ++j) {
+                const float z = scale.power(widen(x[j])), e = exp2_fast(z);
+                tally.total += e;
+                tally.inside += e * fmaxf(z, kLeast);
+            }
+            const Law law(tally);
+            if (a.entropy) a.entropy[row] = law.entropy;
+            if (a.lse) a.lse[row] = law.lse();
+            if (a.logp) a.logp[row] = t < 0 ? 0.0f : spoilt ? __builtin_nanf("") : law.logp(widen(x[t]));
+            uint64_t below = ~0ull;
+            for (uint32_t k = 0; k < a.top; ++k) {
+                uint64_t best = 0;
+                for (uint32_t j = 0; j < a.num_sym; ++j) {
+                    const uint64_t key = key_of(widen(x[j]), j);
+                    if (key >> 32 > kOrderNone && key < below && key > best) best = key;
+                }
+                below = best;
+                put_alternative(a, law, row, k, best);
+            }
+            from = -(up + up_entropy * (law.entropy - logf(law.total))) / law.total;
+            slope = -up_entropy * kLn2 / law.total;
+            zeros |= law.max == -kInf;
+            spoilt |= !(law.max == law.max);
+        }
+        if constexpr (kTrain || kGrad) {
+            if (spoilt) from = __builtin_nanf("");
+            T *grad = (T *)a.grad + row * a.grad_stride;
+            for (uint32_t j = 0; j < a.num_sym; ++j) {
+                const float z = fmaxf(scale.power(widen(x[j])), kLeast);
+                float d = exp2_fast(z) * __builtin_fmaf(slope, z, from);
+                if (in && (int64_t)j == t) d += up;
+                grad[j] = (T)(zeros ? 0.0f : d);
+            }
+        }
+    }
 }
 
 static size_t value_bytes(uint32_t type) { return type == PILC_F32 ? 4 : 2; }
@@ -154,7 +569,119 @@ static bool logits_in_ok(const pilc_logits_shape *s, const void *logits, const v
     return logits && aligned_to(logits, value_bytes(s->dtype)) && aligned_to(target, target_bytes);
 }
 
-static size_t logits_workspace(const pilc_logits_shape &s) { return 256; }
+// How rows are gone through.  Runs are of 64 KB at most, the registers of a workgroup of 256; with few rows they are as
+// much smaller as it takes to give every compute unit two.
+struct LogitsPlan {
+    uint32_t splits, span;
+};
+constexpr uint32_t kLongestRun = 64 << 10, kShortestRun = 4 << 10;
+static uint32_t div_up(uint32_t a, uint32_t b) { return a / b + (a % b != 0); }
+static LogitsPlan logits_plan(uint32_t rows, uint32_t num_sym, uint32_t value, uint32_t longest, uint32_t shortest)
+{
+    const uint32_t vec = 16 / value, needed = div_up(num_sym, longest / value), most = div_up(num_sym, shortest / value);
+    const uint32_t wanted = div_up(2 * compute_units(), std::max(rows, 1u)), splits = std::max(needed, std::min(wanted, most));
+    const uint32_t span = div_up(div_up(num_sym, splits), vec) * vec;
+    return {div_up(num_sym, span), span};
+}
+// Whether pilc_logprobs_train keeps whole rows in registers: up to 256 KB, those of a workgroup of 1024.
+constexpr uint32_t kLongestRow = 256 << 10;
+static bool train_by_row(uint32_t rows, uint32_t num_sym, uint32_t value)
+{
+    const uint64_t bytes = (uint64_t)num_sym * value;
+    return bytes <= kLongestRow && (bytes <= kShortestRun || rows >= compute_units() / 2);
+}
+
+static size_t logits_workspace(const pilc_logits_shape &s)
+{
+    size_t most = 256;
+    const uint32_t values[] = {2, 4};
+    for (uint32_t value : values) {  // whatever the type, so that a caller need not ask for each
+        const LogitsPlan p = logits_plan(s.rows, s.num_sym, value, kLongestRun, kShortestRun);
+        const size_t runs = (size_t)s.rows * p.splits;
+        if (p.splits > 1) most = std::max(most, runs * (sizeof(float4) + sizeof(uint64_t) * s.top) + (s.top ? 0 : 2 * sizeof(float) * (size_t)s.rows));
+    }
+    return most;
+}
+
+// Calls `go` with the lanes and packs a lane for runs of `bytes` bytes.
+template <bool kWholeRows, class Go>
+static void logits_row(uint32_t bytes, Go go)
+{
+    using std::integral_constant;
+    const auto with = [&](auto lanes, auto per) {
+        if (bytes > (uint32_t)(lanes.value * per.value * 16)) return false;
+        go(lanes, per);
+        return true;
+    };
+    const integral_constant<int, 1> one;
+    const integral_constant<int, 2> two;
+    const integral_constant<int, 4> four;
+    const integral_constant<int, 8> eight;
+    const integral_constant<int, 16> sixteen;
+    const integral_constant<int, 256> group;
+    const bool done = with(integral_constant<int, 8>(), one) || with(integral_constant<int, 32>(), one) || with(integral_constant<int, 64>(), one) ||
+                      with(integral_constant<int, 64>(), two) || with(group, one) || with(group, two) || with(group, four) || with(group, eight) ||
+                      with(group, sixteen);
+    if constexpr (kWholeRows)
+        if (!done) (void)(with(integral_constant<int, 1024>(), eight) || with(integral_constant<int, 1024>(), sixteen));
+}
+
+// Workgroups for `items` rows or runs of which each takes `rows` at a time: those that go from one to the next with the
+// next one on its way are launched as often as they fit, eight wavefronts a SIMD, the others once for each.
+static uint32_t logits_blocks(uint64_t items, uint32_t rows, uint32_t threads, bool ahead)
+{
+    const uint64_t all = (items + rows - 1) / rows;
+    return (uint32_t)std::min<uint64_t>(all, ahead ? compute_units() * (2048u / threads) : (1u << 21));
+}
+
+template <class T, bool kTrain>
+static void launch_logits(const LogitsArgs &a, hipStream_t stream)
+{
+    if (a.num_sym < 16 / sizeof(T)) {
+        k_logits_short<T, kTrain, false><<<(uint32_t)std::min<uint64_t>((a.rows + 255ull) / 256, 1u << 20), 256, 0, stream>>>(a);
+        return;
+    }
+    logits_row<kTrain>(a.span * (uint32_t)sizeof(T), [&](auto lanes, auto per) {
+        using Row = LogitsRow<T, decltype(lanes)::value, decltype(per)::value>;
+        const uint32_t blocks = logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, Row::kAhead);
+        k_logits<T, decltype(lanes)::value, decltype(per)::value, kTrain><<<blocks, Row::kThreads, 0, stream>>>(a);
+    });
+}
+
+// The law of each row; the runs of split rows are put together by a second kernel.
+template <class T>
+static void launch_law(LogitsArgs a, uint32_t type, void *workspace, hipStream_t stream)
+{
+    const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kLongestRun, kShortestRun);
+    a.splits = p.splits, a.span = p.span;
+    a.part = (float4 *)workspace;
+    a.part_top = (uint64_t *)(a.part + (size_t)a.rows * a.splits);
+    launch_logits<T, false>(a, stream);
+    if (a.splits > 1) k_logits_join<<<std::min(a.rows, 1u << 20), 256, 0, stream>>>(a, type);
+}
+
+template <class T>
+static void launch_grad(LogitsArgs a, hipStream_t stream)
+{
+    if (a.num_sym < 16 / sizeof(T)) {
+        k_logits_short<T, false, true><<<(uint32_t)std::min<uint64_t>((a.rows + 255ull) / 256, 1u << 20), 256, 0, stream>>>(a);
+        return;
+    }
+    constexpr uint32_t kRun = 16 << 10;
+    const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kRun, kShortestRun);
+    a.splits = p.splits, a.span = p.span;
+    using std::integral_constant;
+    const auto with = [&](auto lanes, auto per) {
+        using Row = LogitsRow<T, decltype(lanes)::value, decltype(per)::value>;
+        if (a.span > Row::kValues) return false;
+        k_logits_grad<T, decltype(lanes)::value, decltype(per)::value>
+            <<<logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, false), Row::kThreads, 0, stream>>>(a);
+        return true;
+    };
+    (void)(with(integral_constant<int, 8>(), integral_constant<int, 1>()) || with(integral_constant<int, 32>(), integral_constant<int, 1>()) ||
+           with(integral_constant<int, 64>(), integral_constant<int, 1>()) || with(integral_constant<int, 256>(), integral_constant<int, 1>()) ||
+           with(integral_constant<int, 256>(), integral_constant<int, 2>()) || with(integral_constant<int, 256>(), integral_constant<int, 4>()));
+}
 
 template <class Launch>
 static void by_value_type(uint32_t type, Launch launch)
@@ -201,9 +728,8 @@ int pilc_logprobs(const pilc_logits_shape *shape, const void *logits_dev, const 
     a.x = logits_dev, a.target = target_dev, a.logp = logp_dev, a.entropy = entropy_dev, a.lse = lse_dev, a.top_sym = top_sym_dev;
     a.top_logp = top_logp_dev, a.stride = shape->stride, a.rows = shape->rows, a.num_sym = shape->num_sym, a.top = shape->top;
     a.target_type = shape->target_type;
-    return by_type(shape->dtype, [&](auto *t) {
-        k_logprobs<std::remove_pointer_t<decltype(t)>, false><<<row_blocks(a.rows), kLogitsThreads, 0, (hipStream_t)hip_stream>>>(a);
-    });
+    return by_type(shape->dtype,
+                   [&](auto *t) { launch_law<std::remove_pointer_t<decltype(t)>>(a, shape->dtype, workspace_dev, (hipStream_t)hip_stream); });
 }
 
 int pilc_logprobs_grad(const pilc_logits_shape *shape, const void *logits_dev, const void *target_dev, const float *lse_dev,
@@ -220,9 +746,7 @@ int pilc_logprobs_grad(const pilc_logits_shape *shape, const void *logits_dev, c
     a.x = logits_dev, a.target = target_dev, a.lse_in = lse_dev, a.entropy_in = entropy_dev, a.up_logp = up_logp_dev;
     a.up_entropy = up_entropy_dev, a.grad = grad_dev, a.grad_stride = grad_stride, a.stride = shape->stride, a.rows = shape->rows;
     a.num_sym = shape->num_sym, a.target_type = shape->target_type;
-    return by_type(shape->dtype, [&](auto *t) {
-        k_logprobs_grad<std::remove_pointer_t<decltype(t)>><<<row_blocks(a.rows), kLogitsThreads, 0, (hipStream_t)hip_stream>>>(a);
-    });
+    return by_type(shape->dtype, [&](auto *t) { launch_grad<std::remove_pointer_t<decltype(t)>>(a, (hipStream_t)hip_stream); });
 }
 
 int pilc_logprobs_train(const pilc_logits_shape *shape, const void *logits_dev, const void *target_dev, const float *up_logp_dev,
@@ -241,8 +765,25 @@ int pilc_logprobs_train(const pilc_logits_shape *shape, const void *logits_dev, 
     a.x = logits_dev, a.target = target_dev, a.up_logp = up_logp_dev, a.up_entropy = up_entropy_dev, a.logp = logp_dev;
     a.entropy = entropy_dev, a.lse = lse_dev, a.grad = grad_dev, a.grad_stride = grad_stride, a.stride = shape->stride;
     a.rows = shape->rows, a.num_sym = shape->num_sym, a.target_type = shape->target_type;
+    const hipStream_t stream = (hipStream_t)hip_stream;
     return by_type(shape->dtype, [&](auto *t) {
-        k_logprobs<std::remove_pointer_t<decltype(t)>, true><<<row_blocks(a.rows), kLogitsThreads, 0, (hipStream_t)hip_stream>>>(a);
+        using T = std::remove_pointer_t<decltype(t)>;
+        if (train_by_row(a.rows, a.num_sym, sizeof(T))) {
+            a.splits = 1, a.span = a.num_sym;
+            launch_logits<T, true>(a, stream);
+            return;
+        }
+        // too few rows to keep the GPU busy one a workgroup, or too long ones: the law first, then the gradient by it
+        LogitsArgs g = a;
+        if (!a.lse || !a.entropy) {  // kept behind the runs' parts where the caller does not want them
+            const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kLongestRun, kShortestRun);
+            float *kept = (float *)((float4 *)workspace_dev + (size_t)a.rows * p.splits);
+            if (!a.lse) a.lse = kept;
+            if (!a.entropy) a.entropy = kept + a.rows;
+        }
+        launch_law<T>(a, shape->dtype, workspace_dev, stream);
+        g.lse_in = a.lse, g.entropy_in = a.entropy;
+        launch_grad<T>(g, stream);
     });
 }
 
