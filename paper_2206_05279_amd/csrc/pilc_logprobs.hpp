@@ -106,8 +106,10 @@ struct LogitsRow {
     static constexpr int kThreads = kLanes > 256 ? kLanes : 256;
     static constexpr int kRows = kThreads / kLanes;  // that a workgroup has in hand
     static constexpr int kWithin = kLanes < 64 ? kLanes : 64, kWaves = kLanes > 64 ? kLanes / 64 : 1;
-    static constexpr bool kAhead = kPer <= 2;  // the next run is asked for early; larger ones have the other workgroups beside them
+    static constexpr bool kAhead = kPer <= 4;  // the next run is asked for early; larger ones have the other workgroups beside them
     static constexpr uint32_t kValues = kLanes * kPer * kVec;
+    // Wavefronts a SIMD that registers are kept down to where the next run is asked for early: so many are launched.
+    static constexpr int waves(bool train) { return kAhead ? (train ? 6 : 5) : kThreads / 256; }
 
     uint32_t lane, row_in_block;
 
@@ -123,37 +125,61 @@ struct LogitsRow {
 #pragma unroll
         for (int q = 0; q < kPer; ++q) x[q] = Raw<T>::load(p + column(q, begin, end));
     }
+    // Packs that are gone through, for all lanes the same: those with values of the row in them, up to a whole group of
+    // four.  The others are loaded, with the row's last values, and left alone.
+    static constexpr int kGroup = kPer < 4 ? kPer : 4;
+    __device__ int used(uint32_t begin, uint32_t end) const
+    {
+        return (int)((end - begin + kLanes * kVec * kGroup - 1) / (kLanes * kVec * kGroup)) * kGroup;
+    }
+    template <class F>
+    __device__ static void for_used(int used, F f)
+    {
+#pragma unroll
+        for (int g = 0; g < kPer; g += kGroup)
+            if (g < used)
+#pragma unroll
+                for (int q = g; q < g + kGroup; ++q) f(q);
+    }
     __device__ void rule_out(uint32_t begin, uint32_t end, Raw<T> (&x)[kPer]) const
     {
-        if (end - begin < kValues)
+        const int whole = (int)((end - begin) / (kLanes * kVec));
+        if (whole < kPer)
 #pragma unroll
-            for (int q = 0; q < kPer; ++q) x[q].rule_out(twice(q, begin, end));
+            for (int q = 0; q < kPer; ++q)
+                if (q >= whole) x[q].rule_out(twice(q, begin, end));
     }
     __device__ static void forget(Raw<T> (&x)[kPer])
     {
 #pragma unroll
         for (int q = 0; q < kPer; ++q) x[q].forget();
     }
-    __device__ float largest(const Raw<T> (&x)[kPer]) const
+    // of each pack, and of all
+    __device__ float largest(const Raw<T> (&x)[kPer], int used, float (&of)[kPer]) const
     {
-        float m[2] = {-kInf, -kInf};
+        float m = -kInf;
+        for_used(used, [&](int q) {
+            float side[2] = {x[q][0], x[q][1]};
 #pragma unroll
-        for (int q = 0; q < kPer; ++q)
-#pragma unroll
-            for (int k = 0; k < kVec; k += 2) m[0] = fmaxf(m[0], x[q][k]), m[1] = fmaxf(m[1], x[q][k + 1]);
-        return fmaxf(m[0], m[1]);
+            for (int k = 2; k < kVec; k += 2) side[0] = fmaxf(side[0], x[q][k]), side[1] = fmaxf(side[1], x[q][k + 1]);
+            of[q] = fmaxf(side[0], side[1]);
+            m = fmaxf(m, of[q]);
+        });
+        return m;
     }
-    // f(order, symbol) for each of the lane's values
+    // f(order, symbol) for each of the lane's values from `least` on; `of`: the packs' largest
     template <class F>
-    __device__ void each(Raw<T> (&x)[kPer], uint32_t begin, uint32_t end, F f) const
+    __device__ void each(Raw<T> (&x)[kPer], const float (&of)[kPer], uint32_t begin, uint32_t end, int used, float least, F f) const
     {
+        for_used(used, [&](int q) {
+            if (of[q] >= least) {
+                x[q].forget();
+                const uint32_t column_q = column(q, begin, end);
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) {
-            x[q].forget();
-            const uint32_t column_q = column(q, begin, end);
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) f(order_of(x[q][k]), column_q + k);
-        }
+                for (int k = 0; k < kVec; ++k)
+                    if (x[q][k] >= least) f(order_of(x[q][k]), column_q + k);
+            }
+        });
     }
     // The same from memory, in little code
     template <class F>
@@ -165,19 +191,19 @@ struct LogitsRow {
             for (uint32_t j = place(q, begin); j < min(place(q, begin) + kVec, end); ++j) f(order_of(widen(p[j])), j);
     }
     // The row's tally in all its lanes; `room` holds 2 * kWaves, its halves are used in turn.
-    __device__ Tally tally(const Raw<T> (&x)[kPer], float own, Tally *room, int half) const
+    __device__ Tally tally(const Raw<T> (&x)[kPer], int used, float own, Tally *room, int half) const
     {
         const float max = lanes_reduce<kWithin>(own, MaxFloat());
         const Scale scale(max);
         float total[2] = {0.0f, 0.0f}, inside[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int q = 0; q < kPer; ++q)
+        for_used(used, [&](int q) {
 #pragma unroll
             for (int k = 0; k < kVec; ++k) {
                 const float z = scale.power(x[q][k]), e = exp2_fast(z);
                 total[k & 1] += e;
                 inside[k & 1] = __builtin_fmaf(e, fmaxf(z, kLeast), inside[k & 1]);
             }
+        });
         Tally t = {max, lanes_reduce<kWithin>(total[0] + total[1], Sum()), lanes_reduce<kWithin>(inside[0] + inside[1], Sum())};
         if constexpr (kWaves > 1) {
             room += half * kWaves;
@@ -194,32 +220,47 @@ struct LogitsRow {
     }
 };
 
-// The `top` best of what the threads of a workgroup hold.  `each` calls its argument with the order (see order_of) and
-// symbol of every value of the calling thread, `again` does the same for the rare way below, `best` is the highest order among them; `put` is called, once for each
-// place in 0 .. top-1 and by some thread, with the place and the key that belongs there, or 0.
+// The `top` best of what kThreads threads hold: a workgroup, or with 64 a wavefront by itself.  `each` calls its second
+// argument with the order (see order_of) and symbol of the calling thread's values from its first on, `again` its argument
+// with all of them for the rare way below, `best` is the highest order among them; `put` is called, once for each place in
+// 0 .. top-1 and by some thread, with the place and the key that belongs there, or 0.
 //
 // The top-th best of the threads' best values has `top` values at least that are as good, and few more in what a model
-// answers with; those are put side by side, and each one's place is the number of better ones.  Rows with many equal
-// values may have too many of them: then the best that is worse than the last is looked for `top` times.
-constexpr int kMostPicked = 256;
+// answers with; those are put side by side, and each one's place is the number of better ones.  The more threads stand
+// for a row the fewer there are to look at: four wavefronts that each pick by themselves before they join take longer
+// (16384 x 32768 bf16, 20 alternatives: 417 against 294 us).  Rows with many equal values may have too many of them:
+// then the best that is worse than the last is looked for `top` times.
 template <int kThreads>
 struct PickRoom {
+    static constexpr uint32_t kMost = kThreads < 256 ? 128 : 256;
     uint32_t best[kThreads];
-    uint64_t picked[kMostPicked], rounds[kThreads / 64];
+    uint64_t picked[kMost], rounds[kThreads / 64];
     uint32_t count;
 };
+template <int kThreads>
+__device__ __forceinline__ void meet()
+{
+    if constexpr (kThreads > 64) {
+        __syncthreads();
+    } else {  // a wavefront's accesses to LDS are done in order: the compiler has to leave them in it
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
 template <int kThreads, int kBits, class Each, class Again, class Put>
 __device__ void pick_top(uint32_t top, uint32_t best, Each each, Again again, Put put, PickRoom<kThreads> &room)
 {
     constexpr int kEach = kThreads / 64;
-    __syncthreads();  // `room` may be in use from a row before
-    room.best[threadIdx.x] = best;
-    if (threadIdx.x == 0) room.count = 0;
-    __syncthreads();
+    const uint32_t thread = threadIdx.x & (kThreads - 1);
+    meet<kThreads>();  // `room` may be in use from a row before
+    if (kEach > 1) room.best[thread] = best;
+    if (thread == 0) room.count = 0;
+    meet<kThreads>();
     // the highest order that `top` threads' best reach, bit by bit from the top; kBits is what the type's values differ in
-    uint32_t b[kEach], line = 0;
+    uint32_t b[kEach] = {best}, line = 0;
+    if (kEach > 1)
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) b[i] = room.best[i * 64 + (threadIdx.x & 63)];
+        for (int i = 0; i < kEach; ++i) b[i] = room.best[i * 64 + (threadIdx.x & 63)];
     for (int bit = 31; bit >= 32 - kBits; --bit) {
         const uint32_t next = line | 1u << bit;
         uint32_t reach = 0;
@@ -229,21 +270,20 @@ __device__ void pick_top(uint32_t top, uint32_t best, Each each, Again again, Pu
     }
     line = max(line, kOrderNone + 1);  // -inf is no alternative
     if (best >= line)
-        each([&](uint32_t order, uint32_t sym) {
-            if (order < line) return;
+        each(line, [&](uint32_t order, uint32_t sym) {
             const uint32_t at = atomicAdd(&room.count, 1u);
-            if (at < kMostPicked) room.picked[at] = (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
+            if (at < room.kMost) room.picked[at] = (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
         });
-    __syncthreads();
+    meet<kThreads>();
     const uint32_t count = room.count;
-    if (count <= (uint32_t)kMostPicked) {
-        for (uint32_t i = threadIdx.x; i < count; i += kThreads) {
+    if (count <= room.kMost) {
+        for (uint32_t i = thread; i < count; i += kThreads) {
             const uint64_t key = room.picked[i];
             uint32_t better = 0;
             for (uint32_t j = 0; j < count; ++j) better += room.picked[j] > key;
             if (better < top) put(better, key);
         }
-        for (uint32_t i = count + threadIdx.x; i < top; i += kThreads) put(i, (uint64_t)0);
+        for (uint32_t i = count + thread; i < top; i += kThreads) put(i, (uint64_t)0);
         return;
     }
     uint64_t below = ~0ull;
@@ -255,7 +295,7 @@ __device__ void pick_top(uint32_t top, uint32_t best, Each each, Again again, Pu
                 if (order >= line && key < below && key > next) next = key;
             });
         below = block_reduce<kThreads / 64>(next, Max(), room.rounds);
-        if (threadIdx.x == 0) put(i, below);
+        if (thread == 0) put(i, below);
     }
 }
 template <class T>
@@ -300,11 +340,14 @@ __device__ __forceinline__ void put_gradient(const Raw<T> &x, T *grad, uint32_t 
 // Rows, or runs of rows, one after another; a row that is one run is finished here.  kTrain: whole rows, and their
 // gradient from the same registers.
 template <class T, int kLanes, int kPer, bool kTrain>
-__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logits(LogitsArgs a)
+__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::waves(kTrain))) void k_logits(LogitsArgs a)
 {
     using Row = LogitsRow<T, kLanes, kPer>;
     constexpr int kVec = Row::kVec;
     __shared__ Tally room[2 * Row::kWaves];
+    constexpr bool kPicks = !kTrain && kLanes >= 64;
+    constexpr int kPickers = kPicks ? kLanes : 64;
+    __shared__ PickRoom<kPickers> picked[kPicks ? Row::kRows : 1];
     const Row r;
     const uint64_t items = (uint64_t)a.rows * a.splits, step = (uint64_t)gridDim.x * Row::kRows;
     uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block;
@@ -335,22 +378,20 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logi
         const uint32_t end = min(begin + a.span, a.num_sym);
         const int64_t t = given.t;
         r.rule_out(begin, end, x);
-        const float own = r.largest(x);
+        const int used = r.used(begin, end);
+        float of[kPer];
+        const float own = r.largest(x, used, of);
         r.forget(x);
-        const Tally tally = r.tally(x, own, room, half);
+        const Tally tally = r.tally(x, used, own, room, half);
         r.forget(x);
         half ^= 1;
+        const auto each = [&](uint32_t line, auto f) { r.each(x, of, begin, end, used, value_of((uint64_t)line << 32), f); };
+        const auto again = [&](auto f) { r.again((const T *)a.x + row * a.stride, begin, end, f); };
+        const auto pick = [&](auto put) { pick_top<kPickers, kOrderBits<T>>(a.top, order_of(own), each, again, put, picked[r.row_in_block]); };
         if (!kTrain && a.splits > 1) {
             if (r.lane == 0) a.part[item] = make_float4(tally.max, tally.total, tally.inside, 0.0f);
-            if constexpr (kLanes == 256)
-                if (a.top) {
-                    __shared__ PickRoom<256> pick;
-                    pick_top<256, kOrderBits<T>>(
-                        a.top, order_of(own),
-                        [&](auto f) { r.each(x, begin, end, f); },
-                        [&](auto f) { r.again((const T *)a.x + row * a.stride, begin, end, f); },
-                        [&](uint32_t place, uint64_t key) { a.part_top[item * a.top + place] = key; }, pick);
-                }
+            if constexpr (kLanes >= 64 && !kTrain)  // no run of several is shorter
+                if (a.top) pick([&](uint32_t place, uint64_t key) { a.part_top[item * a.top + place] = key; });
         } else {
             const Law law(tally);
             if (r.lane == 0) {
@@ -378,22 +419,18 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logi
                 const bool zeros = (up == 0.0f && up_entropy == 0.0f) || law.max == -kInf;
                 if (t >= (int64_t)a.num_sym || !(law.max == law.max)) from = __builtin_nanf("");
                 T *grad = (T *)a.grad + row * a.grad_stride;
-#pragma unroll
-                for (int q = 0; q < kPer; ++q)
+                r.for_used(used, [&](int q) {
                     put_gradient(x[q], grad, r.column(q, begin, end), r.twice(q, begin, end), scale, from, slope, in, t, up, zeros);
+                });
             } else if (a.top) {
-                const auto each = [&](auto f) { r.each(x, begin, end, f); };
-                if constexpr (kLanes == 256) {
-                    __shared__ PickRoom<256> pick;
-                    pick_top<256, kOrderBits<T>>(
-                        a.top, order_of(own), each, [&](auto f) { r.again((const T *)a.x + row * a.stride, begin, end, f); },
-                        [&](uint32_t place, uint64_t key) { put_alternative(a, law, row, place, key); }, pick);
+                if constexpr (kLanes >= 64) {
+                    pick([&](uint32_t place, uint64_t key) { put_alternative(a, law, row, place, key); });
                 } else {
                     // few values a lane: the best that is worse than the last, `top` times
                     uint64_t below = ~0ull;
                     for (uint32_t i = 0; i < a.top; ++i) {
                         uint64_t best = 0;
-                        each([&](uint32_t order, uint32_t sym) {
+                        r.each(x, of, begin, end, used, -kInf, [&](uint32_t order, uint32_t sym) {
                             const uint64_t key = (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
                             if (order > kOrderNone && key < below && key > best) best = key;
                         });
@@ -413,32 +450,37 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logi
     }
 }
 
-// The runs of a row put together, a workgroup a row.
+// The runs of a row put together by kThreads threads: a workgroup, or a wavefront.
+template <int kThreads>
 __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type)
 {
+    constexpr uint32_t kRows = 256 / kThreads;
+    __shared__ PickRoom<kThreads> picked[kRows];
     __shared__ Tally room[4];
-    __shared__ PickRoom<256> pick;
-    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const uint32_t thread = threadIdx.x & (kThreads - 1), which = threadIdx.x / kThreads;
+    for (uint64_t row = (uint64_t)blockIdx.x * kRows + which; row < a.rows; row += (uint64_t)gridDim.x * kRows) {
         Tally t = {-kInf, 0.0f, 0.0f};
-        for (uint32_t s = threadIdx.x; s < a.splits; s += 256) {
-            const float4 p = a.part[(uint64_t)row * a.splits + s];
+        for (uint32_t s = thread; s < a.splits; s += kThreads) {
+            const float4 p = a.part[row * a.splits + s];
             t = both(t, {p.x, p.y, p.z});
         }
         const auto over = [&](int lanes) {
             for (int d = 1; d < lanes; d *= 2) t = both(t, {__shfl_xor(t.max, d, 64), __shfl_xor(t.total, d, 64), __shfl_xor(t.inside, d, 64)});
         };
         over(64);
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = t;
-        __syncthreads();
-        t = room[threadIdx.x & 3];
-        over(4);
+        if (kThreads > 64) {
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = t;
+            __syncthreads();
+            t = room[threadIdx.x & 3];
+            over(4);
+        }
         const Law law(t);
-        if (threadIdx.x == 0) {
+        if (thread == 0) {
             if (a.entropy) a.entropy[row] = law.entropy;
             if (a.lse) a.lse[row] = law.lse();
             if (a.logp) {
-                const int64_t target = target_of(a, row);
+                const int64_t target = target_of(a, (uint32_t)row);
                 float at = 0.0f;
                 if (target >= 0 && target < (int64_t)a.num_sym) {
                     const uint64_t i = row * a.stride + (uint64_t)target;
@@ -448,16 +490,20 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type
             }
         }
         if (a.top) {
-            const uint64_t *keys = a.part_top + (uint64_t)row * a.splits * a.top;
+            const uint64_t *keys = a.part_top + row * a.splits * a.top;
             const uint32_t count = a.splits * a.top;
             uint32_t best = 0;
-            for (uint32_t i = threadIdx.x; i < count; i += 256) best = max(best, (uint32_t)(keys[i] >> 32));
-            const auto each = [&](auto f) {
-                for (uint32_t i = threadIdx.x; i < count; i += 256) f((uint32_t)(keys[i] >> 32), 0xFFFFFFFFu - (uint32_t)keys[i]);
+            for (uint32_t i = thread; i < count; i += kThreads) best = max(best, (uint32_t)(keys[i] >> 32));
+            const auto again = [&](auto f) {
+                for (uint32_t i = thread; i < count; i += kThreads) f((uint32_t)(keys[i] >> 32), 0xFFFFFFFFu - (uint32_t)keys[i]);
             };
-            pick_top<256, 32>(
-                a.top, best, each, each,
-                [&](uint32_t place, uint64_t key) { put_alternative(a, law, row, place, key); }, pick);
+            const auto each = [&](uint32_t line, auto f) {
+                again([&](uint32_t order, uint32_t sym) {
+                    if (order >= line) f(order, sym);
+                });
+            };
+            pick_top<kThreads, 32>(
+                a.top, best, each, again, [&](uint32_t place, uint64_t key) { put_alternative(a, law, (uint32_t)row, place, key); }, picked[which]);
         }
     }
 }
@@ -580,7 +626,8 @@ static LogitsPlan logits_plan(uint32_t rows, uint32_t num_sym, uint32_t value, u
 {
     const uint32_t vec = 16 / value, needed = div_up(num_sym, longest / value), most = div_up(num_sym, shortest / value);
     const uint32_t wanted = div_up(2 * compute_units(), std::max(rows, 1u)), splits = std::max(needed, std::min(wanted, most));
-    const uint32_t span = div_up(div_up(num_sym, splits), vec) * vec;
+    // many rows: full runs, so that only the last one has packs without values
+    const uint32_t span = splits == needed ? longest / value : div_up(div_up(num_sym, splits), vec) * vec;
     return {div_up(num_sym, span), span};
 }
 // Whether pilc_logprobs_train keeps whole rows in registers: up to 256 KB, those of a workgroup of 1024.
@@ -619,19 +666,19 @@ static void logits_row(uint32_t bytes, Go go)
     const integral_constant<int, 8> eight;
     const integral_constant<int, 16> sixteen;
     const integral_constant<int, 256> group;
-    const bool done = with(integral_constant<int, 8>(), one) || with(integral_constant<int, 32>(), one) || with(integral_constant<int, 64>(), one) ||
-                      with(integral_constant<int, 64>(), two) || with(group, one) || with(group, two) || with(group, four) || with(group, eight) ||
-                      with(group, sixteen);
+    const bool done = with(integral_constant<int, 8>(), one) || with(integral_constant<int, 8>(), four) || with(integral_constant<int, 16>(), four) ||
+                      with(integral_constant<int, 32>(), four) || with(integral_constant<int, 64>(), four) || with(group, two) || with(group, four) ||
+                      with(group, eight) || with(group, sixteen);
     if constexpr (kWholeRows)
         if (!done) (void)(with(integral_constant<int, 1024>(), eight) || with(integral_constant<int, 1024>(), sixteen));
 }
 
-// Workgroups for `items` rows or runs of which each takes `rows` at a time: those that go from one to the next with the
-// next one on its way are launched as often as they fit, eight wavefronts a SIMD, the others once for each.
-static uint32_t logits_blocks(uint64_t items, uint32_t rows, uint32_t threads, bool ahead)
+// Workgroups for `items` rows or runs of which each takes `rows` at a time: one for each, or with `waves` as many as that
+// many wavefronts a SIMD are, which go from one to the next.
+static uint32_t logits_blocks(uint64_t items, uint32_t rows, uint32_t threads, uint32_t waves)
 {
     const uint64_t all = (items + rows - 1) / rows;
-    return (uint32_t)std::min<uint64_t>(all, ahead ? compute_units() * (2048u / threads) : (1u << 21));
+    return (uint32_t)std::min<uint64_t>(all, waves ? compute_units() * (waves * 256 / threads) : (1u << 21));
 }
 
 template <class T, bool kTrain>
@@ -643,7 +690,7 @@ static void launch_logits(const LogitsArgs &a, hipStream_t stream)
     }
     logits_row<kTrain>(a.span * (uint32_t)sizeof(T), [&](auto lanes, auto per) {
         using Row = LogitsRow<T, decltype(lanes)::value, decltype(per)::value>;
-        const uint32_t blocks = logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, Row::kAhead);
+        const uint32_t blocks = logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, Row::kAhead ? Row::waves(kTrain) : 0);
         k_logits<T, decltype(lanes)::value, decltype(per)::value, kTrain><<<blocks, Row::kThreads, 0, stream>>>(a);
     });
 }
@@ -653,11 +700,15 @@ template <class T>
 static void launch_law(LogitsArgs a, uint32_t type, void *workspace, hipStream_t stream)
 {
     const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kLongestRun, kShortestRun);
-    a.splits = p.splits, a.span = p.span;
+    a.splits = p.splits, a.span = std::min(p.span, a.num_sym);
     a.part = (float4 *)workspace;
     a.part_top = (uint64_t *)(a.part + (size_t)a.rows * a.splits);
     launch_logits<T, false>(a, stream);
-    if (a.splits > 1) k_logits_join<<<std::min(a.rows, 1u << 20), 256, 0, stream>>>(a, type);
+    if (a.splits == 1) return;
+    if (a.splits > 16)  // few rows: a workgroup each
+        k_logits_join<256><<<std::min(a.rows, 1u << 20), 256, 0, stream>>>(a, type);
+    else
+        k_logits_join<64><<<std::min(div_up(a.rows, 4), 1u << 20), 256, 0, stream>>>(a, type);
 }
 
 template <class T>
@@ -669,13 +720,13 @@ static void launch_grad(LogitsArgs a, hipStream_t stream)
     }
     constexpr uint32_t kRun = 16 << 10;
     const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kRun, kShortestRun);
-    a.splits = p.splits, a.span = p.span;
+    a.splits = p.splits, a.span = std::min(p.span, a.num_sym);
     using std::integral_constant;
     const auto with = [&](auto lanes, auto per) {
         using Row = LogitsRow<T, decltype(lanes)::value, decltype(per)::value>;
         if (a.span > Row::kValues) return false;
         k_logits_grad<T, decltype(lanes)::value, decltype(per)::value>
-            <<<logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, false), Row::kThreads, 0, stream>>>(a);
+            <<<logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, 0), Row::kThreads, 0, stream>>>(a);
         return true;
     };
     (void)(with(integral_constant<int, 8>(), integral_constant<int, 1>()) || with(integral_constant<int, 32>(), integral_constant<int, 1>()) ||
