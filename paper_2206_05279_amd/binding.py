@@ -444,41 +444,61 @@ _VALUES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _SYMBOLS = {torch.uint8: 0, torch.int32: 1, torch.int64: 2}
 
 
-def _on_device(t: torch.Tensor, what: str) -> None:
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise TypeError("%s must be on the current device" % what)
+def _bad(what: str, wanted: str):
+    raise TypeError("%s must be %s on the current device" % (what, wanted))
 
 
-def _vector(t: Optional[torch.Tensor], dtype, count: int, what: str) -> Optional[int]:
+def _device_of(t: torch.Tensor, what: str) -> int:
+    """The number of the current device, which has to hold t."""
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
+        _bad(what, "a tensor")
+    return device
+
+
+def _vector(t: Optional[torch.Tensor], dtype, count: int, device: int, what: str) -> Optional[int]:
     """The address of `count` dense values on the device, or None for None."""
     if t is None:
         return None
-    _on_device(t, what)
-    if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
-        raise TypeError("%s must be %d contiguous values of %s" % (what, count, dtype))
+    if t.dtype is not dtype or t.get_device() != device or t.numel() != count or not t.is_contiguous():
+        _bad(what, "%d contiguous values of %s" % (count, dtype))
     return t.data_ptr()
 
 
-def _rows(t: torch.Tensor, dtype, shape, what: str) -> Tuple[int, int]:
-    """(address, elements from row to row) of a matrix whose rows are dense."""
-    _on_device(t, what)
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise TypeError("%s must be %s rows of %s with dense rows" % (what, tuple(shape), dtype))
-    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if stride < t.shape[1]:
-        raise TypeError("%s: rows overlap" % what)
-    return t.data_ptr(), stride
+def _rows(t: torch.Tensor, dtype, rows: int, width: int, device: int, what: str) -> Tuple[int, int]:
+    """(address, elements from row to row) of a matrix whose rows are dense and do not overlap."""
+    if t.dtype is not dtype or t.get_device() != device or t.dim() != 2 or t.size(0) != rows or t.size(1) != width:
+        _bad(what, "%d x %d values of %s" % (rows, width, dtype))
+    across, along = t.stride()
+    if rows <= 1:
+        across = width
+    if (along != 1 and width > 1) or across < width:
+        _bad(what, "a matrix with dense rows that do not overlap")
+    return t.data_ptr(), across
 
 
-def _logits(logits: torch.Tensor, targets: Optional[torch.Tensor], top: int):
-    if logits.dim() != 2 or logits.dtype not in _VALUES:
-        raise TypeError("logits must be a matrix of float32, bfloat16 or float16")
-    ptr, stride = _rows(logits, logits.dtype, logits.shape, "logits")
-    if targets is not None and targets.dtype not in _SYMBOLS:
-        raise TypeError("targets must be uint8, int32 or int64")
+def _raw_stream(stream: Optional[torch.cuda.Stream], device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
+def _logits(logits: torch.Tensor, targets: Optional[torch.Tensor], top: int, device: int):
+    kind = _VALUES.get(logits.dtype)
+    if kind is None or logits.dim() != 2:
+        _bad("logits", "a matrix of float32, bfloat16 or float16")
     rows, num_sym = logits.shape
-    shape = pilc_logits_shape(rows, num_sym, stride, _VALUES[logits.dtype], _SYMBOLS[targets.dtype] if targets is not None else 0, top)
-    return shape, ptr, _vector(targets, targets.dtype if targets is not None else None, rows, "targets")
+    ptr, stride = _rows(logits, logits.dtype, rows, num_sym, device, "logits")
+    if targets is None:
+        return pilc_logits_shape(rows, num_sym, stride, kind, 0, top), ptr, None
+    t_kind = _SYMBOLS.get(targets.dtype)
+    if t_kind is None:
+        _bad("targets", "uint8, int32 or int64")
+    return (pilc_logits_shape(rows, num_sym, stride, kind, t_kind, top), ptr,
+            _vector(targets, targets.dtype, rows, device, "targets"))
+
+
+def _workspace(workspace: torch.Tensor, device: int) -> Tuple[int, int]:
+    n = workspace.numel()
+    return _vector(workspace, torch.uint8, n, device, "workspace"), n
 
 
 def pilc_logprobs_workspace_size(rows: int, num_sym: int, top: int = 0) -> int:
@@ -491,21 +511,17 @@ def pilc_logprobs_workspace_size(rows: int, num_sym: int, top: int = 0) -> int:
     return int(n.value)
 
 
-def _workspace(workspace: torch.Tensor) -> Tuple[int, int]:
-    return _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel()
-
-
 def pilc_logprobs(logits, targets=None, logp=None, entropy=None, lse=None, top_sym=None, top_logp=None, *, workspace,
                   stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
     """ln p of the targets, entropy, ln of the sum and the most likely symbols of each row; what is None is not wanted.
     logits [rows, num_sym], its rows dense; top_sym int32 and top_logp float32 [rows, top]; the rest [rows]."""
+    dev, f32 = _device_of(logits, "logits"), torch.float32
     top = 0 if top_sym is None else top_sym.shape[-1]
-    shape, x, t = _logits(logits, targets, top)
+    shape, x, t = _logits(logits, targets, top, dev)
     rows = shape.rows
-    rc = lib().pilc_logprobs(C.byref(shape), x, t, _vector(logp, torch.float32, rows, "logp"),
-                             _vector(entropy, torch.float32, rows, "entropy"), _vector(lse, torch.float32, rows, "lse"),
-                             _vector(top_sym, torch.int32, rows * top, "top_sym"),
-                             _vector(top_logp, torch.float32, rows * top, "top_logp"), *_workspace(workspace), _stream_handle(stream))
+    rc = lib().pilc_logprobs(C.byref(shape), x, t, _vector(logp, f32, rows, dev, "logp"), _vector(entropy, f32, rows, dev, "entropy"),
+                             _vector(lse, f32, rows, dev, "lse"), _vector(top_sym, torch.int32, rows * top, dev, "top_sym"),
+                             _vector(top_logp, f32, rows * top, dev, "top_logp"), *_workspace(workspace, dev), _raw_stream(stream, dev))
     if check and rc != PILC_OK:
         raise PilcError(rc, "pilc_logprobs")
     return rc
@@ -514,12 +530,13 @@ def pilc_logprobs(logits, targets=None, logp=None, entropy=None, lse=None, top_s
 def pilc_logprobs_grad(logits, targets, lse, up_logp, grad, entropy=None, up_entropy=None,
                        stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
     """grad = gradient of sum(up_logp * logp) + sum(up_entropy * entropy) by the logits; grad may be the logits."""
-    shape, x, t = _logits(logits, targets, 0)
+    dev, f32 = _device_of(logits, "logits"), torch.float32
+    shape, x, t = _logits(logits, targets, 0, dev)
     rows = shape.rows
-    g, g_stride = _rows(grad, logits.dtype, logits.shape, "grad")
-    rc = lib().pilc_logprobs_grad(C.byref(shape), x, t, _vector(lse, torch.float32, rows, "lse"),
-                                  _vector(entropy, torch.float32, rows, "entropy"), _vector(up_logp, torch.float32, rows, "up_logp"),
-                                  _vector(up_entropy, torch.float32, rows, "up_entropy"), g, g_stride, _stream_handle(stream))
+    g, g_stride = _rows(grad, logits.dtype, rows, shape.num_sym, dev, "grad")
+    rc = lib().pilc_logprobs_grad(C.byref(shape), x, t, _vector(lse, f32, rows, dev, "lse"), _vector(entropy, f32, rows, dev, "entropy"),
+                                  _vector(up_logp, f32, rows, dev, "up_logp"), _vector(up_entropy, f32, rows, dev, "up_entropy"), g,
+                                  g_stride, _raw_stream(stream, dev))
     if check and rc != PILC_OK:
         raise PilcError(rc, "pilc_logprobs_grad")
     return rc
@@ -528,36 +545,46 @@ def pilc_logprobs_grad(logits, targets, lse, up_logp, grad, entropy=None, up_ent
 def pilc_logprobs_train(logits, targets, up_logp, logp, grad, entropy=None, lse=None, up_entropy=None, *, workspace,
                         stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
     """pilc_logprobs (without alternatives) and pilc_logprobs_grad in one call."""
-    shape, x, t = _logits(logits, targets, 0)
+    dev, f32 = _device_of(logits, "logits"), torch.float32
+    shape, x, t = _logits(logits, targets, 0, dev)
     rows = shape.rows
-    g, g_stride = _rows(grad, logits.dtype, logits.shape, "grad")
-    rc = lib().pilc_logprobs_train(C.byref(shape), x, t, _vector(up_logp, torch.float32, rows, "up_logp"),
-                                   _vector(up_entropy, torch.float32, rows, "up_entropy"), _vector(logp, torch.float32, rows, "logp"),
-                                   _vector(entropy, torch.float32, rows, "entropy"), _vector(lse, torch.float32, rows, "lse"),
-                                   g, g_stride, *_workspace(workspace), _stream_handle(stream))
+    g, g_stride = _rows(grad, logits.dtype, rows, shape.num_sym, dev, "grad")
+    rc = lib().pilc_logprobs_train(C.byref(shape), x, t, _vector(up_logp, f32, rows, dev, "up_logp"),
+                                   _vector(up_entropy, f32, rows, dev, "up_entropy"), _vector(logp, f32, rows, dev, "logp"),
+                                   _vector(entropy, f32, rows, dev, "entropy"), _vector(lse, f32, rows, dev, "lse"), g, g_stride,
+                                   *_workspace(workspace, dev), _raw_stream(stream, dev))
     if check and rc != PILC_OK:
         raise PilcError(rc, "pilc_logprobs_train")
     return rc
 
 
-def _norm_weights(x, *weights):
-    kinds = {w.dtype for w in weights if w is not None}
-    if x.dim() != 2 or x.dtype not in _VALUES or len(kinds) > 1 or not kinds <= {x.dtype, torch.float32}:
-        raise TypeError("x must be a matrix of float32, bfloat16 or float16, weight and bias of its type or float32")
-    return kinds.pop() if kinds else x.dtype
+def _norm_types(x, *weights):
+    """The type of x's values, and the one its weights share."""
+    kind = None
+    for w in weights:
+        if w is not None:
+            if kind is not None and w.dtype is not kind:
+                _bad("weights", "of one type")
+            kind = w.dtype
+    if kind is None:
+        kind = x.dtype
+    if x.dim() != 2 or x.dtype not in _VALUES or (kind is not x.dtype and kind is not torch.float32):
+        _bad("x", "a matrix of float32, bfloat16 or float16, its weights of its type or float32,")
+    return x.dtype, kind
 
 
 def pilc_norm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5,
                       stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
     """y = (x - mean) * rstd * weight + bias over each row of x [rows, width]; weight, bias None: 1 and 0."""
-    kind = _norm_weights(x, weight, bias)
+    dev, f32 = _device_of(x, "x"), torch.float32
+    own, kind = _norm_types(x, weight, bias)
     rows, width = x.shape
-    xp, xs = _rows(x, x.dtype, x.shape, "x")
-    yp, ys = _rows(y, x.dtype, x.shape, "y")
-    shape = pilc_norm_shape(rows, width, xs, ys, 0, _VALUES[x.dtype], _VALUES[kind], eps)
-    rc = lib().pilc_norm_forward(C.byref(shape), xp, _vector(weight, kind, width, "weight"), _vector(bias, kind, width, "bias"), yp,
-                                 _vector(mean, torch.float32, rows, "mean"), _vector(rstd, torch.float32, rows, "rstd"),
-                                 _stream_handle(stream))
+    xp, xs = _rows(x, own, rows, width, dev, "x")
+    yp, ys = _rows(y, own, rows, width, dev, "y")
+    shape = pilc_norm_shape(rows, width, xs, ys, 0, _VALUES[own], _VALUES[kind], eps)
+    rc = lib().pilc_norm_forward(C.byref(shape), xp, _vector(weight, kind, width, dev, "weight"), _vector(bias, kind, width, dev, "bias"),
+                                 yp, _vector(mean, f32, rows, dev, "mean"), _vector(rstd, f32, rows, dev, "rstd"),
+                                 _raw_stream(stream, dev))
     if check and rc != PILC_OK:
         raise PilcError(rc, "pilc_norm_forward")
     return rc
@@ -576,16 +603,17 @@ def pilc_norm_workspace_size(rows: int, width: int) -> int:
 def pilc_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, *, workspace,
                        stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
     """Gradients of pilc_norm_forward by x, weight and bias; what is None is not wanted.  dx may be dy."""
-    kind = _norm_weights(x, weight, dweight, dbias)
+    dev, f32 = _device_of(x, "x"), torch.float32
+    own, kind = _norm_types(x, weight, dweight, dbias)
     rows, width = x.shape
-    xp, xs = _rows(x, x.dtype, x.shape, "x")
-    dyp, dys = _rows(dy, x.dtype, x.shape, "dy")
-    dxp, dxs = _rows(dx, x.dtype, x.shape, "dx") if dx is not None else (None, width)
-    shape = pilc_norm_shape(rows, width, xs, dys, dxs, _VALUES[x.dtype], _VALUES[kind], 0.0)
-    rc = lib().pilc_norm_backward(C.byref(shape), dyp, xp, _vector(weight, kind, width, "weight"),
-                                  _vector(mean, torch.float32, rows, "mean"), _vector(rstd, torch.float32, rows, "rstd"), dxp,
-                                  _vector(dweight, kind, width, "dweight"), _vector(dbias, kind, width, "dbias"),
-                                  *_workspace(workspace), _stream_handle(stream))
+    xp, xs = _rows(x, own, rows, width, dev, "x")
+    dyp, dys = _rows(dy, own, rows, width, dev, "dy")
+    dxp, dxs = _rows(dx, own, rows, width, dev, "dx") if dx is not None else (None, width)
+    shape = pilc_norm_shape(rows, width, xs, dys, dxs, _VALUES[own], _VALUES[kind], 0.0)
+    rc = lib().pilc_norm_backward(C.byref(shape), dyp, xp, _vector(weight, kind, width, dev, "weight"),
+                                  _vector(mean, f32, rows, dev, "mean"), _vector(rstd, f32, rows, dev, "rstd"), dxp,
+                                  _vector(dweight, kind, width, dev, "dweight"), _vector(dbias, kind, width, dev, "dbias"),
+                                  *_workspace(workspace, dev), _raw_stream(stream, dev))
     if check and rc != PILC_OK:
         raise PilcError(rc, "pilc_norm_backward")
     return rc
@@ -615,26 +643,26 @@ def make_adamw_tensors(params, grads, ms, vs, m_scales=None, v_scales=None, lr_m
     mults = [1.0] * n if lr_mults is None else [float(m) for m in lr_mults]
     if len(decays) != n or len(mults) != n:
         raise TypeError("one decay and one lr_mult a tensor")
-    records = (pilc_adamw_tensor * n)()
+    records, dev = (pilc_adamw_tensor * n)(), _device_of(params[0], "params")
     for i in range(n):
         count = params[i].numel()
         scales = [None, None] if m_scales is None else [
-            _vector(s[i], torch.uint8, -(-count // 256), "scales") for s in (m_scales, v_scales)]
-        records[i] = pilc_adamw_tensor(_vector(params[i], p_type, count, "params"), _vector(grads[i], g_type, count, "grads"),
-                                       _vector(ms[i], state, count, "ms"), _vector(vs[i], state, count, "vs"), *scales, count,
+            _vector(s[i], torch.uint8, -(-count // 256), dev, "scales") for s in (m_scales, v_scales)]
+        records[i] = pilc_adamw_tensor(_vector(params[i], p_type, count, dev, "params"), _vector(grads[i], g_type, count, dev, "grads"),
+                                       _vector(ms[i], state, count, dev, "ms"), _vector(vs[i], state, count, dev, "vs"), *scales, count,
                                        mults[i], decays[i])
-    return AdamwTensors(records, _VALUES[p_type], _VALUES[g_type], 32 if m_scales is None else 8, params[0].device.index,
-                        [list(k) for k in lists])
+    return AdamwTensors(records, _VALUES[p_type], _VALUES[g_type], 32 if m_scales is None else 8, dev, [list(k) for k in lists])
 
 
 def pilc_adamw_step(tensors: AdamwTensors, lr: float, beta1: float, beta2: float, eps: float, step: int,
                     grad_scale: float = 1.0, dither: int = 0, stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
     """One AdamW step, in place.  dither: with states in 8 bits another number every step, say the step's own."""
-    if tensors.device != torch.cuda.current_device():
-        raise TypeError("tensors must be on the current device")
+    dev = tensors.device
+    if dev != torch.cuda.current_device():
+        _bad("tensors", "those of a list made")
     par = pilc_adamw_params(lr, beta1, beta2, eps, grad_scale, step, tensors.param_type, tensors.grad_type, tensors.state_bits,
                             dither & 0xFFFFFFFF)
-    rc = lib().pilc_adamw_step(C.byref(par), tensors.records, len(tensors.records), _stream_handle(stream))
+    rc = lib().pilc_adamw_step(C.byref(par), tensors.records, len(tensors.records), _raw_stream(stream, dev))
     if check and rc != PILC_OK:
         raise PilcError(rc, "pilc_adamw_step")
     return rc
@@ -642,9 +670,9 @@ def pilc_adamw_step(tensors: AdamwTensors, lr: float, beta1: float, beta2: float
 
 def pilc_adamw_values(codes, scales, values, signed: bool, stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
     """values (float32) = what the codes of an 8-bit state stand for; signed for m, not for v."""
-    n = codes.numel()
-    rc = lib().pilc_adamw_values(_vector(codes, torch.uint8, n, "codes"), _vector(scales, torch.uint8, -(-n // 256), "scales"), n,
-                                 1 if signed else 0, _vector(values, torch.float32, n, "values"), _stream_handle(stream))
+    dev, n = _device_of(codes, "codes"), codes.numel()
+    rc = lib().pilc_adamw_values(_vector(codes, torch.uint8, n, dev, "codes"), _vector(scales, torch.uint8, -(-n // 256), dev, "scales"),
+                                 n, 1 if signed else 0, _vector(values, torch.float32, n, dev, "values"), _raw_stream(stream, dev))
     if check and rc != PILC_OK:
         raise PilcError(rc, "pilc_adamw_values")
     return rc

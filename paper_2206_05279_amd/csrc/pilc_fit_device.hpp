@@ -83,6 +83,16 @@ struct Raw {
         }
     }
     __device__ float operator[](int k) const { return widen(__builtin_bit_cast(Pack<T, kVec>, bits).v[k]); }
+    // value k, for a k that is not known beforehand
+    __device__ float at(uint32_t k) const
+    {
+        const uint32_t i = sizeof(T) == 4 ? k : k / 2;
+        const uint32_t word = i == 0 ? bits[0] : i == 1 ? bits[1] : i == 2 ? bits[2] : bits[3];
+        if constexpr (sizeof(T) == 4)
+            return __uint_as_float(word);
+        else
+            return widen(__builtin_bit_cast(T, (uint16_t)(k & 1 ? word >> 16 : word)));
+    }
     __device__ static Raw of(const float (&v)[kVec])
     {
         Pack<T, kVec> t;
@@ -160,6 +170,13 @@ __device__ __forceinline__ V block_reduce(V v, Op op, V *room)
     return v;
 }
 
+// One instruction, where the compiler would see to it first that no operand is a signalling NaN.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
+}
 // What is not a number is passed over.
 struct MaxFloat {
     __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }

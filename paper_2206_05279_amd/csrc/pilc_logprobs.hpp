@@ -98,6 +98,34 @@ struct Law {
     __device__ float logp(float x) const { return max == -kInf ? -kInf : (x - max) - log_total; }
 };
 
+// Where a workgroup, or with kThreads 64 a wavefront by itself, puts side by side what may be among a row's best.
+template <int kThreads>
+struct PickRoom {
+    static constexpr uint32_t kMost = kThreads < 256 ? 128 : 256;
+    uint32_t best[kThreads];
+    static constexpr uint32_t kMostPacks = kThreads < 256 ? 64 : 192;
+    uint64_t picked[kMost], rounds[kThreads / 64];
+    u32x4_t pack[kMostPacks];
+    uint32_t column[kMostPacks];
+    uint32_t count, packs;
+
+    __device__ __forceinline__ void add(uint32_t order, uint32_t sym)
+    {
+        const uint32_t at = atomicAdd(&count, 1u);
+        if (at < kMost) picked[at] = (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
+    }
+};
+template <int kThreads>
+__device__ __forceinline__ void meet()
+{
+    if constexpr (kThreads > 64) {
+        __syncthreads();
+    } else {  // a wavefront's accesses to LDS are done in order: the compiler has to leave them in it
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
 // A row, or a run of it, in registers: kLanes lanes hold kPer packs of 16 bytes each.  A pack that would reach over the
 // end begins earlier, and what another holds of it already is ruled out.  Rows need a pack's values at least.
 template <class T, int kLanes, int kPer>
@@ -125,9 +153,8 @@ struct LogitsRow {
 #pragma unroll
         for (int q = 0; q < kPer; ++q) x[q] = Raw<T>::load(p + column(q, begin, end));
     }
-    // Packs that are gone through, for all lanes the same: those with values of the row in them, up to a whole group of
-    // four.  The others are loaded, with the row's last values, and left alone.
-    static constexpr int kGroup = kPer < 4 ? kPer : 4;
+    // Packs that are gone through, for all lanes the same: those with values of the row in them, up to a whole group.  The others are loaded, with the row's last values, and left alone.
+    static constexpr int kGroup = kLanes == 1024 ? 2 : kPer < 4 ? kPer : 4;
     __device__ int used(uint32_t begin, uint32_t end) const
     {
         return (int)((end - begin + kLanes * kVec * kGroup - 1) / (kLanes * kVec * kGroup)) * kGroup;
@@ -159,26 +186,43 @@ struct LogitsRow {
     {
         float m = -kInf;
         for_used(used, [&](int q) {
-            float side[2] = {x[q][0], x[q][1]};
-#pragma unroll
-            for (int k = 2; k < kVec; k += 2) side[0] = fmaxf(side[0], x[q][k]), side[1] = fmaxf(side[1], x[q][k + 1]);
-            of[q] = fmaxf(side[0], side[1]);
-            m = fmaxf(m, of[q]);
+            of[q] = max3(x[q][0], x[q][1], x[q][2]);
+            if constexpr (kVec == 8) of[q] = max3(of[q], max3(x[q][3], x[q][4], x[q][5]), x[q][6]);
+            of[q] = max3(of[q], x[q][kVec - 1], of[q]);
+            m = max3(m, of[q], m);
         });
         return m;
     }
-    // f(order, symbol) for each of the lane's values from `least` on; `of`: the packs' largest
-    template <class F>
-    __device__ void each(Raw<T> (&x)[kPer], const float (&of)[kPer], uint32_t begin, uint32_t end, int used, float least, F f) const
+    // The keys of the values whose order is `line` at least.  Packs with such values are put into LDS and looked through
+    // there by all threads: to take them apart value by value in registers would be code for each of them.
+    __device__ bool collect(const Raw<T> (&x)[kPer], const float (&of)[kPer], uint32_t begin, uint32_t end, int used, uint32_t line,
+                            PickRoom<kLanes> &room) const
     {
+        const float least = value_of((uint64_t)line << 32);
         for_used(used, [&](int q) {
             if (of[q] >= least) {
-                x[q].forget();
-                const uint32_t column_q = column(q, begin, end);
-#pragma unroll
-                for (int k = 0; k < kVec; ++k)
-                    if (x[q][k] >= least) f(order_of(x[q][k]), column_q + k);
+                const uint32_t at = atomicAdd(&room.packs, 1u);
+                if (at < room.kMostPacks) room.pack[at] = x[q].bits, room.column[at] = column(q, begin, end);
             }
+        });
+        meet<kLanes>();
+        const uint32_t packs = room.packs;
+        if (packs > room.kMostPacks) return false;
+        for (uint32_t i = threadIdx.x & (kLanes - 1); i < packs * kVec; i += kLanes) {
+            const uint32_t order = order_of(widen(((const T *)&room.pack[i / kVec])[i % kVec]));
+            if (order >= line) room.add(order, room.column[i / kVec] + i % kVec);
+        }
+        return true;
+    }
+    // f(order, symbol) for each of the lane's values
+    template <class F>
+    __device__ void each(Raw<T> (&x)[kPer], uint32_t begin, uint32_t end, int used, F f) const
+    {
+        for_used(used, [&](int q) {
+            x[q].forget();
+            const uint32_t column_q = column(q, begin, end);
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) f(order_of(x[q][k]), column_q + k);
         });
     }
     // The same from memory, in little code
@@ -220,41 +264,25 @@ struct LogitsRow {
     }
 };
 
-// The `top` best of what kThreads threads hold: a workgroup, or with 64 a wavefront by itself.  `each` calls its second
-// argument with the order (see order_of) and symbol of the calling thread's values from its first on, `again` its argument
-// with all of them for the rare way below, `best` is the highest order among them; `put` is called, once for each place in
-// 0 .. top-1 and by some thread, with the place and the key that belongs there, or 0.
+// The `top` best of what kThreads threads hold: a workgroup, or with 64 a wavefront by itself.  `best` is the highest order
+// (see order_of) among the calling thread's values; `collect` puts the keys of all threads' values from an order on into
+// `room`, or says that they are too many; `again` calls its argument with order and symbol of all of the thread's values, for
+// the rare way below; `put` is called, once for each place in 0 .. top-1 and by some thread, with the place and the key that
+// belongs there, or 0.
 //
 // The top-th best of the threads' best values has `top` values at least that are as good, and few more in what a model
 // answers with; those are put side by side, and each one's place is the number of better ones.  The more threads stand
 // for a row the fewer there are to look at: four wavefronts that each pick by themselves before they join take longer
 // (16384 x 32768 bf16, 20 alternatives: 417 against 294 us).  Rows with many equal values may have too many of them:
 // then the best that is worse than the last is looked for `top` times.
-template <int kThreads>
-struct PickRoom {
-    static constexpr uint32_t kMost = kThreads < 256 ? 128 : 256;
-    uint32_t best[kThreads];
-    uint64_t picked[kMost], rounds[kThreads / 64];
-    uint32_t count;
-};
-template <int kThreads>
-__device__ __forceinline__ void meet()
-{
-    if constexpr (kThreads > 64) {
-        __syncthreads();
-    } else {  // a wavefront's accesses to LDS are done in order: the compiler has to leave them in it
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
-}
-template <int kThreads, int kBits, class Each, class Again, class Put>
-__device__ void pick_top(uint32_t top, uint32_t best, Each each, Again again, Put put, PickRoom<kThreads> &room)
+template <int kThreads, int kBits, class Collect, class Again, class Put>
+__device__ void pick_top(uint32_t top, uint32_t best, Collect collect, Again again, Put put, PickRoom<kThreads> &room)
 {
     constexpr int kEach = kThreads / 64;
     const uint32_t thread = threadIdx.x & (kThreads - 1);
     meet<kThreads>();  // `room` may be in use from a row before
     if (kEach > 1) room.best[thread] = best;
-    if (thread == 0) room.count = 0;
+    if (thread == 0) room.count = room.packs = 0;
     meet<kThreads>();
     // the highest order that `top` threads' best reach, bit by bit from the top; kBits is what the type's values differ in
     uint32_t b[kEach] = {best}, line = 0;
@@ -269,14 +297,10 @@ __device__ void pick_top(uint32_t top, uint32_t best, Each each, Again again, Pu
         if (reach >= top) line = next;
     }
     line = max(line, kOrderNone + 1);  // -inf is no alternative
-    if (best >= line)
-        each(line, [&](uint32_t order, uint32_t sym) {
-            const uint32_t at = atomicAdd(&room.count, 1u);
-            if (at < room.kMost) room.picked[at] = (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
-        });
+    const bool few = collect(line, room);
     meet<kThreads>();
     const uint32_t count = room.count;
-    if (count <= room.kMost) {
+    if (few && count <= room.kMost) {
         for (uint32_t i = thread; i < count; i += kThreads) {
             const uint64_t key = room.picked[i];
             uint32_t better = 0;
@@ -385,15 +409,11 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         const Tally tally = r.tally(x, used, own, room, half);
         r.forget(x);
         half ^= 1;
-        const auto each = [&](uint32_t line, auto f) { r.each(x, of, begin, end, used, value_of((uint64_t)line << 32), f); };
-        const auto again = [&](auto f) { r.again((const T *)a.x + row * a.stride, begin, end, f); };
-        const auto pick = [&](auto put) { pick_top<kPickers, kOrderBits<T>>(a.top, order_of(own), each, again, put, picked[r.row_in_block]); };
-        if (!kTrain && a.splits > 1) {
+        const bool whole = kTrain || a.splits == 1;
+        const Law law(tally);
+        if (!whole) {
             if (r.lane == 0) a.part[item] = make_float4(tally.max, tally.total, tally.inside, 0.0f);
-            if constexpr (kLanes >= 64 && !kTrain)  // no run of several is shorter
-                if (a.top) pick([&](uint32_t place, uint64_t key) { a.part_top[item * a.top + place] = key; });
         } else {
-            const Law law(tally);
             if (r.lane == 0) {
                 if (a.entropy) a.entropy[row] = law.entropy;
                 if (a.lse) a.lse[row] = law.lse();
@@ -405,10 +425,7 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
                 for (int q = 0; q < kPer; ++q) {
                     const uint32_t k = (uint32_t)t - r.column(q, begin, end);
                     if (k < (uint32_t)kVec && (int)k >= r.twice(q, begin, end)) {
-                        float at = 0.0f;
-#pragma unroll
-                        for (int i = 0; i < kVec; ++i) at = i == (int)k ? x[q][i] : at;
-                        a.logp[row] = law.logp(at);
+                        a.logp[row] = law.logp(x[q].at(k));
                     }
                 }
             if constexpr (kTrain) {
@@ -422,24 +439,33 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
                 r.for_used(used, [&](int q) {
                     put_gradient(x[q], grad, r.column(q, begin, end), r.twice(q, begin, end), scale, from, slope, in, t, up, zeros);
                 });
-            } else if (a.top) {
-                if constexpr (kLanes >= 64) {
-                    pick([&](uint32_t place, uint64_t key) { put_alternative(a, law, row, place, key); });
-                } else {
-                    // few values a lane: the best that is worse than the last, `top` times
-                    uint64_t below = ~0ull;
-                    for (uint32_t i = 0; i < a.top; ++i) {
-                        uint64_t best = 0;
-                        r.each(x, of, begin, end, used, -kInf, [&](uint32_t order, uint32_t sym) {
-                            const uint64_t key = (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
-                            if (order > kOrderNone && key < below && key > best) best = key;
-                        });
-                        const uint32_t high = lanes_reduce<Row::kWithin>((uint32_t)(best >> 32), Max());
-                        const uint32_t low = lanes_reduce<Row::kWithin>(best >> 32 == high ? (uint32_t)best : 0u, Max());
-                        below = (uint64_t)high << 32 | low;
-                        if (r.lane == 0) put_alternative(a, law, row, i, below);
-                    }
-                }
+            }
+        }
+        if constexpr (kPicks) {
+            if (a.top)
+                pick_top<kLanes, kOrderBits<T>>(
+                    a.top, order_of(own), [&](uint32_t line, auto &to) { return r.collect(x, of, begin, end, used, line, to); },
+                    [&](auto f) { r.again((const T *)a.x + row * a.stride, begin, end, f); },
+                    [&](uint32_t place, uint64_t key) {
+                        if (whole)
+                            put_alternative(a, law, row, place, key);
+                        else
+                            a.part_top[item * a.top + place] = key;
+                    },
+                    picked[r.row_in_block]);
+        } else if constexpr (!kTrain) {
+            // few values a lane, in whole rows: the best that is worse than the last, `top` times
+            uint64_t below = ~0ull;
+            for (uint32_t i = 0; i < a.top; ++i) {
+                uint64_t best = 0;
+                r.each(x, begin, end, used, [&](uint32_t order, uint32_t sym) {
+                    const uint64_t key = (uint64_t)order << 32 | (0xFFFFFFFFu - sym);
+                    if (order > kOrderNone && key < below && key > best) best = key;
+                });
+                const uint32_t high = lanes_reduce<Row::kWithin>((uint32_t)(best >> 32), Max());
+                const uint32_t low = lanes_reduce<Row::kWithin>(best >> 32 == high ? (uint32_t)best : 0u, Max());
+                below = (uint64_t)high << 32 | low;
+                if (r.lane == 0) put_alternative(a, law, row, i, below);
             }
         }
         if (Row::kAhead) {
@@ -497,13 +523,14 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type
             const auto again = [&](auto f) {
                 for (uint32_t i = thread; i < count; i += kThreads) f((uint32_t)(keys[i] >> 32), 0xFFFFFFFFu - (uint32_t)keys[i]);
             };
-            const auto each = [&](uint32_t line, auto f) {
+            const auto collect = [&](uint32_t line, auto &room) {
                 again([&](uint32_t order, uint32_t sym) {
-                    if (order >= line) f(order, sym);
+                    if (order >= line) room.add(order, sym);
                 });
+                return true;
             };
             pick_top<kThreads, 32>(
-                a.top, best, each, again, [&](uint32_t place, uint64_t key) { put_alternative(a, law, (uint32_t)row, place, key); }, picked[which]);
+                a.top, best, collect, again, [&](uint32_t place, uint64_t key) { put_alternative(a, law, (uint32_t)row, place, key); }, picked[which]);
         }
     }
 }
@@ -729,9 +756,10 @@ static void launch_grad(LogitsArgs a, hipStream_t stream)
             <<<logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, 0), Row::kThreads, 0, stream>>>(a);
         return true;
     };
-    (void)(with(integral_constant<int, 8>(), integral_constant<int, 1>()) || with(integral_constant<int, 32>(), integral_constant<int, 1>()) ||
-           with(integral_constant<int, 64>(), integral_constant<int, 1>()) || with(integral_constant<int, 256>(), integral_constant<int, 1>()) ||
-           with(integral_constant<int, 256>(), integral_constant<int, 2>()) || with(integral_constant<int, 256>(), integral_constant<int, 4>()));
+    (void)(with(integral_constant<int, 8>(), integral_constant<int, 1>()) || with(integral_constant<int, 8>(), integral_constant<int, 4>()) ||
+           with(integral_constant<int, 16>(), integral_constant<int, 4>()) || with(integral_constant<int, 32>(), integral_constant<int, 4>()) ||
+           with(integral_constant<int, 64>(), integral_constant<int, 4>()) || with(integral_constant<int, 256>(), integral_constant<int, 2>()) ||
+           with(integral_constant<int, 256>(), integral_constant<int, 4>()));
 }
 
 template <class Launch>
