@@ -275,8 +275,8 @@ struct LogitsRow {
 // for a row the fewer there are to look at: four wavefronts that each pick by themselves before they join take longer
 // (16384 x 32768 bf16, 20 alternatives: 417 against 294 us).  Rows with many equal values may have too many of them:
 // then the best that is worse than the last is looked for `top` times.
-template <int kThreads, int kBits, class Collect, class Again, class Put>
-__device__ void pick_top(uint32_t top, uint32_t best, Collect collect, Again again, Put put, PickRoom<kThreads> &room)
+template <int kThreads, class Collect, class Again, class Put>
+__device__ void pick_top(uint32_t top, int bits, uint32_t best, Collect collect, Again again, Put put, PickRoom<kThreads> &room)
 {
     constexpr int kEach = kThreads / 64;
     const uint32_t thread = threadIdx.x & (kThreads - 1);
@@ -284,12 +284,12 @@ __device__ void pick_top(uint32_t top, uint32_t best, Collect collect, Again aga
     if (kEach > 1) room.best[thread] = best;
     if (thread == 0) room.count = room.packs = 0;
     meet<kThreads>();
-    // the highest order that `top` threads' best reach, bit by bit from the top; kBits is what the type's values differ in
+    // the highest order that `top` threads' best reach, bit by bit from the top; `bits` is what the type's values differ in
     uint32_t b[kEach] = {best}, line = 0;
     if (kEach > 1)
 #pragma unroll
         for (int i = 0; i < kEach; ++i) b[i] = room.best[i * 64 + (threadIdx.x & 63)];
-    for (int bit = 31; bit >= 32 - kBits; --bit) {
+    for (int bit = 31; bit >= 32 - bits; --bit) {
         const uint32_t next = line | 1u << bit;
         uint32_t reach = 0;
 #pragma unroll
@@ -443,8 +443,8 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         }
         if constexpr (kPicks) {
             if (a.top)
-                pick_top<kLanes, kOrderBits<T>>(
-                    a.top, order_of(own), [&](uint32_t line, auto &to) { return r.collect(x, of, begin, end, used, line, to); },
+                pick_top<kLanes>(
+                    a.top, kOrderBits<T>, order_of(own), [&](uint32_t line, auto &to) { return r.collect(x, of, begin, end, used, line, to); },
                     [&](auto f) { r.again((const T *)a.x + row * a.stride, begin, end, f); },
                     [&](uint32_t place, uint64_t key) {
                         if (whole)
@@ -481,10 +481,17 @@ template <int kThreads>
 __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type)
 {
     constexpr uint32_t kRows = 256 / kThreads;
+    constexpr int kHeld = 4;
     __shared__ PickRoom<kThreads> picked[kRows];
     __shared__ Tally room[4];
     const uint32_t thread = threadIdx.x & (kThreads - 1), which = threadIdx.x / kThreads;
     for (uint64_t row = (uint64_t)blockIdx.x * kRows + which; row < a.rows; row += (uint64_t)gridDim.x * kRows) {
+        // the first keys are asked for with the rest, and kept
+        const uint64_t *keys = a.part_top + row * a.splits * a.top;
+        const uint32_t count = a.splits * a.top;
+        uint64_t held[kHeld];
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) held[i] = i * kThreads + thread < count ? keys[i * kThreads + thread] : 0;
         Tally t = {-kInf, 0.0f, 0.0f};
         for (uint32_t s = thread; s < a.splits; s += kThreads) {
             const float4 p = a.part[row * a.splits + s];
@@ -516,12 +523,14 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type
             }
         }
         if (a.top) {
-            const uint64_t *keys = a.part_top + row * a.splits * a.top;
-            const uint32_t count = a.splits * a.top;
             uint32_t best = 0;
-            for (uint32_t i = thread; i < count; i += kThreads) best = max(best, (uint32_t)(keys[i] >> 32));
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) best = max(best, (uint32_t)(held[i] >> 32));
+            for (uint32_t i = kHeld * kThreads + thread; i < count; i += kThreads) best = max(best, (uint32_t)(keys[i] >> 32));
             const auto again = [&](auto f) {
-                for (uint32_t i = thread; i < count; i += kThreads) f((uint32_t)(keys[i] >> 32), 0xFFFFFFFFu - (uint32_t)keys[i]);
+#pragma unroll
+                for (int i = 0; i < kHeld; ++i) f((uint32_t)(held[i] >> 32), 0xFFFFFFFFu - (uint32_t)held[i]);
+                for (uint32_t i = kHeld * kThreads + thread; i < count; i += kThreads) f((uint32_t)(keys[i] >> 32), 0xFFFFFFFFu - (uint32_t)keys[i]);
             };
             const auto collect = [&](uint32_t line, auto &room) {
                 again([&](uint32_t order, uint32_t sym) {
@@ -529,8 +538,9 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type
                 });
                 return true;
             };
-            pick_top<kThreads, 32>(
-                a.top, best, collect, again, [&](uint32_t place, uint64_t key) { put_alternative(a, law, (uint32_t)row, place, key); }, picked[which]);
+            pick_top<kThreads>(
+                a.top, type == PILC_BF16 ? kOrderBits<bf16_t> : type == PILC_F16 ? kOrderBits<f16_t> : kOrderBits<float>, best, collect, again,
+                [&](uint32_t place, uint64_t key) { put_alternative(a, law, (uint32_t)row, place, key); }, picked[which]);
         }
     }
 }
@@ -642,19 +652,20 @@ static bool logits_in_ok(const pilc_logits_shape *s, const void *logits, const v
     return logits && aligned_to(logits, value_bytes(s->dtype)) && aligned_to(target, target_bytes);
 }
 
-// How rows are gone through.  Runs are of 64 KB at most, the registers of a workgroup of 256; with few rows they are as
-// much smaller as it takes to give every compute unit two.
+// How rows are gone through.  Rows of up to 64 KB, in the registers of a workgroup of 256, are one run; longer ones go in
+// runs of 32 KB, of which more are on their way at a time (4093 x 100003 bf16: 184 us, in runs of 64 KB 209).  With few rows
+// runs are as much smaller as it takes to give every compute unit two.
 struct LogitsPlan {
     uint32_t splits, span;
 };
-constexpr uint32_t kLongestRun = 64 << 10, kShortestRun = 4 << 10;
+constexpr uint32_t kWholeRow = 64 << 10, kLongestRun = 32 << 10, kShortestRun = 8 << 10;
 static uint32_t div_up(uint32_t a, uint32_t b) { return a / b + (a % b != 0); }
-static LogitsPlan logits_plan(uint32_t rows, uint32_t num_sym, uint32_t value, uint32_t longest, uint32_t shortest)
+static LogitsPlan logits_plan(uint32_t rows, uint32_t num_sym, uint32_t value, uint32_t whole, uint32_t longest, uint32_t shortest)
 {
-    const uint32_t vec = 16 / value, needed = div_up(num_sym, longest / value), most = div_up(num_sym, shortest / value);
+    const uint32_t vec = 16 / value, needed = num_sym <= whole / value ? 1 : div_up(num_sym, longest / value), most = div_up(num_sym, shortest / value);
     const uint32_t wanted = div_up(2 * compute_units(), std::max(rows, 1u)), splits = std::max(needed, std::min(wanted, most));
     // many rows: full runs, so that only the last one has packs without values
-    const uint32_t span = splits == needed ? longest / value : div_up(div_up(num_sym, splits), vec) * vec;
+    const uint32_t span = splits == needed ? (splits == 1 ? num_sym : longest / value) : div_up(div_up(num_sym, splits), vec) * vec;
     return {div_up(num_sym, span), span};
 }
 // Whether pilc_logprobs_train keeps whole rows in registers: up to 256 KB, those of a workgroup of 1024.
@@ -662,7 +673,7 @@ constexpr uint32_t kLongestRow = 256 << 10;
 static bool train_by_row(uint32_t rows, uint32_t num_sym, uint32_t value)
 {
     const uint64_t bytes = (uint64_t)num_sym * value;
-    return bytes <= kLongestRow && (bytes <= kShortestRun || rows >= compute_units() / 2);
+    return bytes <= kLongestRow && (bytes <= (4u << 10) || rows >= compute_units() / 2);
 }
 
 static size_t logits_workspace(const pilc_logits_shape &s)
@@ -670,16 +681,18 @@ static size_t logits_workspace(const pilc_logits_shape &s)
     size_t most = 256;
     const uint32_t values[] = {2, 4};
     for (uint32_t value : values) {  // whatever the type, so that a caller need not ask for each
-        const LogitsPlan p = logits_plan(s.rows, s.num_sym, value, kLongestRun, kShortestRun);
+        const LogitsPlan p = logits_plan(s.rows, s.num_sym, value, kWholeRow, kLongestRun, kShortestRun);
         const size_t runs = (size_t)s.rows * p.splits;
         if (p.splits > 1) most = std::max(most, runs * (sizeof(float4) + sizeof(uint64_t) * s.top) + (s.top ? 0 : 2 * sizeof(float) * (size_t)s.rows));
     }
     return most;
 }
 
-// Calls `go` with the lanes and packs a lane for runs of `bytes` bytes.
+// Calls `go` with the lanes and packs a lane for runs of `bytes` bytes.  Alternatives of short rows are looked for by a whole
+// wavefront where twice as many of its lanes as alternatives have values (65536 x 256 f32, 20 alternatives: 109 us in
+// groups of 16 lanes, 59 by 64).
 template <bool kWholeRows, class Go>
-static void logits_row(uint32_t bytes, Go go)
+static void logits_row(uint32_t bytes, uint32_t top, Go go)
 {
     using std::integral_constant;
     const auto with = [&](auto lanes, auto per) {
@@ -693,6 +706,8 @@ static void logits_row(uint32_t bytes, Go go)
     const integral_constant<int, 8> eight;
     const integral_constant<int, 16> sixteen;
     const integral_constant<int, 256> group;
+    if constexpr (!kWholeRows)
+        if (top && bytes >= 32 * top && (with(integral_constant<int, 64>(), one) || with(integral_constant<int, 64>(), two))) return;
     const bool done = with(integral_constant<int, 8>(), one) || with(integral_constant<int, 8>(), four) || with(integral_constant<int, 16>(), four) ||
                       with(integral_constant<int, 32>(), four) || with(integral_constant<int, 64>(), four) || with(group, two) || with(group, four) ||
                       with(group, eight) || with(group, sixteen);
@@ -715,7 +730,7 @@ static void launch_logits(const LogitsArgs &a, hipStream_t stream)
         k_logits_short<T, kTrain, false><<<(uint32_t)std::min<uint64_t>((a.rows + 255ull) / 256, 1u << 20), 256, 0, stream>>>(a);
         return;
     }
-    logits_row<kTrain>(a.span * (uint32_t)sizeof(T), [&](auto lanes, auto per) {
+    logits_row<kTrain>(a.span * (uint32_t)sizeof(T), a.top, [&](auto lanes, auto per) {
         using Row = LogitsRow<T, decltype(lanes)::value, decltype(per)::value>;
         const uint32_t blocks = logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, Row::kAhead ? Row::waves(kTrain) : 0);
         k_logits<T, decltype(lanes)::value, decltype(per)::value, kTrain><<<blocks, Row::kThreads, 0, stream>>>(a);
@@ -726,7 +741,7 @@ static void launch_logits(const LogitsArgs &a, hipStream_t stream)
 template <class T>
 static void launch_law(LogitsArgs a, uint32_t type, void *workspace, hipStream_t stream)
 {
-    const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kLongestRun, kShortestRun);
+    const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kWholeRow, kLongestRun, kShortestRun);
     a.splits = p.splits, a.span = std::min(p.span, a.num_sym);
     a.part = (float4 *)workspace;
     a.part_top = (uint64_t *)(a.part + (size_t)a.rows * a.splits);
@@ -746,7 +761,7 @@ static void launch_grad(LogitsArgs a, hipStream_t stream)
         return;
     }
     constexpr uint32_t kRun = 16 << 10;
-    const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kRun, kShortestRun);
+    const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kRun, kRun, kShortestRun);
     a.splits = p.splits, a.span = std::min(p.span, a.num_sym);
     using std::integral_constant;
     const auto with = [&](auto lanes, auto per) {
@@ -855,7 +870,7 @@ int pilc_logprobs_train(const pilc_logits_shape *shape, const void *logits_dev, 
         // too few rows to keep the GPU busy one a workgroup, or too long ones: the law first, then the gradient by it
         LogitsArgs g = a;
         if (!a.lse || !a.entropy) {  // kept behind the runs' parts where the caller does not want them
-            const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kLongestRun, kShortestRun);
+            const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kWholeRow, kLongestRun, kShortestRun);
             float *kept = (float *)((float4 *)workspace_dev + (size_t)a.rows * p.splits);
             if (!a.lse) a.lse = kept;
             if (!a.entropy) a.entropy = kept + a.rows;
