@@ -676,14 +676,19 @@ static bool train_by_row(uint32_t rows, uint32_t num_sym, uint32_t value)
     return bytes <= kLongestRow && (bytes <= (4u << 10) || rows >= compute_units() / 2);
 }
 
+// What the runs of split rows leave for the kernel that puts them together.
+static size_t parts_bytes(const LogitsPlan &p, uint32_t rows, uint32_t top)
+{
+    return p.splits > 1 ? (size_t)rows * p.splits * (sizeof(float4) + sizeof(uint64_t) * top) : 0;
+}
 static size_t logits_workspace(const pilc_logits_shape &s)
 {
     size_t most = 256;
-    const uint32_t values[] = {2, 4};
-    for (uint32_t value : values) {  // whatever the type, so that a caller need not ask for each
+    for (uint32_t value : {2u, 4u}) {  // whatever the type, so that a caller need not ask for each
         const LogitsPlan p = logits_plan(s.rows, s.num_sym, value, kWholeRow, kLongestRun, kShortestRun);
-        const size_t runs = (size_t)s.rows * p.splits;
-        if (p.splits > 1) most = std::max(most, runs * (sizeof(float4) + sizeof(uint64_t) * s.top) + (s.top ? 0 : 2 * sizeof(float) * (size_t)s.rows));
+        // pilc_logprobs_train, where it goes two ways, keeps lse and entropy behind the parts
+        const size_t kept = s.top == 0 && !train_by_row(s.rows, s.num_sym, value) ? 2 * sizeof(float) * (size_t)s.rows : 0;
+        most = std::max(most, parts_bytes(p, s.rows, s.top) + kept);
     }
     return most;
 }
@@ -794,8 +799,6 @@ static int by_type(uint32_t type, Launch launch)
     return PILC_OK;
 }
 
-static uint32_t row_blocks(uint32_t rows) { return std::min(rows, 1u << 20); }
-
 }  // namespace pilc
 
 extern "C" {
@@ -871,7 +874,7 @@ int pilc_logprobs_train(const pilc_logits_shape *shape, const void *logits_dev, 
         LogitsArgs g = a;
         if (!a.lse || !a.entropy) {  // kept behind the runs' parts where the caller does not want them
             const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kWholeRow, kLongestRun, kShortestRun);
-            float *kept = (float *)((float4 *)workspace_dev + (size_t)a.rows * p.splits);
+            float *kept = (float *)((char *)workspace_dev + parts_bytes(p, a.rows, 0));
             if (!a.lse) a.lse = kept;
             if (!a.entropy) a.entropy = kept + a.rows;
         }

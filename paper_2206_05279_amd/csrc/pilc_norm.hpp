@@ -14,7 +14,7 @@ struct NormArgs {
     float eps;
 };
 
-constexpr int kNormThreads = 256;
+constexpr int kNormThreads = 256, kNormLongThreads = 1024;
 // Wavefronts a SIMD that the kernels' registers are kept down to, and that are launched: all at once, each going from row to row.
 constexpr int kNormForwardWaves = 5, kNormBackwardWaves = 3;
 
@@ -241,39 +241,113 @@ k_norm_backward_rows(NormArgs a)
     }
 }
 
-// Rows too long for registers, or shorter than a pack.
+// Rows shorter than eight values: a thread a row.
 template <class T, class W>
-__global__ __launch_bounds__(kNormThreads) void k_norm_forward(NormArgs a)
+__global__ __launch_bounds__(kNormThreads) void k_norm_forward_narrow(NormArgs a)
 {
-    constexpr int kWaves = kNormThreads / 64;
+    const W *weight = (const W *)a.weight, *bias = (const W *)a.bias;
+    for (uint64_t row = blockIdx.x * (uint64_t)kNormThreads + threadIdx.x; row < a.rows; row += gridDim.x * (uint64_t)kNormThreads) {
+        const T *x = (const T *)a.x + row * a.x_stride;
+        T *y = (T *)a.y + row * a.y_stride;
+        float mean = 0.0f, square = 0.0f;
+        for (uint32_t j = 0; j < a.width; ++j) mean += widen(x[j]);
+        mean /= (float)a.width;
+        for (uint32_t j = 0; j < a.width; ++j) {
+            const float d = widen(x[j]) - mean;
+            square += d * d;
+        }
+        const float rstd = 1.0f / sqrtf(square / (float)a.width + a.eps);
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+        for (uint32_t j = 0; j < a.width; ++j)
+            y[j] = (T)((widen(x[j]) - mean) * rstd * (weight ? widen(weight[j]) : 1.0f) + (bias ? widen(bias[j]) : 0.0f));
+    }
+}
+template <class T, class W>
+__global__ __launch_bounds__(kNormThreads) void k_norm_dx_narrow(NormArgs a)
+{
+    const W *weight = (const W *)a.weight;
+    for (uint64_t row = blockIdx.x * (uint64_t)kNormThreads + threadIdx.x; row < a.rows; row += gridDim.x * (uint64_t)kNormThreads) {
+        const T *x = (const T *)a.x + row * a.x_stride, *dy = (const T *)a.dy + row * a.y_stride;
+        T *dx = (T *)a.dx + row * a.dx_stride;
+        const float mean = a.mean_in[row], rstd = a.rstd_in[row];
+        float c1 = 0.0f, c2 = 0.0f;
+        for (uint32_t j = 0; j < a.width; ++j) {
+            const float q = widen(dy[j]) * (weight ? widen(weight[j]) : 1.0f);
+            c1 += q;
+            c2 += q * ((widen(x[j]) - mean) * rstd);
+        }
+        c1 /= (float)a.width, c2 /= (float)a.width;
+        for (uint32_t j = 0; j < a.width; ++j) {
+            const float q = widen(dy[j]) * (weight ? widen(weight[j]) : 1.0f);
+            dx[j] = (T)(rstd * (q - c1 - (widen(x[j]) - mean) * rstd * c2));
+        }
+    }
+}
+
+// Rows too long for registers: a workgroup goes through them two or three times, a pack a thread at a time, and finds
+// them in the caches after the first.
+template <class T, int kVec, class F>
+__device__ __forceinline__ void for_packs(uint32_t width, F f)
+{
+    for (uint32_t place = threadIdx.x * kVec; place < width; place += kNormLongThreads * kVec) {
+        const uint32_t column = min(place, width - kVec);  // the last one begins earlier: its first values have been gone through
+        f(column, (int)(place - column));
+    }
+}
+template <int kVec, class T>
+__device__ __forceinline__ Pack<T, kVec> pack_at(const T *p) { return *(const Pack<T, kVec> *)p; }
+
+// No __restrict__, and what is stored twice is the same: y may be x.
+template <class T, class W>
+__global__ __launch_bounds__(kNormLongThreads) void k_norm_forward_long(NormArgs a)
+{
+    constexpr int kVec = 16 / sizeof(T);
+    constexpr int kWaves = kNormLongThreads / 64;
     __shared__ float room[kWaves];
     const W *weight = (const W *)a.weight, *bias = (const W *)a.bias;
     for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *x = (const T *)a.x + row * a.x_stride;
         T *y = (T *)a.y + row * a.y_stride;
-        float sum = 0.0f;
-        for (uint32_t j = threadIdx.x; j < a.width; j += kNormThreads) sum += widen(x[j]);
+        float sum = 0.0f, square = 0.0f;
+        for_packs<T, kVec>(a.width, [&](uint32_t column, int twice) {
+            const auto t = pack_at<kVec>(x + column);
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) sum += k >= twice ? widen(t.v[k]) : 0.0f;
+        });
         const float mean = block_reduce<kWaves>(sum, Sum(), room) / (float)a.width;
-        float square = 0.0f;
-        for (uint32_t j = threadIdx.x; j < a.width; j += kNormThreads) {
-            const float d = widen(x[j]) - mean;
-            square += d * d;
-        }
+        for_packs<T, kVec>(a.width, [&](uint32_t column, int twice) {
+            const auto t = pack_at<kVec>(x + column);
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) {
+                const float d = k >= twice ? widen(t.v[k]) - mean : 0.0f;
+                square += d * d;
+            }
+        });
         const float rstd = 1.0f / sqrtf(block_reduce<kWaves>(square, Sum(), room) / (float)a.width + a.eps);
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
-        for (uint32_t j = threadIdx.x; j < a.width; j += kNormThreads)
-            y[j] = (T)((widen(x[j]) - mean) * rstd * (weight ? widen(weight[j]) : 1.0f) + (bias ? widen(bias[j]) : 0.0f));
+        for (uint32_t place = threadIdx.x * kVec; place < a.width; place += kNormLongThreads * kVec) {
+            const int valid = (int)min(a.width - place, (uint32_t)kVec);  // not a value twice: the other may be y already
+            const auto t = load_pack<kVec>(x + place, valid);
+            Pack<T, kVec> out;
+#pragma unroll
+            for (int k = 0; k < kVec; ++k)
+                out.v[k] = (T)((widen(t.v[k]) - mean) * rstd * (weight && k < valid ? widen(weight[place + k]) : 1.0f) +
+                               (bias && k < valid ? widen(bias[place + k]) : 0.0f));
+            store_pack(y + place, valid, out);
+        }
         __syncthreads();
     }
 }
 
 template <class T, class W>
-__global__ __launch_bounds__(kNormThreads) void k_norm_dx(NormArgs a)
+__global__ __launch_bounds__(kNormLongThreads) void k_norm_dx_long(NormArgs a)
 {
-    constexpr int kWaves = kNormThreads / 64;
+    constexpr int kVec = 16 / sizeof(T);
+    constexpr int kWaves = kNormLongThreads / 64;
     __shared__ float room[kWaves];
     const W *weight = (const W *)a.weight;
     for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -281,34 +355,56 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_dx(NormArgs a)
         T *dx = (T *)a.dx + row * a.dx_stride;
         const float mean = a.mean_in[row], rstd = a.rstd_in[row];
         float q_sum = 0.0f, qx_sum = 0.0f;
-        for (uint32_t j = threadIdx.x; j < a.width; j += kNormThreads) {
-            const float q = widen(dy[j]) * (weight ? widen(weight[j]) : 1.0f);
-            q_sum += q;
-            qx_sum += q * ((widen(x[j]) - mean) * rstd);
-        }
+        for_packs<T, kVec>(a.width, [&](uint32_t column, int twice) {
+            const auto tx = pack_at<kVec>(x + column), td = pack_at<kVec>(dy + column);
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) {
+                const float q = k >= twice ? widen(td.v[k]) * (weight ? widen(weight[column + k]) : 1.0f) : 0.0f;
+                q_sum += q;
+                qx_sum += q * ((widen(tx.v[k]) - mean) * rstd);
+            }
+        });
         const float c1 = block_reduce<kWaves>(q_sum, Sum(), room) / (float)a.width;
         const float c2 = block_reduce<kWaves>(qx_sum, Sum(), room) / (float)a.width;
-        for (uint32_t j = threadIdx.x; j < a.width; j += kNormThreads) {
-            const float q = widen(dy[j]) * (weight ? widen(weight[j]) : 1.0f);
-            dx[j] = (T)(rstd * (q - c1 - (widen(x[j]) - mean) * rstd * c2));
+        for (uint32_t place = threadIdx.x * kVec; place < a.width; place += kNormLongThreads * kVec) {
+            const int valid = (int)min(a.width - place, (uint32_t)kVec);
+            const auto tx = load_pack<kVec>(x + place, valid), td = load_pack<kVec>(dy + place, valid);
+            Pack<T, kVec> out;
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) {
+                const float q = widen(td.v[k]) * (weight && k < valid ? widen(weight[place + k]) : 1.0f);
+                out.v[k] = (T)(rstd * (q - c1 - (widen(tx.v[k]) - mean) * rstd * c2));
+            }
+            store_pack(dx + place, valid, out);
         }
+        __syncthreads();
     }
 }
 
-// Thread per column, the rows in num_parts runs; before dx, which may take dy's place.
-template <class T>
+// A pack of columns a thread, the rows in num_parts runs; before dx, which may take dy's place.
+template <class T, int kVec>
 __global__ __launch_bounds__(kNormThreads) void k_norm_parts(NormArgs a)
 {
-    const uint32_t j = blockIdx.x * kNormThreads + threadIdx.x;
-    if (j >= a.width) return;
-    float dw = 0.0f, db = 0.0f;
+    const uint32_t place = (blockIdx.x * kNormThreads + threadIdx.x) * kVec;
+    if (place >= a.width) return;
+    const uint32_t column = min(place, a.width - kVec);
+    float dw[kVec] = {}, db[kVec] = {};
+#pragma unroll 4
     for (uint32_t row = blockIdx.y; row < a.rows; row += a.num_parts) {
-        const float d = widen(((const T *)a.dy)[row * a.y_stride + j]);
-        db += d;
-        dw += d * ((widen(((const T *)a.x)[row * a.x_stride + j]) - a.mean_in[row]) * a.rstd_in[row]);
+        const auto tx = pack_at<kVec>((const T *)a.x + row * a.x_stride + column), td = pack_at<kVec>((const T *)a.dy + row * a.y_stride + column);
+        const float mean = a.mean_in[row], rstd = a.rstd_in[row];
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) {
+            const float d = widen(td.v[k]);
+            db[k] += d;
+            dw[k] += d * ((widen(tx.v[k]) - mean) * rstd);
+        }
     }
-    a.parts[(size_t)blockIdx.y * a.width + j] = dw;
-    a.parts[(size_t)(a.num_parts + blockIdx.y) * a.width + j] = db;
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+        a.parts[(size_t)blockIdx.y * a.width + column + k] = dw[k];
+        a.parts[(size_t)(a.num_parts + blockIdx.y) * a.width + column + k] = db[k];
+    }
 }
 
 // The parts added up: 64 columns a workgroup, each by sixteen threads that take every sixteenth part.
@@ -351,6 +447,7 @@ static bool norm_row(uint32_t width, Go go)
 }
 
 constexpr uint32_t kNormLongParts = 64;
+static uint32_t narrow_blocks(uint32_t rows) { return std::min(div_up(rows, kNormThreads), 1u << 20); }
 template <class Row>
 static uint32_t norm_blocks(uint32_t rows, int most_waves)
 {
@@ -407,7 +504,11 @@ int pilc_norm_forward(const pilc_norm_shape *shape, const void *x_dev, const voi
             const uint32_t blocks = norm_blocks<Row>(a.rows, kNormForwardWaves);
             k_norm_forward_rows<T, W, decltype(lanes)::value, decltype(each)::value><<<blocks, Row::kThreads, 0, (hipStream_t)hip_stream>>>(a);
         });
-        if (!done) k_norm_forward<T, W><<<row_blocks(a.rows), kNormThreads, 0, (hipStream_t)hip_stream>>>(a);
+        if (done) return;
+        if (a.width < 8)
+            k_norm_forward_narrow<T, W><<<narrow_blocks(a.rows), kNormThreads, 0, (hipStream_t)hip_stream>>>(a);
+        else
+            k_norm_forward_long<T, W><<<std::min(a.rows, 1u << 20), kNormLongThreads, 0, (hipStream_t)hip_stream>>>(a);
     });
 }
 
@@ -448,9 +549,21 @@ int pilc_norm_backward(const pilc_norm_shape *shape, const void *dy_dev, const v
         });
         if (!done) {
             a.num_parts = std::min(a.rows, kNormLongParts);
-            // before dx, which may take dy's place
-            if (a.parts && a.rows) k_norm_parts<T><<<dim3((a.width + kNormThreads - 1) / kNormThreads, a.num_parts), kNormThreads, 0, stream>>>(a);
-            if (a.dx && a.rows) k_norm_dx<T, W><<<row_blocks(a.rows), kNormThreads, 0, stream>>>(a);
+            const bool narrow = a.width < 8;
+            const uint32_t each = kNormThreads * (narrow ? 1 : 16 / sizeof(T));
+            const dim3 grid((a.width + each - 1) / each, a.num_parts);
+            if (a.parts && a.rows) {
+                if (narrow)
+                    k_norm_parts<T, 1><<<grid, kNormThreads, 0, stream>>>(a);
+                else
+                    k_norm_parts<T, 16 / sizeof(T)><<<grid, kNormThreads, 0, stream>>>(a);
+            }
+            if (a.dx && a.rows) {
+                if (narrow)
+                    k_norm_dx_narrow<T, W><<<narrow_blocks(a.rows), kNormThreads, 0, stream>>>(a);
+                else
+                    k_norm_dx_long<T, W><<<std::min(a.rows, 1u << 20), kNormLongThreads, 0, stream>>>(a);
+            }
         }
         if (a.parts) k_norm_join<W><<<dim3((a.width + 63) / 64, 2), 1024, 0, stream>>>(a);
     });

@@ -173,6 +173,25 @@ def test_what_is_not_wanted_is_not_written_and_need_not_be_there():
     close(c.logp, c.law["logp"], c.law["logp_err"], torch.float32, "logp alone")
 
 
+@pytest.mark.parametrize("rows,n", [(1, 3000), (100, 3000), (100, 1500), (127, 2500), (5, 70000), (40, 9000), (130, 200000), (3, 1100000)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_training_without_lse_and_entropy_stays_in_its_workspace(rows, n, dtype):
+    rng = np.random.default_rng(n)
+    t = rng.integers(0, n, rows)
+    x, _ = placed(rng.normal(size=(rows, n)), TYPES[dtype])
+    size = pb.pilc_logprobs_workspace_size(rows, n)
+    whole = torch.full((size + 8192,), 0x5A, dtype=torch.uint8, device=DEV)
+    a, b = torch.ones(rows, device=DEV), torch.full((rows,), 0.5, device=DEV)
+    logp, grad = torch.empty(rows, device=DEV), torch.empty_like(x)
+    pb.pilc_logprobs_train(x, torch.from_numpy(t).to(DEV), a, logp, grad, up_entropy=b, workspace=whole[:size])
+    assert (whole[size:] == 0x5A).all()
+    some = [0, rows // 2, rows - 1]
+    law = orc.logprobs(up(x[some]), t[some], 0)
+    want, err = orc.logprobs_grad(up(x[some]), t[some], np.ones(3), np.full(3, 0.5))
+    close(logp[some], law["logp"], law["logp_err"], torch.float32, "logp")
+    close(grad[some], want, err, TYPES[dtype], "gradient")
+
+
 def test_no_rows():
     e = torch.empty(0, 40, device=DEV)
     ws = torch.empty(256, dtype=torch.uint8, device=DEV)
