@@ -26,6 +26,7 @@ template <class T, class W, int kLanes, int kEach>
 struct NormRow {
     static constexpr int kVec = 16 / sizeof(T), kPer = kEach / kVec;
     static constexpr bool kAhead = kLanes < 1024;  // the next row is asked for early; the largest workgroups lack the registers
+    static constexpr bool kKeep = kEach <= 16;     // the weights stay in registers; the longest rows' come from the caches
     static constexpr int kThreads = kLanes > 256 ? kLanes : 256;
     static constexpr int kRows = kThreads / kLanes;  // that a workgroup has in hand
     static constexpr int kWaves = kLanes / 64;       // that share a row
@@ -49,16 +50,18 @@ struct NormRow {
         for (int q = 0; q < kPer; ++q) out[q] = Raw<T>::load(p + column(q));
     }
     // weights as they lie in memory, `none` where there are none
+    __device__ Pack<W, kVec> weights(const W *p, float none, int q) const
+    {
+        if (p) return *(const Pack<W, kVec> *)(p + column(q));
+        Pack<W, kVec> t;
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) t.v[k] = (W)none;
+        return t;
+    }
     __device__ void load_weights(const W *p, float none, Pack<W, kVec> (&out)[kPer]) const
     {
 #pragma unroll
-        for (int q = 0; q < kPer; ++q)
-            if (p) {
-                out[q] = *(const Pack<W, kVec> *)(p + column(q));
-            } else {
-#pragma unroll
-                for (int k = 0; k < kVec; ++k) out[q].v[k] = (W)none;
-            }
+        for (int q = 0; q < kPer; ++q) out[q] = weights(p, none, q);
     }
 
     // The sum over a lane's values of f(pack, value)
@@ -114,8 +117,10 @@ k_norm_forward_rows(NormArgs a)
     const Row r(a.width);
     const float per_value = 1.0f / (float)a.width;
     Pack<W, kVec> weight[kPer], bias[kPer];
-    r.load_weights((const W *)a.weight, 1.0f, weight);
-    r.load_weights((const W *)a.bias, 0.0f, bias);
+    if (Row::kKeep) {
+        r.load_weights((const W *)a.weight, 1.0f, weight);
+        r.load_weights((const W *)a.bias, 0.0f, bias);
+    }
     Raw<T> x[kPer], next[kPer];
     uint32_t row = blockIdx.x * Row::kRows + r.row_in_block;
     const uint32_t step = gridDim.x * Row::kRows, last = a.rows - 1;
@@ -139,6 +144,10 @@ k_norm_forward_rows(NormArgs a)
         T *y = (T *)a.y + row * a.y_stride;
 #pragma unroll
         for (int q = 0; q < kPer; ++q) {
+            if (!Row::kKeep) {
+                weight[q] = r.weights((const W *)a.weight, 1.0f, q);
+                bias[q] = r.weights((const W *)a.bias, 0.0f, q);
+            }
             float out[kVec];
 #pragma unroll
             for (int k = 0; k < kVec; ++k) out[k] = (x[q][k] - mean) * rstd * widen(weight[q].v[k]) + widen(bias[q].v[k]);
@@ -149,7 +158,7 @@ k_norm_forward_rows(NormArgs a)
 }
 
 // dx row by row as above, and what the rows a workgroup meets add to the weights' gradients, in registers; at the end
-// the workgroup's rows are added up and put down as one part.
+// the workgroup's rows are added up and put down as one part.  The longest rows leave no room for that: k_norm_parts.
 template <class T, class W, int kLanes, int kEach>
 __global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads), (NormRow<T, W, kLanes, kEach>::waves(kNormBackwardWaves))) void
 k_norm_backward_rows(NormArgs a)
@@ -162,7 +171,7 @@ k_norm_backward_rows(NormArgs a)
     const float per_value = 1.0f / (float)a.width;
     Pack<W, kVec> weight[kPer];
     float dw[kPer][kVec] = {}, db[kPer][kVec] = {};
-    r.load_weights((const W *)a.weight, 1.0f, weight);
+    if (Row::kKeep) r.load_weights((const W *)a.weight, 1.0f, weight);
     Raw<T> x[kPer], dy[kPer], next_x[kPer], next_dy[kPer];
     uint32_t row = blockIdx.x * Row::kRows + r.row_in_block;
     const uint32_t step = gridDim.x * Row::kRows, last = a.rows - 1;
@@ -181,18 +190,20 @@ k_norm_backward_rows(NormArgs a)
             fetch(last - row > step ? row + step : last, next_mean, next_rstd, next_x, next_dy);
         else
             fetch(row, mean, rstd, x, dy);
+        if (!Row::kKeep) r.load_weights((const W *)a.weight, 1.0f, weight);
         float2 sums = r.own_sum(make_float2(0.0f, 0.0f), [&](float2 &s, int q, int k) {
             const float g = dy[q][k] * widen(weight[q].v[k]);
             s.x += g;
             s.y += g * ((x[q][k] - mean) * rstd);
         });
+        if (Row::kKeep)
 #pragma unroll
-        for (int q = 0; q < kPer; ++q)
+            for (int q = 0; q < kPer; ++q)
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                dw[q][k] += dy[q][k] * ((x[q][k] - mean) * rstd);
-                db[q][k] += dy[q][k];
-            }
+                for (int k = 0; k < kVec; ++k) {
+                    dw[q][k] += dy[q][k] * ((x[q][k] - mean) * rstd);
+                    db[q][k] += dy[q][k];
+                }
         if (a.dx) {
             sums = r.sum(sums, room, half);
             half ^= 1;
@@ -212,7 +223,7 @@ k_norm_backward_rows(NormArgs a)
             for (int q = 0; q < kPer; ++q) x[q] = next_x[q], dy[q] = next_dy[q];
         }
     }
-    if (!a.parts) return;
+    if (!Row::kKeep || !a.parts) return;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         float *part = a.parts + ((size_t)which * gridDim.x + blockIdx.x) * a.width;
@@ -264,23 +275,42 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_forward_narrow(NormArgs a
     }
 }
 template <class T, class W>
-__global__ __launch_bounds__(kNormThreads) void k_norm_dx_narrow(NormArgs a)
+__global__ __launch_bounds__(kNormThreads) void k_norm_backward_narrow(NormArgs a)
 {
+    constexpr int kMost = 7, kWaves = kNormThreads / 64;
+    __shared__ float room[kWaves];
     const W *weight = (const W *)a.weight;
+    float dw[kMost] = {}, db[kMost] = {};
     for (uint64_t row = blockIdx.x * (uint64_t)kNormThreads + threadIdx.x; row < a.rows; row += gridDim.x * (uint64_t)kNormThreads) {
         const T *x = (const T *)a.x + row * a.x_stride, *dy = (const T *)a.dy + row * a.y_stride;
-        T *dx = (T *)a.dx + row * a.dx_stride;
         const float mean = a.mean_in[row], rstd = a.rstd_in[row];
-        float c1 = 0.0f, c2 = 0.0f;
-        for (uint32_t j = 0; j < a.width; ++j) {
-            const float q = widen(dy[j]) * (weight ? widen(weight[j]) : 1.0f);
-            c1 += q;
-            c2 += q * ((widen(x[j]) - mean) * rstd);
+        float q[kMost], xh[kMost], c1 = 0.0f, c2 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kMost; ++j) {
+            q[j] = xh[j] = 0.0f;
+            if (j < (int)a.width) {
+                const float d = widen(dy[j]);
+                q[j] = d * (weight ? widen(weight[j]) : 1.0f);
+                xh[j] = (widen(x[j]) - mean) * rstd;
+                dw[j] += d * xh[j];
+                db[j] += d;
+            }
+            c1 += q[j];
+            c2 += q[j] * xh[j];
         }
         c1 /= (float)a.width, c2 /= (float)a.width;
-        for (uint32_t j = 0; j < a.width; ++j) {
-            const float q = widen(dy[j]) * (weight ? widen(weight[j]) : 1.0f);
-            dx[j] = (T)(rstd * (q - c1 - (widen(x[j]) - mean) * rstd * c2));
+        if (a.dx)
+#pragma unroll
+            for (int j = 0; j < kMost; ++j)
+                if (j < (int)a.width) ((T *)a.dx + row * a.dx_stride)[j] = (T)(rstd * (q[j] - c1 - xh[j] * c2));
+    }
+    if (!a.parts) return;
+#pragma unroll
+    for (int j = 0; j < kMost; ++j) {
+        const float sw = block_reduce<kWaves>(dw[j], Sum(), room), sb = block_reduce<kWaves>(db[j], Sum(), room);
+        if (threadIdx.x == 0 && j < (int)a.width) {
+            a.parts[(size_t)blockIdx.x * a.width + j] = sw;
+            a.parts[(size_t)(gridDim.x + blockIdx.x) * a.width + j] = sb;
         }
     }
 }
@@ -382,9 +412,10 @@ __global__ __launch_bounds__(kNormLongThreads) void k_norm_dx_long(NormArgs a)
 }
 
 // A pack of columns a thread, the rows in num_parts runs; before dx, which may take dy's place.
-template <class T, int kVec>
+template <class T>
 __global__ __launch_bounds__(kNormThreads) void k_norm_parts(NormArgs a)
 {
+    constexpr int kVec = 16 / sizeof(T);
     const uint32_t place = (blockIdx.x * kNormThreads + threadIdx.x) * kVec;
     if (place >= a.width) return;
     const uint32_t column = min(place, a.width - kVec);
@@ -443,7 +474,7 @@ static bool norm_row(uint32_t width, Go go)
     return with(integral_constant<int, 8>(), integral_constant<int, 8>()) || with(integral_constant<int, 32>(), integral_constant<int, 8>()) ||
            with(integral_constant<int, 64>(), integral_constant<int, 16>()) || with(integral_constant<int, 256>(), integral_constant<int, 8>()) ||
            with(integral_constant<int, 256>(), integral_constant<int, 16>()) || with(integral_constant<int, 512>(), integral_constant<int, 16>()) ||
-           with(integral_constant<int, 1024>(), integral_constant<int, 16>());
+           with(integral_constant<int, 1024>(), integral_constant<int, 16>()) || with(integral_constant<int, 1024>(), integral_constant<int, 32>());
 }
 
 constexpr uint32_t kNormLongParts = 64;
@@ -541,29 +572,25 @@ int pilc_norm_backward(const pilc_norm_shape *shape, const void *dy_dev, const v
     return by_types(shape->dtype, shape->weight_type, [&](auto *t, auto *w) {
         using T = std::remove_pointer_t<decltype(t)>;
         using W = std::remove_pointer_t<decltype(w)>;
-        const bool done = norm_row(a.width, [&](auto lanes, auto each) {
-            using Row = NormRow<T, W, decltype(lanes)::value, decltype(each)::value>;
-            a.num_parts = norm_blocks<Row>(a.rows, kNormBackwardWaves);
-            if (a.rows)
-                k_norm_backward_rows<T, W, decltype(lanes)::value, decltype(each)::value><<<a.num_parts, Row::kThreads, 0, stream>>>(a);
-        });
-        if (!done) {
-            a.num_parts = std::min(a.rows, kNormLongParts);
-            const bool narrow = a.width < 8;
-            const uint32_t each = kNormThreads * (narrow ? 1 : 16 / sizeof(T));
-            const dim3 grid((a.width + each - 1) / each, a.num_parts);
-            if (a.parts && a.rows) {
-                if (narrow)
-                    k_norm_parts<T, 1><<<grid, kNormThreads, 0, stream>>>(a);
-                else
-                    k_norm_parts<T, 16 / sizeof(T)><<<grid, kNormThreads, 0, stream>>>(a);
-            }
-            if (a.dx && a.rows) {
-                if (narrow)
-                    k_norm_dx_narrow<T, W><<<narrow_blocks(a.rows), kNormThreads, 0, stream>>>(a);
-                else
-                    k_norm_dx_long<T, W><<<std::min(a.rows, 1u << 20), kNormLongThreads, 0, stream>>>(a);
-            }
+        const auto parts = [&](uint32_t most) {
+            a.num_parts = std::min(a.rows, most);
+            const uint32_t each = kNormThreads * 16 / sizeof(T);
+            if (a.parts && a.rows)
+                k_norm_parts<T><<<dim3((a.width + each - 1) / each, a.num_parts), kNormThreads, 0, stream>>>(a);  // before dx, which may take dy's place
+        };
+        if (a.width < 8) {
+            a.num_parts = std::min(narrow_blocks(a.rows), compute_units());
+            if (a.rows) k_norm_backward_narrow<T, W><<<a.num_parts, kNormThreads, 0, stream>>>(a);
+        } else if (!norm_row(a.width, [&](auto lanes, auto each) {
+                       using Row = NormRow<T, W, decltype(lanes)::value, decltype(each)::value>;
+                       if (!Row::kKeep) parts(kNormLongParts);
+                       if (Row::kKeep) a.num_parts = norm_blocks<Row>(a.rows, kNormBackwardWaves);
+                       if (a.rows && (Row::kKeep || a.dx))
+                           k_norm_backward_rows<T, W, decltype(lanes)::value, decltype(each)::value>
+                               <<<norm_blocks<Row>(a.rows, kNormBackwardWaves), Row::kThreads, 0, stream>>>(a);
+                   })) {
+            parts(kNormLongParts);
+            if (a.dx && a.rows) k_norm_dx_long<T, W><<<std::min(a.rows, 1u << 20), kNormLongThreads, 0, stream>>>(a);
         }
         if (a.parts) k_norm_join<W><<<dim3((a.width + 63) / 64, 2), 1024, 0, stream>>>(a);
     });
