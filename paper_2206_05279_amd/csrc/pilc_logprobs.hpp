@@ -126,6 +126,9 @@ __device__ __forceinline__ void meet()
     }
 }
 
+// By what is done with a row (see Task).
+constexpr int kWavesOf[] = {6, 5, 6};
+
 // A row, or a run of it, in registers: kLanes lanes hold kPer packs of 16 bytes each.  A pack that would reach over the
 // end begins earlier, and what another holds of it already is ruled out.  Rows need a pack's values at least.
 template <class T, int kLanes, int kPer>
@@ -137,7 +140,7 @@ struct LogitsRow {
     static constexpr bool kAhead = kPer <= 4;  // the next run is asked for early; larger ones have the other workgroups beside them
     static constexpr uint32_t kValues = kLanes * kPer * kVec;
     // Wavefronts a SIMD that registers are kept down to where the next run is asked for early: so many are launched.
-    static constexpr int waves(bool train) { return kAhead ? (train ? 6 : 5) : kThreads / 256; }
+    static constexpr int waves(int task) { return kAhead ? kWavesOf[task] : kThreads / 256; }
 
     uint32_t lane, row_in_block;
 
@@ -361,15 +364,18 @@ __device__ __forceinline__ void put_gradient(const Raw<T> &x, T *grad, uint32_t 
     }
 }
 
-// Rows, or runs of rows, one after another; a row that is one run is finished here.  kTrain: whole rows, and their
-// gradient from the same registers.
-template <class T, int kLanes, int kPer, bool kTrain>
-__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::waves(kTrain))) void k_logits(LogitsArgs a)
+// What k_logits does: the rows' laws, alternatives too, or (whole rows) their gradient from the same registers.
+enum Task { kLaw, kPick, kTrainRows };
+
+// Rows, or runs of rows, one after another; a row that is one run is finished here.
+template <class T, int kLanes, int kPer, Task kTask>
+__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::waves(kTask))) void k_logits(LogitsArgs a)
 {
     using Row = LogitsRow<T, kLanes, kPer>;
     constexpr int kVec = Row::kVec;
+    constexpr bool kTrain = kTask == kTrainRows;
     __shared__ Tally room[2 * Row::kWaves];
-    constexpr bool kPicks = !kTrain && kLanes >= 64;
+    constexpr bool kPicks = kTask == kPick && kLanes >= 64;
     constexpr int kPickers = kPicks ? kLanes : 64;
     __shared__ PickRoom<kPickers> picked[kPicks ? Row::kRows : 1];
     const Row r;
@@ -442,18 +448,17 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
             }
         }
         if constexpr (kPicks) {
-            if (a.top)
-                pick_top<kLanes>(
-                    a.top, kOrderBits<T>, order_of(own), [&](uint32_t line, auto &to) { return r.collect(x, of, begin, end, used, line, to); },
-                    [&](auto f) { r.again((const T *)a.x + row * a.stride, begin, end, f); },
-                    [&](uint32_t place, uint64_t key) {
-                        if (whole)
-                            put_alternative(a, law, row, place, key);
-                        else
-                            a.part_top[item * a.top + place] = key;
-                    },
-                    picked[r.row_in_block]);
-        } else if constexpr (!kTrain) {
+            pick_top<kLanes>(
+                a.top, kOrderBits<T>, order_of(own), [&](uint32_t line, auto &to) { return r.collect(x, of, begin, end, used, line, to); },
+                [&](auto f) { r.again((const T *)a.x + row * a.stride, begin, end, f); },
+                [&](uint32_t place, uint64_t key) {
+                    if (whole)
+                        put_alternative(a, law, row, place, key);
+                    else
+                        a.part_top[item * a.top + place] = key;
+                },
+                picked[r.row_in_block]);
+        } else if constexpr (kTask == kPick) {
             // few values a lane, in whole rows: the best that is worse than the last, `top` times
             uint64_t below = ~0ull;
             for (uint32_t i = 0; i < a.top; ++i) {
@@ -696,7 +701,7 @@ static size_t logits_workspace(const pilc_logits_shape &s)
 // Calls `go` with the lanes and packs a lane for runs of `bytes` bytes.  Alternatives of short rows are looked for by a whole
 // wavefront where twice as many of its lanes as alternatives have values (65536 x 256 f32, 20 alternatives: 109 us in
 // groups of 16 lanes, 59 by 64).
-template <bool kWholeRows, class Go>
+template <Task kTask, class Go>
 static void logits_row(uint32_t bytes, uint32_t top, Go go)
 {
     using std::integral_constant;
@@ -710,13 +715,14 @@ static void logits_row(uint32_t bytes, uint32_t top, Go go)
     const integral_constant<int, 4> four;
     const integral_constant<int, 8> eight;
     const integral_constant<int, 16> sixteen;
+    const integral_constant<int, 64> wave;
     const integral_constant<int, 256> group;
-    if constexpr (!kWholeRows)
-        if (top && bytes >= 32 * top && (with(integral_constant<int, 64>(), one) || with(integral_constant<int, 64>(), two))) return;
+    if constexpr (kTask == kPick)
+        if (bytes >= 32 * top && (with(wave, one) || with(wave, two))) return;
     const bool done = with(integral_constant<int, 8>(), one) || with(integral_constant<int, 8>(), four) || with(integral_constant<int, 16>(), four) ||
-                      with(integral_constant<int, 32>(), four) || with(integral_constant<int, 64>(), four) || with(group, two) || with(group, four) ||
-                      with(group, eight) || with(group, sixteen);
-    if constexpr (kWholeRows)
+                      with(integral_constant<int, 32>(), four) || with(wave, four) || with(group, two) || with(group, four) || with(group, eight) ||
+                      with(group, sixteen);
+    if constexpr (kTask == kTrainRows)
         if (!done) (void)(with(integral_constant<int, 1024>(), eight) || with(integral_constant<int, 1024>(), sixteen));
 }
 
@@ -728,17 +734,17 @@ static uint32_t logits_blocks(uint64_t items, uint32_t rows, uint32_t threads, u
     return (uint32_t)std::min<uint64_t>(all, waves ? compute_units() * (waves * 256 / threads) : (1u << 21));
 }
 
-template <class T, bool kTrain>
+template <class T, Task kTask>
 static void launch_logits(const LogitsArgs &a, hipStream_t stream)
 {
     if (a.num_sym < 16 / sizeof(T)) {
-        k_logits_short<T, kTrain, false><<<(uint32_t)std::min<uint64_t>((a.rows + 255ull) / 256, 1u << 20), 256, 0, stream>>>(a);
+        k_logits_short<T, kTask == kTrainRows, false><<<(uint32_t)std::min<uint64_t>((a.rows + 255ull) / 256, 1u << 20), 256, 0, stream>>>(a);
         return;
     }
-    logits_row<kTrain>(a.span * (uint32_t)sizeof(T), a.top, [&](auto lanes, auto per) {
+    logits_row<kTask>(a.span * (uint32_t)sizeof(T), a.top, [&](auto lanes, auto per) {
         using Row = LogitsRow<T, decltype(lanes)::value, decltype(per)::value>;
-        const uint32_t blocks = logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, Row::kAhead ? Row::waves(kTrain) : 0);
-        k_logits<T, decltype(lanes)::value, decltype(per)::value, kTrain><<<blocks, Row::kThreads, 0, stream>>>(a);
+        const uint32_t blocks = logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, Row::kAhead ? Row::waves(kTask) : 0);
+        k_logits<T, decltype(lanes)::value, decltype(per)::value, kTask><<<blocks, Row::kThreads, 0, stream>>>(a);
     });
 }
 
@@ -750,7 +756,10 @@ static void launch_law(LogitsArgs a, uint32_t type, void *workspace, hipStream_t
     a.splits = p.splits, a.span = std::min(p.span, a.num_sym);
     a.part = (float4 *)workspace;
     a.part_top = (uint64_t *)(a.part + (size_t)a.rows * a.splits);
-    launch_logits<T, false>(a, stream);
+    if (a.top)
+        launch_logits<T, kPick>(a, stream);
+    else
+        launch_logits<T, kLaw>(a, stream);
     if (a.splits == 1) return;
     if (a.splits > 16)  // few rows: a workgroup each
         k_logits_join<256><<<std::min(a.rows, 1u << 20), 256, 0, stream>>>(a, type);
@@ -867,7 +876,7 @@ int pilc_logprobs_train(const pilc_logits_shape *shape, const void *logits_dev, 
         using T = std::remove_pointer_t<decltype(t)>;
         if (train_by_row(a.rows, a.num_sym, sizeof(T))) {
             a.splits = 1, a.span = a.num_sym;
-            launch_logits<T, true>(a, stream);
+            launch_logits<T, kTrainRows>(a, stream);
             return;
         }
         // too few rows to keep the GPU busy one a workgroup, or too long ones: the law first, then the gradient by it
