@@ -126,9 +126,6 @@ __device__ __forceinline__ void meet()
     }
 }
 
-// By what is done with a row (see Task).
-constexpr int kWavesOf[] = {6, 5, 6};
-
 // A row, or a run of it, in registers: kLanes lanes hold kPer packs of 16 bytes each.  A pack that would reach over the
 // end begins earlier, and what another holds of it already is ruled out.  Rows need a pack's values at least.
 template <class T, int kLanes, int kPer>
@@ -137,10 +134,10 @@ struct LogitsRow {
     static constexpr int kThreads = kLanes > 256 ? kLanes : 256;
     static constexpr int kRows = kThreads / kLanes;  // that a workgroup has in hand
     static constexpr int kWithin = kLanes < 64 ? kLanes : 64, kWaves = kLanes > 64 ? kLanes / 64 : 1;
-    static constexpr bool kAhead = kPer <= 4;  // the next run is asked for early; larger ones have the other workgroups beside them
     static constexpr uint32_t kValues = kLanes * kPer * kVec;
-    // Wavefronts a SIMD that registers are kept down to where the next run is asked for early: so many are launched.
-    static constexpr int waves(int task) { return kAhead ? kWavesOf[task] : kThreads / 256; }
+    // Wavefronts a SIMD that registers are kept down to: with two of 16 packs a lane, as the compiler would have it, 16384 x
+    // 32768 bf16 with 20 alternatives takes 280 us, with three 215.
+    static constexpr int kResident = kLanes == 1024 ? 4 : kPer == 16 ? 3 : kPer == 8 ? 5 : 1;
 
     uint32_t lane, row_in_block;
 
@@ -369,7 +366,7 @@ enum Task { kLaw, kPick, kTrainRows };
 
 // Rows, or runs of rows, one after another; a row that is one run is finished here.
 template <class T, int kLanes, int kPer, Task kTask>
-__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::waves(kTask))) void k_logits(LogitsArgs a)
+__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::kResident)) void k_logits(LogitsArgs a)
 {
     using Row = LogitsRow<T, kLanes, kPer>;
     constexpr int kVec = Row::kVec;
@@ -381,32 +378,16 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
     const Row r;
     const uint64_t items = (uint64_t)a.rows * a.splits, step = (uint64_t)gridDim.x * Row::kRows;
     uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block;
-    Raw<T> x[kPer], next[kPer];
-    // what comes with a row is asked for before its values: loads come back in order
-    struct Given {
-        int64_t t;
-        float up, up_entropy;
-    } given = {-1, 0.0f, 0.0f}, next_given = given;
     int half = 0;
-    const auto fetch = [&](uint64_t i, Given &to, Raw<T>(&to_x)[kPer]) {
-        i = min(i, items - 1);
-        const uint32_t row = (uint32_t)(a.splits == 1 ? i : i / a.splits), begin = (uint32_t)(i - (uint64_t)row * a.splits) * a.span;
-        if (a.target && (kTrain || a.splits == 1)) to.t = target_of(a, row);
-        if (kTrain) {
-            to.up = a.up_logp[row];
-            if (a.up_entropy) to.up_entropy = a.up_entropy[row];
-        }
-        r.load((const T *)a.x + row * a.stride, begin, min(begin + a.span, a.num_sym), to_x);
-    };
-    if (Row::kAhead) fetch(item, given, x);
     for (; item < items; item += step) {
-        if (Row::kAhead)
-            fetch(item + step, next_given, next);
-        else
-            fetch(item, given, x);
         const uint32_t row = (uint32_t)(a.splits == 1 ? item : item / a.splits), begin = (uint32_t)(item - (uint64_t)row * a.splits) * a.span;
+        const bool whole = kTrain || a.splits == 1;
+        // what comes with a row is asked for before its values: loads come back in order
+        const int64_t t = a.target && whole ? target_of(a, row) : -1;
+        const float up_given = kTrain ? a.up_logp[row] : 0.0f, up_entropy = kTrain && a.up_entropy ? a.up_entropy[row] : 0.0f;
+        Raw<T> x[kPer];
         const uint32_t end = min(begin + a.span, a.num_sym);
-        const int64_t t = given.t;
+        r.load((const T *)a.x + row * a.stride, begin, end, x);
         r.rule_out(begin, end, x);
         const int used = r.used(begin, end);
         float of[kPer];
@@ -415,7 +396,6 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         const Tally tally = r.tally(x, used, own, room, half);
         r.forget(x);
         half ^= 1;
-        const bool whole = kTrain || a.splits == 1;
         const Law law(tally);
         if (!whole) {
             if (r.lane == 0) a.part[item] = make_float4(tally.max, tally.total, tally.inside, 0.0f);
@@ -435,7 +415,7 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
                     }
                 }
             if constexpr (kTrain) {
-                const float up = t < 0 ? 0.0f : given.up, up_entropy = given.up_entropy;
+                const float up = t < 0 ? 0.0f : up_given;
                 // grad = e (from + slope z), ln p being ln 2 z - ln total
                 const Scale scale(tally.max);
                 float from = -(up + up_entropy * (law.entropy - logf(law.total))) / law.total, slope = -up_entropy * kLn2 / law.total;
@@ -472,11 +452,6 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
                 below = (uint64_t)high << 32 | low;
                 if (r.lane == 0) put_alternative(a, law, row, i, below);
             }
-        }
-        if (Row::kAhead) {
-            given = next_given;
-#pragma unroll
-            for (int q = 0; q < kPer; ++q) x[q] = next[q];
         }
     }
 }
@@ -701,8 +676,11 @@ static size_t logits_workspace(const pilc_logits_shape &s)
 // Calls `go` with the lanes and packs a lane for runs of `bytes` bytes.  Alternatives of short rows are looked for by a whole
 // wavefront where twice as many of its lanes as alternatives have values (65536 x 256 f32, 20 alternatives: 109 us in
 // groups of 16 lanes, 59 by 64).
+//
+// Whole rows of up to 16 KB are a wavefront's by itself, which has no other to wait for (16384 x 4096 bf16: 26 us, by
+// workgroups 38; 30000 x 3000 f32: 61 and 73); runs of a split row, of which there are few, a workgroup's.
 template <Task kTask, class Go>
-static void logits_row(uint32_t bytes, uint32_t top, Go go)
+static void logits_row(uint32_t bytes, uint32_t top, bool whole, Go go)
 {
     using std::integral_constant;
     const auto with = [&](auto lanes, auto per) {
@@ -720,19 +698,15 @@ static void logits_row(uint32_t bytes, uint32_t top, Go go)
     if constexpr (kTask == kPick)
         if (bytes >= 32 * top && (with(wave, one) || with(wave, two))) return;
     const bool done = with(integral_constant<int, 8>(), one) || with(integral_constant<int, 8>(), four) || with(integral_constant<int, 16>(), four) ||
-                      with(integral_constant<int, 32>(), four) || with(wave, four) || with(group, two) || with(group, four) || with(group, eight) ||
-                      with(group, sixteen);
+                      with(integral_constant<int, 32>(), four) || with(wave, four) || (whole && (with(wave, eight) || with(wave, sixteen))) ||
+                      with(group, two) || with(group, four) || with(group, eight) || with(group, sixteen);
     if constexpr (kTask == kTrainRows)
         if (!done) (void)(with(integral_constant<int, 1024>(), eight) || with(integral_constant<int, 1024>(), sixteen));
 }
 
-// Workgroups for `items` rows or runs of which each takes `rows` at a time: one for each, or with `waves` as many as that
-// many wavefronts a SIMD are, which go from one to the next.
-static uint32_t logits_blocks(uint64_t items, uint32_t rows, uint32_t threads, uint32_t waves)
-{
-    const uint64_t all = (items + rows - 1) / rows;
-    return (uint32_t)std::min<uint64_t>(all, waves ? compute_units() * (waves * 256 / threads) : (1u << 21));
-}
+// A workgroup for each `rows` of the rows or runs: what one asks for early is no gain over what the others ask for
+// beside it (65536 x 256 bf16, training: 17.6 us, with workgroups that go from row to row, the next one on its way, 19.1).
+static uint32_t logits_blocks(uint64_t items, uint32_t rows) { return (uint32_t)std::min<uint64_t>((items + rows - 1) / rows, 1u << 21); }
 
 template <class T, Task kTask>
 static void launch_logits(const LogitsArgs &a, hipStream_t stream)
@@ -741,9 +715,9 @@ static void launch_logits(const LogitsArgs &a, hipStream_t stream)
         k_logits_short<T, kTask == kTrainRows, false><<<(uint32_t)std::min<uint64_t>((a.rows + 255ull) / 256, 1u << 20), 256, 0, stream>>>(a);
         return;
     }
-    logits_row<kTask>(a.span * (uint32_t)sizeof(T), a.top, [&](auto lanes, auto per) {
+    logits_row<kTask>(a.span * (uint32_t)sizeof(T), a.top, a.splits == 1, [&](auto lanes, auto per) {
         using Row = LogitsRow<T, decltype(lanes)::value, decltype(per)::value>;
-        const uint32_t blocks = logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, Row::kAhead ? Row::waves(kTask) : 0);
+        const uint32_t blocks = logits_blocks((uint64_t)a.rows * a.splits, Row::kRows);
         k_logits<T, decltype(lanes)::value, decltype(per)::value, kTask><<<blocks, Row::kThreads, 0, stream>>>(a);
     });
 }
@@ -782,7 +756,7 @@ static void launch_grad(LogitsArgs a, hipStream_t stream)
         using Row = LogitsRow<T, decltype(lanes)::value, decltype(per)::value>;
         if (a.span > Row::kValues) return false;
         k_logits_grad<T, decltype(lanes)::value, decltype(per)::value>
-            <<<logits_blocks((uint64_t)a.rows * a.splits, Row::kRows, Row::kThreads, 0), Row::kThreads, 0, stream>>>(a);
+            <<<logits_blocks((uint64_t)a.rows * a.splits, Row::kRows), Row::kThreads, 0, stream>>>(a);
         return true;
     };
     (void)(with(integral_constant<int, 8>(), integral_constant<int, 1>()) || with(integral_constant<int, 8>(), integral_constant<int, 4>()) ||
