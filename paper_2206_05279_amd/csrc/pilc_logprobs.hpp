@@ -148,10 +148,19 @@ struct LogitsRow {
     {
         return (int)min(place(q, begin) - column(q, begin, end), (uint32_t)kVec);
     }
+    // Where column `column` of a row at p is, by way of the run's first place: the same for a workgroup's lanes, and what
+    // is added to it fits 32 bits, so that a pack's address takes one register.
+    template <class V>
+    __device__ static V *address(V *p, uint32_t column, uint32_t begin, uint32_t end)
+    {
+        const uint32_t first = min(begin, end - kVec);
+        using Byte = std::conditional_t<std::is_const_v<V>, const char, char>;
+        return (V *)((Byte *)(p + first) + (uint32_t)((column - first) * (uint32_t)sizeof(T)));
+    }
     __device__ void load(const T *p, uint32_t begin, uint32_t end, Raw<T> (&x)[kPer]) const
     {
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) x[q] = Raw<T>::load(p + column(q, begin, end));
+        for (int q = 0; q < kPer; ++q) x[q] = Raw<T>::load(address(p, column(q, begin, end), begin, end));
     }
     // Packs that are gone through, for all lanes the same: those with values of the row in them, up to a whole group.  The others are loaded, with the row's last values, and left alone.
     static constexpr int kGroup = kLanes == 1024 ? 2 : kPer < 4 ? kPer : 4;
@@ -176,8 +185,10 @@ struct LogitsRow {
             for (int q = 0; q < kPer; ++q)
                 if (q >= whole) x[q].rule_out(twice(q, begin, end));
     }
-    __device__ static void forget(Raw<T> (&x)[kPer])
+    // Neither what the values were widened to nor where the packs lie is kept for after: worked out again it takes no registers.
+    __device__ void forget(Raw<T> (&x)[kPer])
     {
+        asm volatile("" : "+v"(lane));
 #pragma unroll
         for (int q = 0; q < kPer; ++q) x[q].forget();
     }
@@ -333,9 +344,10 @@ __device__ __forceinline__ void put_alternative(const LogitsArgs &a, const Law &
     a.top_logp[at] = none ? __builtin_nanf("") : key ? law.logp(value_of(key)) : -kInf;
 }
 
-// The gradient of one pack's values: 2^z (from + slope z), and `up` more at the target.
+// The gradient of one pack's values, the first of which is that of symbol `column` and goes to `to`: 2^z (from + slope z), and
+// `up` more at the target.
 template <class T>
-__device__ __forceinline__ void put_gradient(const Raw<T> &x, T *grad, uint32_t column, int twice, const Scale &scale, float from, float slope,
+__device__ __forceinline__ void put_gradient(const Raw<T> &x, T *to, uint32_t column, int twice, const Scale &scale, float from, float slope,
                                              bool in, int64_t t, float up, bool zeros)
 {
     constexpr int kVec = 16 / sizeof(T);
@@ -353,11 +365,11 @@ __device__ __forceinline__ void put_gradient(const Raw<T> &x, T *grad, uint32_t 
 #pragma unroll
         for (int i = 0; i < kVec; ++i) d[i] = 0.0f;
     if (twice == 0) {
-        Raw<T>::of(d).store(grad + column);
+        Raw<T>::of(d).store(to);
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
-            if (i >= twice) grad[column + i] = (T)d[i];
+            if (i >= twice) to[i] = (T)d[i];
     }
 }
 
@@ -375,7 +387,7 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
     constexpr bool kPicks = kTask == kPick && kLanes >= 64;
     constexpr int kPickers = kPicks ? kLanes : 64;
     __shared__ PickRoom<kPickers> picked[kPicks ? Row::kRows : 1];
-    const Row r;
+    Row r;
     const uint64_t items = (uint64_t)a.rows * a.splits, step = (uint64_t)gridDim.x * Row::kRows;
     uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block;
     int half = 0;
@@ -422,8 +434,10 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
                 const bool zeros = (up == 0.0f && up_entropy == 0.0f) || law.max == -kInf;
                 if (t >= (int64_t)a.num_sym || !(law.max == law.max)) from = __builtin_nanf("");
                 T *grad = (T *)a.grad + row * a.grad_stride;
+                r.forget(x);
                 r.for_used(used, [&](int q) {
-                    put_gradient(x[q], grad, r.column(q, begin, end), r.twice(q, begin, end), scale, from, slope, in, t, up, zeros);
+                    const uint32_t column = r.column(q, begin, end);
+                    put_gradient(x[q], Row::address(grad, column, begin, end), column, r.twice(q, begin, end), scale, from, slope, in, t, up, zeros);
                 });
             }
         }
@@ -549,8 +563,10 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logi
         T *grad = (T *)a.grad + row * a.grad_stride;
         const bool in = t >= 0 && t < (int64_t)a.num_sym;
 #pragma unroll
-        for (int q = 0; q < kPer; ++q)
-            put_gradient(x[q], grad, r.column(q, begin, end), r.twice(q, begin, end), scale, from, slope, in, t, up, zeros);
+        for (int q = 0; q < kPer; ++q) {
+            const uint32_t column = r.column(q, begin, end);
+            put_gradient(x[q], Row::address(grad, column, begin, end), column, r.twice(q, begin, end), scale, from, slope, in, t, up, zeros);
+        }
     }
 }
 
