@@ -465,6 +465,10 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
                 const uint32_t high = lanes_reduce<Row::kWithin>((uint32_t)(best >> 32), Max());
                 const uint32_t low = lanes_reduce<Row::kWithin>(best >> 32 == high ? (uint32_t)best : 0u, Max());
                 below = (uint64_t)high << 32 | low;
+                if (below == 0) {  // no more
+                    for (uint32_t j = i + r.lane; j < a.top; j += kLanes) put_alternative(a, law, row, j, 0);
+                    break;
+                }
                 if (r.lane == 0) put_alternative(a, law, row, i, below);
             }
         }
@@ -609,7 +613,7 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitsArgs a)
             uint64_t below = ~0ull;
             for (uint32_t k = 0; k < a.top; ++k) {
                 uint64_t best = 0;
-                for (uint32_t j = 0; j < a.num_sym; ++j) {
+                for (uint32_t j = 0; j < a.num_sym && k < a.num_sym; ++j) {
                     const uint64_t key = key_of(widen(x[j]), j);
                     if (key >> 32 > kOrderNone && key < below && key > best) best = key;
                 }
