@@ -263,7 +263,7 @@ struct LogitsRow {
         Tally t = {max, lanes_reduce<kWithin>(total[0] + total[1], Sum()), lanes_reduce<kWithin>(inside[0] + inside[1], Sum())};
         if constexpr (kWaves > 1) {
             room += half * kWaves;
-            if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = t;
+            if ((threadIdx.x & 63) == 0) room[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)] = t;
             __syncthreads();
             t = room[threadIdx.x & (kWaves - 1)];
 #pragma unroll
@@ -389,12 +389,13 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
     constexpr int kPickers = kPicks ? kLanes : 64;
     __shared__ PickRoom<kPickers> picked[kPicks ? Row::kRows : 1];
     Row r;
-    const uint64_t items = (uint64_t)a.rows * a.splits, step = (uint64_t)gridDim.x * Row::kRows;
+    const uint32_t splits = kTrain ? 1 : a.splits;
+    const uint64_t items = (uint64_t)a.rows * splits, step = (uint64_t)gridDim.x * Row::kRows;
     uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block;
     int half = 0;
     for (; item < items; item += step) {
-        const uint32_t row = (uint32_t)(a.splits == 1 ? item : item / a.splits), begin = (uint32_t)(item - (uint64_t)row * a.splits) * a.span;
-        const bool whole = kTrain || a.splits == 1;
+        const uint32_t row = (uint32_t)(splits == 1 ? item : item / splits), begin = (uint32_t)(item - (uint64_t)row * splits) * a.span;
+        const bool whole = splits == 1;
         // what comes with a row is asked for before its values: loads come back in order
         const int64_t t = a.target && whole ? target_of(a, row) : -1;
         const float up_given = kTrain ? a.up_logp[row] : 0.0f, up_entropy = kTrain && a.up_entropy ? a.up_entropy[row] : 0.0f;
