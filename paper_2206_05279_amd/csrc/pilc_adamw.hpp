@@ -24,7 +24,7 @@ struct AdamwArgs {
     uint32_t block[kAdamwTensors];      // blocks of 256 of the launch's tensors before this one
     uint64_t first_block;               // and of those before the launch's
     float b1, b1_rest, b2, b2_rest, grad_scale, root_scale, eps;
-    uint32_t dither, num, chunk;        // values a workgroup takes
+    uint32_t dither, num;
 };
 static_assert(sizeof(AdamwArgs) <= 4096, "what a launch may carry");
 
@@ -104,42 +104,41 @@ __device__ __forceinline__ uint32_t tensor_of(const AdamwArgs &a, uint32_t chunk
 }
 
 constexpr int kAdamwThreads = 256;
-// Values a workgroup takes: this many, or with few values as many as its threads take at once, so that all of them
-// are on their way at the same time (24 tensors of 200,000 values: 10.4 against 5.2 us).
-constexpr uint32_t kAdamwChunk = 4096;
-constexpr uint64_t kAdamwFew = 1u << 21;
+// Values a thread takes, and it takes no more: what would follow in a loop is on its way earlier in another workgroup (150
+// million values f32 with states in 32 bits 787 us, in chunks of 4096 831; 300 million bf16 in 8 bits 564 and 632).
+constexpr int kAdamwEach = 4, kAdamwBytesEach = 8;
+constexpr uint32_t kAdamwChunk = kAdamwThreads * kAdamwEach, kAdamwBytesChunk = kAdamwThreads * kAdamwBytesEach;
 
-// States in 32 bits: four values a thread at a time.
+// States in 32 bits.  28 bytes a value in f32 and some thirty instructions: memory bounds it, at 5.3 TB/s (150 million
+// values in 291 tensors).
 template <class P, class G>
 __global__ __launch_bounds__(kAdamwThreads) void k_adamw(AdamwArgs a)
 {
-    constexpr int kEach = 4;
+    constexpr int kEach = kAdamwEach;
     const uint32_t k = __builtin_amdgcn_readfirstlane(tensor_of(a, blockIdx.x));
     const AdamwTensor &t = a.tensor[k];
-    const uint64_t begin = (uint64_t)(blockIdx.x - (k ? a.chunk_end[k - 1] : 0)) * a.chunk;
-    P *param = (P *)t.param + begin;
-    const G *grad = (const G *)t.grad + begin;
-    float *ms = (float *)t.m + begin, *vs = (float *)t.v + begin;
-    const uint32_t left = (uint32_t)min((uint64_t)a.chunk, t.count - begin);
-    const auto some = [&](uint32_t i, int valid) {
-        auto p = load_pack<kEach>(param + i, valid);
-        const auto g = load_pack<kEach>(grad + i, valid);
-        auto m = load_pack<kEach>(ms + i, valid), v = load_pack<kEach>(vs + i, valid);
+    const uint64_t begin = (uint64_t)(blockIdx.x - (k ? a.chunk_end[k - 1] : 0)) * kAdamwChunk, i = begin + threadIdx.x * kEach;
+    P *param = (P *)t.param + i;
+    const G *grad = (const G *)t.grad + i;
+    float *ms = (float *)t.m + i, *vs = (float *)t.v + i;
+    const auto step = [&](int valid) {
+        auto p = load_pack<kEach>(param, valid);
+        const auto g = load_pack<kEach>(grad, valid);
+        auto m = load_pack<kEach>(ms, valid), v = load_pack<kEach>(vs, valid);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             const Moments s = move_moments(a, {m.v[j], v.v[j]}, widen(g.v[j]));
             p.v[j] = (P)move_param(a, t, widen(p.v[j]), s);
             m.v[j] = s.m, v.v[j] = s.v;
         }
-        store_pack(param + i, valid, p);
-        store_pack(ms + i, valid, m);
-        store_pack(vs + i, valid, v);
+        store_pack(param, valid, p);
+        store_pack(ms, valid, m);
+        store_pack(vs, valid, v);
     };
-    if (left == a.chunk) {
-        for (uint32_t i = threadIdx.x * kEach; i < a.chunk; i += kAdamwThreads * kEach) some(i, kEach);
-    } else {
-        for (uint32_t i = threadIdx.x * kEach; i < left; i += kAdamwThreads * kEach) some(i, (int)(left - i));
-    }
+    if (t.count - begin >= kAdamwChunk)  // the same for all threads: their loads need not be told apart
+        step(kEach);
+    else if (i < t.count)
+        step((int)min((uint64_t)kEach, t.count - i));
 }
 
 // `valid` codes, four a word; 0 behind them.
@@ -157,31 +156,27 @@ __device__ __forceinline__ void store_codes(uint8_t *p, int valid, const uint32_
     store_pack(p, valid, t);
 }
 
-// States in 8 bits: eight values a thread, half a wavefront a block of 256.
+// States in 8 bits: half a wavefront a block of 256, whose largest values it finds among its lanes.  10 bytes a value in
+// bf16 and 69 vector instructions, a third of them for the random numbers and the coding: the vector units are busy 91 % of
+// the time, memory at 5.3 TB/s (300 million values: 564 us).
 template <class P, class G>
 __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
 {
-    constexpr int kEach = 8;
+    constexpr int kEach = kAdamwBytesEach;
     const uint32_t k = __builtin_amdgcn_readfirstlane(tensor_of(a, blockIdx.x));
     const AdamwTensor &t = a.tensor[k];
-    const uint32_t chunk = blockIdx.x - (k ? a.chunk_end[k - 1] : 0);
-    const uint64_t begin = (uint64_t)chunk * a.chunk;
-    P *param = (P *)t.param + begin;
-    const G *grad = (const G *)t.grad + begin;
-    uint8_t *ms = (uint8_t *)t.m + begin, *vs = (uint8_t *)t.v + begin;
-    uint8_t *m_scale = t.m_scale + begin / kStateBlock, *v_scale = t.v_scale + begin / kStateBlock;
-    // the number of the chunk's first value
-    const uint64_t number = (a.first_block + a.block[k]) * kStateBlock + begin;
-    const uint32_t left = (uint32_t)min((uint64_t)a.chunk, t.count - begin);
-    const auto some = [&](uint32_t i, int valid) {
-        const uint32_t b = i / kStateBlock;
-        auto p = load_pack<kEach>(param + i, valid);
-        const auto g = load_pack<kEach>(grad + i, valid);
+    const uint64_t begin = (uint64_t)(blockIdx.x - (k ? a.chunk_end[k - 1] : 0)) * kAdamwBytesChunk, i = begin + threadIdx.x * kEach;
+    P *param = (P *)t.param + i;
+    uint8_t *ms = (uint8_t *)t.m + i, *vs = (uint8_t *)t.v + i, *m_scale = t.m_scale + i / kStateBlock, *v_scale = t.v_scale + i / kStateBlock;
+    const G *grad = (const G *)t.grad + i;
+    const auto step = [&](int valid) {
+        auto p = load_pack<kEach>(param, valid);
+        const auto g = load_pack<kEach>(grad, valid);
         uint32_t mc[kEach / 4], vc[kEach / 4];
-        load_codes(ms + i, valid, mc);
-        load_codes(vs + i, valid, vc);
+        load_codes(ms, valid, mc);
+        load_codes(vs, valid, vc);
         float m[kEach], v[kEach];
-        const float m_unit = Coding<true>::scale_of(m_scale[b]), v_unit = Coding<false>::scale_of(v_scale[b]);
+        const float m_unit = Coding<true>::scale_of(*m_scale), v_unit = Coding<false>::scale_of(*v_scale);
         uint32_t m_most = 0, v_most = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
@@ -193,36 +188,32 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
             m_most = max(m_most, __float_as_uint(s.m) & 0x7FFFFFFFu);
             v_most = max(v_most, __float_as_uint(s.v));
         }
-        store_pack(param + i, valid, p);
-        // the block is half a wavefront's; the other half may be in another block, but not outside the loop
-#pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) {
-            m_most = max(m_most, (uint32_t)__shfl_xor((int)m_most, d, 64));
-            v_most = max(v_most, (uint32_t)__shfl_xor((int)v_most, d, 64));
-        }
+        store_pack(param, valid, p);
+        m_most = lanes_reduce<32>(m_most, Max());
+        v_most = lanes_reduce<32>(v_most, Max());
         const uint32_t em = max(1u, m_most >> 23), ev = max(1u, v_most >> 23 & 255);  // a NaN may have its sign set
         const float m_inverse = Coding<true>::inverse_of(em), v_inverse = Coding<false>::inverse_of(ev);
+        const uint64_t number = (a.first_block + a.block[k]) * kStateBlock + i;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             if (j % 4 == 0) mc[j / 4] = vc[j / 4] = 0;
-            const uint32_t h = hash_of(number + i + j, a.dither);
+            const uint32_t h = hash_of(number + j, a.dither);
             mc[j / 4] |= (Coding<true>::encode(m[j], m_inverse, h & 0xFFFF) & 255) << (8 * (j & 3));
             vc[j / 4] |= (Coding<false>::encode(v[j], v_inverse, h >> 16) & 255) << (8 * (j & 3));
         }
-        store_codes(ms + i, valid, mc);
-        store_codes(vs + i, valid, vc);
-        if (i % kStateBlock == 0) m_scale[b] = (uint8_t)em, v_scale[b] = (uint8_t)ev;
+        store_codes(ms, valid, mc);
+        store_codes(vs, valid, vc);
+        if (i % kStateBlock == 0) *m_scale = (uint8_t)em, *v_scale = (uint8_t)ev;
     };
-    if (left == a.chunk) {
-        for (uint32_t i = threadIdx.x * kEach; i < a.chunk; i += kAdamwThreads * kEach) some(i, kEach);
-    } else {
-        const uint32_t end = (left + kStateBlock - 1) / kStateBlock * kStateBlock;  // whole halves of wavefronts
-        for (uint32_t i = threadIdx.x * kEach; i < end; i += kAdamwThreads * kEach) some(i, (int)left - (int)i);
-    }
+    if (t.count - begin >= kAdamwBytesChunk)  // the same for all threads: their loads need not be told apart
+        step(kEach);
+    else if (i / kStateBlock * kStateBlock < t.count)  // whole halves of wavefronts
+        step(i < t.count ? (int)min((uint64_t)kEach, t.count - i) : 0);
 }
 
 // Thirty-two values a thread, four at a time, all codes asked for before the first value is written: a byte read
-// makes four written, so that reads of four bytes a lane leave too few bytes on their way if one waits for the other.
+// makes four written, so that reads of four bytes a lane leave too few bytes on their way if one waits for the other (300
+// million values: 251 us, 6.0 TB/s; four values a thread 370).
 constexpr int kValuesParts = 8;
 constexpr uint32_t kValuesChunk = 256 * 4 * kValuesParts;
 template <bool kSigned>
@@ -291,9 +282,8 @@ int pilc_adamw_step(const pilc_adamw_params *params_host, const pilc_adamw_tenso
     a.grad_scale = (float)h.grad_scale, a.eps = (float)h.eps, a.dither = h.dither;
     const double c1 = 1.0 - std::pow(h.beta1, (double)h.step), c2 = 1.0 - std::pow(h.beta2, (double)h.step);
     a.root_scale = (float)(1.0 / std::sqrt(c2));
-    uint64_t blocks = 0, values = 0;
-    for (uint32_t k = 0; k < num_tensors; ++k) values += tensors_host[k].count;
-    a.chunk = values > kAdamwFew ? kAdamwChunk : kAdamwThreads * (h.state_bits == 32 ? 4 : 8);
+    uint64_t blocks = 0;
+    const uint32_t chunk = h.state_bits == 32 ? kAdamwChunk : kAdamwBytesChunk;
     uint32_t chunks = 0;
     const auto launch = [&]() -> int {
         if (a.num == 0) return PILC_OK;
@@ -314,8 +304,8 @@ int pilc_adamw_step(const pilc_adamw_params *params_host, const pilc_adamw_tenso
         pilc_adamw_tensor x = tensors_host[k];
         const double lr = h.lr * x.lr_mult;
         while (x.count) {  // a tensor of more chunks than a launch has room for goes on in the next
-            const uint64_t room = kAdamwMostChunks - chunks, wanted = ceil_div(x.count, a.chunk);
-            const uint64_t here = std::min(room, wanted), count = here < wanted ? here * a.chunk : x.count;
+            const uint64_t room = kAdamwMostChunks - chunks, wanted = ceil_div(x.count, chunk);
+            const uint64_t here = std::min(room, wanted), count = here < wanted ? here * chunk : x.count;
             AdamwTensor &t = a.tensor[a.num];
             t = {x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, count, (float)(1.0 - lr * x.decay), (float)(lr / c1)};
             a.block[a.num] = (uint32_t)(blocks - a.first_block);

@@ -3,8 +3,13 @@
 
 namespace pilc {
 
-constexpr int kMaxTop = 32;
+// Per row of logits x: M = max x, S = sum of e^(x - M), U = sum of (x - M) e^(x - M); lse = M + ln S, ln p of symbol t = x_t - lse,
+// entropy = ln S - U / S, and the gradient of a logp + b entropy is a (1[j = t] - p_j) - b p_j (ln p_j + entropy).  A value
+// takes some ten instructions, four of their issue slots for the power of two, and two or four bytes: memory and the vector
+// units bound the kernels about alike in 16 bits, memory in 32.  So a value is read once, into registers, and gone through
+// there: for M, for S and U, for the alternatives, for the gradient.
 
+constexpr int kMaxTop = 32;
 
 struct LogitsArgs {
     const void *x;
@@ -102,8 +107,8 @@ struct Law {
 template <int kThreads>
 struct PickRoom {
     static constexpr uint32_t kMost = kThreads < 256 ? 128 : 256;
-    uint32_t best[kThreads];
     static constexpr uint32_t kMostPacks = kThreads < 256 ? 64 : 192;
+    uint32_t best[kThreads];
     uint64_t picked[kMost], rounds[kThreads / 64];
     u32x4_t pack[kMostPacks];
     uint32_t column[kMostPacks];
@@ -377,7 +382,9 @@ __device__ __forceinline__ void put_gradient(const Raw<T> &x, T *to, uint32_t co
 // What k_logits does: the rows' laws, alternatives too, or (whole rows) their gradient from the same registers.
 enum Task { kLaw, kPick, kTrainRows };
 
-// Rows, or runs of rows, one after another; a row that is one run is finished here.
+// A row, or a run of one, a workgroup or a part of it; a row that is one run is finished here.  Measured (whole calls):
+// laws of 16384 x 32768 bf16 192 us (5.6 TB/s), of 65536 x 256 f32 12.6 (5.4); with alternatives 4093 x 100003 bf16 177 (4.6,
+// with the joining kernel); with the gradient 16384 x 65536 bf16 745 (5.8), 65536 x 256 bf16 16.0 (4.3).
 template <class T, int kLanes, int kPer, Task kTask>
 __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::kResident)) void k_logits(LogitsArgs a)
 {
@@ -476,7 +483,8 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
     }
 }
 
-// The runs of a row put together by kThreads threads: a workgroup, or a wavefront.
+// The runs of a row put together by kThreads threads: a workgroup, or a wavefront.  A launch and a few trips to memory: 5.4 us
+// for one row of 16 runs with 20 alternatives each, 7.2 for 4093 rows of 7 runs with 5.
 template <int kThreads>
 __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type)
 {
@@ -545,7 +553,8 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type
     }
 }
 
-// The gradient where a row's law is known: run by run.
+// The gradient where a row's law is known: run by run, 16 KB at most, read once and written once.  Memory bounds it: 8190 x
+// 50001 f16 275 us (5.9 TB/s).
 template <class T, int kLanes, int kPer>
 __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logits_grad(LogitsArgs a)
 {
@@ -670,12 +679,15 @@ static LogitsPlan logits_plan(uint32_t rows, uint32_t num_sym, uint32_t value, u
     const uint32_t span = splits == needed ? (splits == 1 ? num_sym : longest / value) : div_up(div_up(num_sym, splits), vec) * vec;
     return {div_up(num_sym, span), span};
 }
-// Whether pilc_logprobs_train keeps whole rows in registers: up to 256 KB, those of a workgroup of 1024.
+// Whether pilc_logprobs_train keeps whole rows in registers: up to 256 KB, those of a workgroup of 1024.  Few rows of over
+// 32 KB keep more of the GPU busy in runs, which costs two launches more (bf16, us by rows and by runs: 16000 symbols 6.7
+// and 9.4 for 16 rows; 50000 symbols 13.7 and 9.7 for 16, 15.6 and 16.4 for 128; 131072 symbols 22.8 and 17.9 for 64, 25.2
+// and 25.5 for 128).
 constexpr uint32_t kLongestRow = 256 << 10;
 static bool train_by_row(uint32_t rows, uint32_t num_sym, uint32_t value)
 {
     const uint64_t bytes = (uint64_t)num_sym * value;
-    return bytes <= kLongestRow && (bytes <= (4u << 10) || rows >= compute_units() / 2);
+    return bytes <= kLongestRow && (bytes <= (32u << 10) || rows >= compute_units() / 2);
 }
 
 // What the runs of split rows leave for the kernel that puts them together.
@@ -757,7 +769,9 @@ static void launch_law(LogitsArgs a, uint32_t type, void *workspace, hipStream_t
     else
         launch_logits<T, kLaw>(a, stream);
     if (a.splits == 1) return;
-    if (a.splits > 16)  // few rows: a workgroup each
+    // by wavefronts, or few rows with many keys or runs by workgroups (bf16, 131072 symbols, 20 alternatives: one row 13.1 and
+    // 10.8 us, 64 rows 13.8 and 14.0; without alternatives one row 6.4 and 6.8)
+    if (a.splits > (a.top ? 16u : 256u))
         k_logits_join<256><<<std::min(a.rows, 1u << 20), 256, 0, stream>>>(a, type);
     else
         k_logits_join<64><<<std::min(div_up(a.rows, 4), 1u << 20), 256, 0, stream>>>(a, type);
