@@ -211,10 +211,10 @@ __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
         step(i < t.count ? (int)min((uint64_t)kEach, t.count - i) : 0);
 }
 
-// Thirty-two values a thread, four at a time, all codes asked for before the first value is written: a byte read
-// makes four written, so that reads of four bytes a lane leave too few bytes on their way if one waits for the other (300
-// million values: 251 us, 6.0 TB/s; four values a thread 370).
-constexpr int kValuesParts = 8;
+// Eight values a thread, two times four, all codes asked for before the first value is written.  Memory bounds it, four bytes
+// written for a byte read (300 million values with 4, 8, 12, 16 and 32 values a thread: signed 290, 238, 263, 266 and 262 us,
+// unsigned 281, 245, 285, 270 and 262; 6.2 TB/s with 8).
+constexpr int kValuesParts = 2;
 constexpr uint32_t kValuesChunk = 256 * 4 * kValuesParts;
 template <bool kSigned>
 __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *__restrict__ code, const uint8_t *__restrict__ scale, uint64_t count,

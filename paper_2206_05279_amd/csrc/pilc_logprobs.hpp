@@ -383,7 +383,7 @@ __device__ __forceinline__ void put_gradient(const Raw<T> &x, T *to, uint32_t co
 enum Task { kLaw, kPick, kTrainRows };
 
 // A row, or a run of one, a workgroup or a part of it; a row that is one run is finished here.  Measured (whole calls):
-// laws of 16384 x 32768 bf16 192 us (5.6 TB/s), of 65536 x 256 f32 12.6 (5.4); with alternatives 4093 x 100003 bf16 177 (4.6,
+// laws of 16384 x 32768 bf16 197 us (5.5 TB/s), of 65536 x 256 f32 13.6 (4.9); with alternatives 4093 x 100003 bf16 183 (4.5,
 // with the joining kernel); with the gradient 16384 x 65536 bf16 745 (5.8), 65536 x 256 bf16 16.0 (4.3).
 template <class T, int kLanes, int kPer, Task kTask>
 __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::kResident)) void k_logits(LogitsArgs a)
@@ -483,8 +483,8 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
     }
 }
 
-// The runs of a row put together by kThreads threads: a workgroup, or a wavefront.  A launch and a few trips to memory: 5.4 us
-// for one row of 16 runs with 20 alternatives each, 7.2 for 4093 rows of 7 runs with 5.
+// The runs of a row put together by kThreads threads: a workgroup, or a wavefront.  A launch and a few trips to memory: 5.2 us
+// for one row of 32 runs with 20 alternatives each, 7.2 for 4093 rows of 7 runs with 5.
 template <int kThreads>
 __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type)
 {

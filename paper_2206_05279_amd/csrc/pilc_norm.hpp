@@ -15,8 +15,10 @@ struct NormArgs {
 };
 
 constexpr int kNormThreads = 256, kNormLongThreads = 1024;
-// Wavefronts a SIMD that the kernels' registers are kept down to, and that are launched: all at once, each going from row to row.
-constexpr int kNormForwardWaves = 5, kNormBackwardWaves = 3;
+// Wavefronts a SIMD that the kernels' registers are kept down to, and that are launched: all at once, each going from row to row
+// (forward with 4, 5 and 6 within 3 % of each other; backward, 32768 x 4096 bf16, with 2, 3 and 4: 154, 161 and 293 us, and
+// 8192 x 4096 f32 with 2 and 3: 82 and 89, as more of them put down more parts and 4 leave too few registers).
+constexpr int kNormForwardWaves = 5, kNormBackwardWaves = 2;
 
 // Rows held in registers: kLanes lanes of a wavefront, or a whole workgroup of kLanes threads, hold kEach values of a
 // row each, as packs of 16 bytes, and go from row to row with the weights in registers.  A pack that would reach over
@@ -319,7 +321,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_backward_narrow(NormArgs 
 }
 
 // Rows too long for registers, over 32768 values: a workgroup goes through them two or three times, a pack a thread at a
-// time, and finds them in the caches after the first (8192 x 20000 bf16, while such rows came here, 538 us; 174 in registers).
+// time, and finds them in the caches after the first (8192 x 20000 bf16, while such rows came here, 539 us; 182 in registers).
 template <class T, int kVec, class F>
 __device__ __forceinline__ void for_packs(uint32_t width, F f)
 {
@@ -488,6 +490,15 @@ static uint32_t norm_blocks(uint32_t rows, int most_waves)
 {
     return std::min((rows + Row::kRows - 1) / Row::kRows, compute_units() * (uint32_t)(Row::waves(most_waves) * 256 / Row::kThreads));
 }
+// Workgroups of the backward pass.  With weights' gradients each puts down a part, as much as two rows in 32 bits, so that few
+// rows are shared out by four, once half the compute units have one (4096 columns bf16, us with a row and with four a workgroup:
+// 16 rows 6.2 and 8.2, 256 rows 11.2 and 10.5, by two 9.4, 500 rows 17.9 and 12.7, 1000 rows 18.7 and 15.2).
+template <class Row>
+static uint32_t norm_backward_blocks(uint32_t rows, bool with_parts)
+{
+    const uint32_t blocks = (rows + Row::kRows - 1) / Row::kRows, most = norm_blocks<Row>(rows, kNormBackwardWaves);
+    return with_parts ? std::min(most, std::max(compute_units() / 2, blocks / 4)) : most;
+}
 static uint32_t norm_most_parts(uint32_t rows) { return std::max(1u, std::min(rows, std::max(kNormLongParts, 4 * compute_units()))); }
 static size_t norm_workspace(const pilc_norm_shape &s)
 {
@@ -588,10 +599,11 @@ int pilc_norm_backward(const pilc_norm_shape *shape, const void *dy_dev, const v
         } else if (!norm_row(a.width, [&](auto lanes, auto each) {
                        using Row = NormRow<T, W, decltype(lanes)::value, decltype(each)::value>;
                        if (!Row::kKeep) parts(kNormLongParts);
-                       if (Row::kKeep) a.num_parts = norm_blocks<Row>(a.rows, kNormBackwardWaves);
+                       const uint32_t blocks = norm_backward_blocks<Row>(a.rows, Row::kKeep && a.parts);
+                       if (Row::kKeep) a.num_parts = blocks;
                        if (a.rows && (Row::kKeep || a.dx))
                            k_norm_backward_rows<T, W, decltype(lanes)::value, decltype(each)::value>
-                               <<<norm_blocks<Row>(a.rows, kNormBackwardWaves), Row::kThreads, 0, stream>>>(a);
+                               <<<blocks, Row::kThreads, 0, stream>>>(a);
                    })) {
             parts(kNormLongParts);
             if (a.dx && a.rows) k_norm_dx_long<T, W><<<std::min(a.rows, 1u << 20), kNormLongThreads, 0, stream>>>(a);
