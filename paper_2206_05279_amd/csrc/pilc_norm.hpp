@@ -320,15 +320,35 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_backward_narrow(NormArgs 
     }
 }
 
-// Rows too long for registers, over 32768 values: a workgroup goes through them two or three times, a pack a thread at a
-// time, and finds them in the caches after the first (8192 x 20000 bf16, while such rows came here, 539 us; 182 in registers).
-template <class T, int kVec, class F>
-__device__ __forceinline__ void for_packs(uint32_t width, F f)
+// Rows too long for registers, over 32768 values: a workgroup goes through them two or three times and finds them in the caches
+// after the first (8192 x 20000 bf16, while such rows came here, 539 us; 182 in registers).  Four packs a thread at a time, so
+// that four loads are on their way: forward 4096 x 40000 bf16 247 us, with one at a time 531.
+constexpr int kNormLongEach = 4;
+constexpr uint32_t kNormLongStep = kNormLongThreads * kNormLongEach;
+template <int kVec, class F>
+__device__ __forceinline__ void for_packs(uint32_t width, F f)  // f(columns, how many of a pack's first values others have)
 {
-    for (uint32_t place = threadIdx.x * kVec; place < width; place += kNormLongThreads * kVec) {
-        const uint32_t column = min(place, width - kVec);  // the last one begins earlier: its first values have been gone through
-        f(column, (int)(place - column));
+    for (uint32_t first = threadIdx.x * kVec; first < width; first += kNormLongStep * kVec) {
+        uint32_t column[kNormLongEach];
+        int twice[kNormLongEach];
+#pragma unroll
+        for (int q = 0; q < kNormLongEach; ++q) {
+            const uint32_t place = first + q * kNormLongThreads * kVec;
+            column[q] = min(place, width - kVec);  // the last one begins earlier: its first values have been gone through
+            twice[q] = (int)min(place - column[q], (uint32_t)kVec);
+        }
+        f(column, twice);
     }
+}
+// What is written may be what is read: no value is gone through twice.
+template <int kVec, class F>
+__device__ __forceinline__ void for_whole_packs(uint32_t width, F f)  // f(count, column, valid)
+{
+    const uint32_t step = kNormLongStep * kVec;
+    uint32_t begin = 0;
+    for (; width - begin >= step; begin += step) f(std::integral_constant<int, kNormLongEach>(), begin + threadIdx.x * kVec, kVec);
+    for (uint32_t place = begin + threadIdx.x * kVec; place < width; place += kNormLongThreads * kVec)
+        f(std::integral_constant<int, 1>(), place, (int)min(width - place, (uint32_t)kVec));
 }
 template <int kVec, class T>
 __device__ __forceinline__ Pack<T, kVec> pack_at(const T *p) { return *(const Pack<T, kVec> *)p; }
@@ -345,35 +365,52 @@ __global__ __launch_bounds__(kNormLongThreads) void k_norm_forward_long(NormArgs
         const T *x = (const T *)a.x + row * a.x_stride;
         T *y = (T *)a.y + row * a.y_stride;
         float sum = 0.0f, square = 0.0f;
-        for_packs<T, kVec>(a.width, [&](uint32_t column, int twice) {
-            const auto t = pack_at<kVec>(x + column);
+        for_packs<kVec>(a.width, [&](const auto &column, const auto &twice) {
+            Pack<T, kVec> t[kNormLongEach];
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) sum += k >= twice ? widen(t.v[k]) : 0.0f;
+            for (int q = 0; q < kNormLongEach; ++q) t[q] = pack_at<kVec>(x + column[q]);
+#pragma unroll
+            for (int q = 0; q < kNormLongEach; ++q)
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) sum += k >= twice[q] ? widen(t[q].v[k]) : 0.0f;
         });
         const float mean = block_reduce<kWaves>(sum, Sum(), room) / (float)a.width;
-        for_packs<T, kVec>(a.width, [&](uint32_t column, int twice) {
-            const auto t = pack_at<kVec>(x + column);
+        for_packs<kVec>(a.width, [&](const auto &column, const auto &twice) {
+            Pack<T, kVec> t[kNormLongEach];
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                const float d = k >= twice ? widen(t.v[k]) - mean : 0.0f;
-                square += d * d;
-            }
+            for (int q = 0; q < kNormLongEach; ++q) t[q] = pack_at<kVec>(x + column[q]);
+#pragma unroll
+            for (int q = 0; q < kNormLongEach; ++q)
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    const float d = k >= twice[q] ? widen(t[q].v[k]) - mean : 0.0f;
+                    square += d * d;
+                }
         });
         const float rstd = 1.0f / sqrtf(block_reduce<kWaves>(square, Sum(), room) / (float)a.width + a.eps);
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
-        for (uint32_t place = threadIdx.x * kVec; place < a.width; place += kNormLongThreads * kVec) {
-            const int valid = (int)min(a.width - place, (uint32_t)kVec);  // not a value twice: the other may be y already
-            const auto t = load_pack<kVec>(x + place, valid);
-            Pack<T, kVec> out;
+        for_whole_packs<kVec>(a.width, [&](auto count, uint32_t place, int valid) {
+            constexpr int kCount = decltype(count)::value;
+            Pack<T, kVec> t[kCount];
+            Pack<W, kVec> w[kCount], c[kCount];
 #pragma unroll
-            for (int k = 0; k < kVec; ++k)
-                out.v[k] = (T)((widen(t.v[k]) - mean) * rstd * (weight && k < valid ? widen(weight[place + k]) : 1.0f) +
-                               (bias && k < valid ? widen(bias[place + k]) : 0.0f));
-            store_pack(y + place, valid, out);
-        }
+            for (int q = 0; q < kCount; ++q) {
+                const uint32_t at = place + q * kNormLongThreads * kVec;
+                t[q] = load_pack<kVec>(x + at, valid);
+                if (weight) w[q] = load_pack<kVec>(weight + at, valid);
+                if (bias) c[q] = load_pack<kVec>(bias + at, valid);
+            }
+#pragma unroll
+            for (int q = 0; q < kCount; ++q) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k)
+                    t[q].v[k] = (T)((widen(t[q].v[k]) - mean) * rstd * (weight ? widen(w[q].v[k]) : 1.0f) + (bias ? widen(c[q].v[k]) : 0.0f));
+                store_pack(y + place + q * kNormLongThreads * kVec, valid, t[q]);
+            }
+        });
         __syncthreads();
     }
 }
@@ -390,28 +427,45 @@ __global__ __launch_bounds__(kNormLongThreads) void k_norm_dx_long(NormArgs a)
         T *dx = (T *)a.dx + row * a.dx_stride;
         const float mean = a.mean_in[row], rstd = a.rstd_in[row];
         float q_sum = 0.0f, qx_sum = 0.0f;
-        for_packs<T, kVec>(a.width, [&](uint32_t column, int twice) {
-            const auto tx = pack_at<kVec>(x + column), td = pack_at<kVec>(dy + column);
+        for_packs<kVec>(a.width, [&](const auto &column, const auto &twice) {
+            Pack<T, kVec> tx[kNormLongEach], td[kNormLongEach];
+            Pack<W, kVec> w[kNormLongEach];
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                const float q = k >= twice ? widen(td.v[k]) * (weight ? widen(weight[column + k]) : 1.0f) : 0.0f;
-                q_sum += q;
-                qx_sum += q * ((widen(tx.v[k]) - mean) * rstd);
+            for (int q = 0; q < kNormLongEach; ++q) {
+                tx[q] = pack_at<kVec>(x + column[q]), td[q] = pack_at<kVec>(dy + column[q]);
+                if (weight) w[q] = pack_at<kVec>(weight + column[q]);
             }
+#pragma unroll
+            for (int q = 0; q < kNormLongEach; ++q)
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    const float g = k >= twice[q] ? widen(td[q].v[k]) * (weight ? widen(w[q].v[k]) : 1.0f) : 0.0f;
+                    q_sum += g;
+                    qx_sum += k >= twice[q] ? g * ((widen(tx[q].v[k]) - mean) * rstd) : 0.0f;
+                }
         });
         const float c1 = block_reduce<kWaves>(q_sum, Sum(), room) / (float)a.width;
         const float c2 = block_reduce<kWaves>(qx_sum, Sum(), room) / (float)a.width;
-        for (uint32_t place = threadIdx.x * kVec; place < a.width; place += kNormLongThreads * kVec) {
-            const int valid = (int)min(a.width - place, (uint32_t)kVec);
-            const auto tx = load_pack<kVec>(x + place, valid), td = load_pack<kVec>(dy + place, valid);
-            Pack<T, kVec> out;
+        for_whole_packs<kVec>(a.width, [&](auto count, uint32_t place, int valid) {
+            constexpr int kCount = decltype(count)::value;
+            Pack<T, kVec> tx[kCount], td[kCount];
+            Pack<W, kVec> w[kCount];
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                const float q = widen(td.v[k]) * (weight && k < valid ? widen(weight[place + k]) : 1.0f);
-                out.v[k] = (T)(rstd * (q - c1 - (widen(tx.v[k]) - mean) * rstd * c2));
+            for (int q = 0; q < kCount; ++q) {
+                const uint32_t at = place + q * kNormLongThreads * kVec;
+                tx[q] = load_pack<kVec>(x + at, valid), td[q] = load_pack<kVec>(dy + at, valid);
+                if (weight) w[q] = load_pack<kVec>(weight + at, valid);
             }
-            store_pack(dx + place, valid, out);
-        }
+#pragma unroll
+            for (int q = 0; q < kCount; ++q) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    const float g = widen(td[q].v[k]) * (weight ? widen(w[q].v[k]) : 1.0f);
+                    td[q].v[k] = (T)(rstd * (g - c1 - (widen(tx[q].v[k]) - mean) * rstd * c2));
+                }
+                store_pack(dx + place + q * kNormLongThreads * kVec, valid, td[q]);
+            }
+        });
         __syncthreads();
     }
 }
@@ -483,7 +537,7 @@ static bool norm_row(uint32_t width, Go go)
            with(integral_constant<int, 1024>(), integral_constant<int, 16>()) || with(integral_constant<int, 1024>(), integral_constant<int, 32>());
 }
 
-constexpr uint32_t kNormLongParts = 64;
+constexpr uint32_t kNormLongParts = 64, kNormLongestKept = 16384;
 static uint32_t narrow_blocks(uint32_t rows) { return std::min(div_up(rows, kNormThreads), 1u << 20); }
 template <class Row>
 static uint32_t norm_blocks(uint32_t rows, int most_waves)
@@ -499,10 +553,16 @@ static uint32_t norm_backward_blocks(uint32_t rows, bool with_parts)
     const uint32_t blocks = (rows + Row::kRows - 1) / Row::kRows, most = norm_blocks<Row>(rows, kNormBackwardWaves);
     return with_parts ? std::min(most, std::max(compute_units() / 2, blocks / 4)) : most;
 }
-static uint32_t norm_most_parts(uint32_t rows) { return std::max(1u, std::min(rows, std::max(kNormLongParts, 4 * compute_units()))); }
+// The most parts of any of the ways below: rows too long for kKeep go by kNormLongParts, the others by workgroups that are all
+// there at once, or with less than a pack a row by one a compute unit.
+static uint32_t norm_most_parts(uint32_t rows, uint32_t width)
+{
+    const uint32_t most = width > kNormLongestKept ? kNormLongParts : std::max(kNormLongParts, (uint32_t)kNormBackwardWaves * compute_units());
+    return std::max(1u, std::min(rows, most));
+}
 static size_t norm_workspace(const pilc_norm_shape &s)
 {
-    return std::max<size_t>(256, 2 * sizeof(float) * (size_t)norm_most_parts(s.rows) * s.width);
+    return std::max<size_t>(256, 2 * sizeof(float) * (size_t)norm_most_parts(s.rows, s.width) * s.width);
 }
 
 static bool norm_shape_ok(const pilc_norm_shape *s, bool backward)
@@ -600,6 +660,8 @@ int pilc_norm_backward(const pilc_norm_shape *shape, const void *dy_dev, const v
                        using Row = NormRow<T, W, decltype(lanes)::value, decltype(each)::value>;
                        if (!Row::kKeep) parts(kNormLongParts);
                        const uint32_t blocks = norm_backward_blocks<Row>(a.rows, Row::kKeep && a.parts);
+                       static_assert(Row::waves(kNormBackwardWaves) * 256 / Row::kThreads <= kNormBackwardWaves &&
+                                     Row::kKeep == (Row::kThreads == 256 || decltype(lanes)::value * decltype(each)::value <= kNormLongestKept));
                        if (Row::kKeep) a.num_parts = blocks;
                        if (a.rows && (Row::kKeep || a.dx))
                            k_norm_backward_rows<T, W, decltype(lanes)::value, decltype(each)::value>
