@@ -611,12 +611,18 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitsArgs a)
             spoilt |= !(scale.max == scale.max);
         } else {
             Tally tally = {largest, 0.0f, 0.0f};
+            float first = 0.0f, rest = 0.0f;  // the largest's power and the others', apart: a nearly certain symbol's ln p is the others'
+            bool met = false;
             for (uint32_t j = 0; j < a.num_sym; ++j) {
-                const float z = scale.power(widen(x[j])), e = exp2_fast(z);
-                tally.total += e;
+                const float v = widen(x[j]), z = scale.power(v), e = exp2_fast(z);
+                const bool it = v == largest && !met;
+                met |= it;
+                it ? first = e : rest += e;
                 tally.inside += e * fmaxf(z, kLeast);
             }
-            const Law law(tally);
+            tally.total = first + rest;
+            Law law(tally);
+            if (law.max > -kInf) law.log_total = log1pf(rest / first);
             if (a.entropy) a.entropy[row] = law.entropy;
             if (a.lse) a.lse[row] = law.lse();
             if (a.logp) a.logp[row] = t < 0 ? 0.0f : spoilt ? __builtin_nanf("") : law.logp(widen(x[t]));

@@ -285,3 +285,24 @@ def test_same_bits_every_time():
     for _ in range(5):
         c.forward()
         assert all(torch.equal(p, q) for p, q in zip(first, (c.logp, c.entropy, c.lse, c.top_sym, c.top_logp)))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n", [2, 3, 7])
+def test_nearly_certain_symbol_of_a_short_row_keeps_its_digits(n, dtype):
+    if n * torch.empty(0, dtype=TYPES[dtype]).element_size() >= 16:
+        pytest.skip("as long as a pack")
+    rng = np.random.default_rng(n)
+    rows = 400
+    values = rng.uniform(4.0, 6.0, (rows, n))
+    targets = rng.integers(0, n, rows)
+    values[np.arange(rows), targets] += rng.uniform(4.0, 12.0, rows)
+    c = Case(values, targets, TYPES[dtype])
+    c.forward()
+    z = c.x64 - c.x64[np.arange(rows), targets][:, None]
+    z[np.arange(rows), targets] = -np.inf
+    want = -np.log1p(np.exp(z).sum(1))
+    # a power of two's exponent is below 24, rounded twice (24 units of 2^-24 each), and the power, the sum of six, the quotient
+    # and the logarithm take less than 16: 64 units are room enough, where 1 - p by itself would leave none
+    off = np.abs(c.logp.cpu().double().numpy() / want - 1)
+    assert off.max() <= 2.0 ** -18, off.max()
