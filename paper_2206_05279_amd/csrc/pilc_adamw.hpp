@@ -109,7 +109,7 @@ constexpr int kAdamwThreads = 256;
 constexpr int kAdamwEach = 4, kAdamwBytesEach = 8;
 constexpr uint32_t kAdamwChunk = kAdamwThreads * kAdamwEach, kAdamwBytesChunk = kAdamwThreads * kAdamwBytesEach;
 
-// States in 32 bits.  28 bytes a value in f32 and some thirty instructions: memory bounds it, at 5.3 TB/s (150 million
+// States in 32 bits.  28 bytes a value in f32 and 24 vector instructions: memory bounds it, at 5.3 TB/s (150 million
 // values in 291 tensors).
 template <class P, class G>
 __global__ __launch_bounds__(kAdamwThreads) void k_adamw(AdamwArgs a)
@@ -157,8 +157,7 @@ __device__ __forceinline__ void store_codes(uint8_t *p, int valid, const uint32_
 }
 
 // States in 8 bits: half a wavefront a block of 256, whose largest values it finds among its lanes.  10 bytes a value in
-// bf16 and 69 vector instructions, a third of them for the random numbers and the coding: the vector units are busy 91 % of
-// the time, memory at 5.3 TB/s (300 million values: 564 us).
+// bf16 and 67 vector instructions: the vector units are busy 90 % of the time, memory at 5.3 TB/s (300 million values: 564 us).
 template <class P, class G>
 __global__ __launch_bounds__(kAdamwThreads) void k_adamw_bytes(AdamwArgs a)
 {

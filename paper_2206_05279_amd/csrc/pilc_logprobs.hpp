@@ -5,9 +5,9 @@ namespace pilc {
 
 // Per row of logits x: M = max x, S = sum of e^(x - M), U = sum of (x - M) e^(x - M); lse = M + ln S, ln p of symbol t = x_t - lse,
 // entropy = ln S - U / S, and the gradient of a logp + b entropy is a (1[j = t] - p_j) - b p_j (ln p_j + entropy).  A value
-// takes some ten instructions, four of their issue slots for the power of two, and two or four bytes: memory and the vector
-// units bound the kernels about alike in 16 bits, memory in 32.  So a value is read once, into registers, and gone through
-// there: for M, for S and U, for the alternatives, for the gradient.
+// takes 11 vector instructions for the gradient alone, 15 for the law of a long row with alternatives and 22 for law and gradient
+// (counted), and two or four bytes: vector units and memory bound the kernels about alike.  So a value is read once, into
+// registers, and gone through there: for M, for S and U, for the alternatives, for the gradient.
 
 constexpr int kMaxTop = 32;
 

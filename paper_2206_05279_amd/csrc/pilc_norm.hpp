@@ -163,7 +163,7 @@ k_norm_forward_rows(NormArgs a)
 
 // dx row by row as above, and what the rows a workgroup meets add to the weights' gradients, in registers; at the end
 // the workgroup's rows are added up and put down as one part.  The longest rows leave no room for that: k_norm_parts.
-// Memory bounds it: 32768 x 4096 bf16 155 us and 6 for k_norm_join (5.0 TB/s with the parts).
+// Memory bounds it: 32768 x 4096 bf16 144 us and 5 for k_norm_join (5.7 TB/s with the parts).
 template <class T, class W, int kLanes, int kEach>
 __global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads), (NormRow<T, W, kLanes, kEach>::waves(kNormBackwardWaves))) void
 k_norm_backward_rows(NormArgs a)
@@ -497,8 +497,8 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_parts(NormArgs a)
     }
 }
 
-// The parts added up: 64 columns a workgroup, each by sixteen threads that take every sixteenth part (768 parts of 4096
-// columns, 25 MB: 6.4 us).
+// The parts added up: 64 columns a workgroup, each by sixteen threads that take every sixteenth part (512 parts of 4096
+// columns, 17 MB: 5.4 us).
 template <class W>
 __global__ __launch_bounds__(1024) void k_norm_join(NormArgs a)
 {
