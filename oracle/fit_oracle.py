@@ -16,11 +16,22 @@ def chain(n: int) -> float:
     return min(n, n / 64 + 64) + 16
 
 
+def apart_sums(n: int, first: float) -> float:
+    """What a row's sum of powers may be off, in units of U of itself.  A power's exponent is rounded when the largest value is
+    taken from it, when it goes from e to 2 and by log2 e having 24 bits, less than three units of its size together (`first` is
+    the sizes' mean under the law); the power itself is two off; a common factor of all of a part's powers is taken out (three),
+    and parts are joined by powers of their own (a few units each)."""
+    return chain(n) + 24 + 3 * first
+
+
 def logprobs(x, target, top):
     """x [rows, n] float64, target [rows] int64 or None.  Returns a dict: lse, entropy, logp, top_sym, top_logp,
-    and the bounds of the errors that 32-bit arithmetic may make in lse, entropy and logp."""
+    and the bounds of the errors that 32-bit arithmetic may make in lse, entropy and logp.  logp_apart is logp by the largest
+    value and the logarithm of the sum one after the other, which lse, however many bits it has, swallows where the logits lie far
+    from zero; its bound logp_apart_err has no share of |lse|."""
     rows, n = x.shape
-    out = {k: np.zeros(rows) for k in ("lse", "entropy", "logp", "lse_err", "entropy_err", "logp_err")}
+    out = {k: np.zeros(rows) for k in ("lse", "entropy", "logp", "lse_err", "entropy_err", "logp_err", "logp_apart",
+                                         "logp_apart_err")}
     out["top_sym"] = np.full((rows, top), -1, dtype=np.int32)
     out["top_logp"] = np.full((rows, top), -np.inf)
     for r in range(rows):
@@ -29,13 +40,13 @@ def logprobs(x, target, top):
         t = None if target is None else int(target[r])
         if bad:
             out["lse"][r] = out["entropy"][r] = np.nan
-            out["logp"][r] = 0.0 if t is not None and t < 0 else np.nan
+            out["logp"][r] = out["logp_apart"][r] = 0.0 if t is not None and t < 0 else np.nan
             out["top_logp"][r] = np.nan
             continue
         there = v > -np.inf
         if not there.any():
             out["lse"][r] = -np.inf
-            out["logp"][r] = 0.0 if t is not None and t < 0 else np.nan if t is not None and t >= n else -np.inf
+            out["logp"][r] = out["logp_apart"][r] = 0.0 if t is not None and t < 0 else np.nan if t is not None and t >= n else -np.inf
             continue
         big = v.max()
         z = v[there] - big
@@ -54,14 +65,20 @@ def logprobs(x, target, top):
             out["logp"][r] = 0.0 if t < 0 else np.nan if t >= n else v[t] - out["lse"][r]
             if 0 <= t < n and v[t] > -np.inf:
                 out["logp_err"][r] = U * (sums + 4 * log_total + 3 * abs(v[t] - big) + 3 * abs(out["logp"][r]) + 2 * abs(out["lse"][r]) + 1)
+            out["logp_apart"][r] = 0.0 if t < 0 else np.nan if t >= n else (v[t] - big) - log_total
+            if 0 <= t < n and v[t] > -np.inf:
+                out["logp_apart_err"][r] = U * (apart_sums(n, first) + 4 * log_total + 3 * abs(v[t] - big) + 3 * abs(out["logp_apart"][r]) + 1)
+        if top == 0:
+            continue
         order = sorted(np.flatnonzero(there), key=lambda j: (-v[j], j))[:top]
         out["top_sym"][r, :len(order)] = order
         out["top_logp"][r, :len(order)] = v[order] - out["lse"][r]
     return out
 
 
-def logprobs_grad(x, target, up_logp, up_entropy):
-    """(gradient, bound of its error before the last rounding) by the logits; up_entropy may be None."""
+def logprobs_grad(x, target, up_logp, up_entropy, apart=False):
+    """(gradient, bound of its error before the last rounding) by the logits; up_entropy may be None.  apart: the law as it is by
+    the largest value and the sum, not by an lse that was rounded; its bound has no share of |lse|."""
     rows, n = x.shape
     g, err = np.zeros_like(x), np.zeros_like(x)
     law = logprobs(x, target, 0)
@@ -77,14 +94,23 @@ def logprobs_grad(x, target, up_logp, up_entropy):
             continue
         if lse == -np.inf:
             continue
-        lp = np.where(x[r] > -np.inf, x[r] - lse, -np.inf)
+        there = x[r] > -np.inf
+        big = x[r][there].max()
+        z = np.where(there, x[r] - big, -np.inf)
+        total = np.exp(z).sum()
+        lp = z - np.log(total) if apart else np.where(there, x[r] - lse, -np.inf)
         p = np.exp(lp)
         fall = np.where(p > 0, lp, 0.0)
         g[r] = -a * p - b * p * (fall + h)
         if t >= 0:
             g[r, t] += a
-        off = law["lse_err"][r] + U * (2 * np.abs(fall) + abs(lse) + 4)         # relative error of p
-        err[r] = p * (abs(a) * (off + 4 * U) + abs(b) * ((np.abs(fall) + h) * (off + 6 * U) + off + law["entropy_err"][r])) + U * np.abs(g[r])
+        if apart:       # of a power, of the sum and of what is made of both
+            near = np.where(p > 0, -z, 0.0)
+            off = U * (apart_sums(n, (p * near).sum()) + 3 * near + 2 * np.abs(fall) + 4 * np.log(total) + 12)
+        else:
+            off = law["lse_err"][r] + U * (2 * np.abs(fall) + abs(lse) + 4)         # relative error of p
+        h_err = law["entropy_err"][r] * (3 if apart else 1)     # three roundings of an exponent for one
+        err[r] = p * (abs(a) * (off + 4 * U) + abs(b) * ((np.abs(fall) + h) * (off + 6 * U) + off + h_err)) + U * np.abs(g[r])
         if t >= 0:
             err[r, t] += 2 * U * abs(a)
     return g, err

@@ -73,13 +73,13 @@ struct Tally {
     float max, total, inside;
 };
 
-// Both tallies' values together.
+// Both tallies' values together.  A tally's powers are 2^off too large, each with its own rounding of the shift; between the
+// maxima themselves lies what the exponents are apart.  Where neither maximum is a number's (-inf twice) there is nothing to add.
 __device__ __forceinline__ Tally both(Tally a, Tally b)
 {
-    const float max = fmaxf(a.max, b.max);
-    // the exponents' difference as the powers were taken, each with its own rounding of the shift
-    const Scale of(max), sa(a.max), sb(b.max);
-    const float da = a.max == -kInf ? kLeast : fmaxf(sa.shift - of.shift, kLeast), db = b.max == -kInf ? kLeast : fmaxf(sb.shift - of.shift, kLeast);
+    const float max = fmaxf(a.max, b.max), off = Scale(max).off;
+    const float da = fmaxf((a.max - max) * kLog2e + (off - Scale(a.max).off), kLeast);
+    const float db = fmaxf((b.max - max) * kLog2e + (off - Scale(b.max).off), kLeast);
     const float fa = exp2_fast(da), fb = exp2_fast(db);
     return {max, a.total * fa + b.total * fb, (a.inside + da * a.total) * fa + (b.inside + db * b.total) * fb};
 }
