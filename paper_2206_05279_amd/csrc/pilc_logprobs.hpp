@@ -47,39 +47,52 @@ __device__ __forceinline__ float value_of(uint64_t key)
     return __uint_as_float(order & 0x80000000u ? order & 0x7FFFFFFFu : ~order);
 }
 
-// How exponentials of a row's values are taken: 2^(x rate - shift), one fused multiply-add and one power a value.  shift
-// is the largest value times rate, rounded, so that all powers are the same factor 2^off too large; it cancels in
-// probabilities and is taken out of logarithms.  Where the product would overflow, values that differ at all differ by
-// so much that any rate does.
-struct Scale {
-    float max, rate, shift, off;
-
-    __device__ explicit Scale(float m) : max(m)
-    {
-        const bool plain = fabsf(m) < 1e38f;
-        rate = plain ? kLog2e : 0x1p-60f;
-        shift = m == -kInf ? 0.0f : m * rate;
-        off = plain ? __builtin_fmaf(m, rate, -shift) : 0.0f;
-    }
-    __device__ float power(float x) const { return __builtin_fmaf(x, rate, -shift); }
-};
 constexpr float kLn2 = 0.693147180559945309f;
 // No 32-bit power of two is left here: what a power is multiplied with need not go on falling, and may not be -inf.
 constexpr float kLeast = -200.0f;
 
-// What is known of a row or of a part of it: its largest value, the sum of the powers of its values and the sum of their
-// products with the exponents.
+// How exponentials of a row's values are taken: 2^(x log2 e - shift), one fused multiply-add and one power a value.  shift is
+// the largest value times log2 e, rounded, so that all powers are the same factor 2^off too large, which is taken out of
+// sums.  off is half a unit of shift at most: 1/16 where the largest value is under 2^20 in size, but 128, and 2^off no
+// number, from 2^31 on.  Rows whose largest value lies further out than 2^20 have it subtracted first, which is an instruction more a
+// value (4093 x 100003 bf16 with alternatives 162 us, all rows that way 168; training 65536 x 256 bf16 16.0 and 16.5, 16384 x 65536
+// 744 and 745).
+struct Scale {
+    static constexpr float kFused = 0x1p20f;
+    float center, shift, off;
+    bool apart;
+
+    __device__ explicit Scale(float m)
+    {
+        center = m == -kInf ? 0.0f : m;
+        apart = !(fabsf(center) < kFused);
+        shift = center * kLog2e;
+        off = apart ? 0.0f : __builtin_fmaf(center, kLog2e, -shift);
+    }
+    template <bool kApart>
+    __device__ float power(float x) const { return kApart ? (x - center) * kLog2e : __builtin_fmaf(x, kLog2e, -shift); }
+    // f(std::bool_constant) with the way that this row's values go
+    template <class F>
+    __device__ void by_power(F f) const
+    {
+        if (apart)
+            f(std::true_type());
+        else
+            f(std::false_type());
+    }
+};
+
+// What is known of a row or of a part of it: its largest value, the sum of its values' powers 2^z, z = (x - max) log2 e, and
+// the sum of z 2^z.
 struct Tally {
     float max, total, inside;
 };
 
-// Both tallies' values together.  A tally's powers are 2^off too large, each with its own rounding of the shift; between the
-// maxima themselves lies what the exponents are apart.  Where neither maximum is a number's (-inf twice) there is nothing to add.
+// Both tallies' values together.  Where neither maximum is a number's (-inf twice) there is nothing to add.
 __device__ __forceinline__ Tally both(Tally a, Tally b)
 {
-    const float max = fmaxf(a.max, b.max), off = Scale(max).off;
-    const float da = fmaxf((a.max - max) * kLog2e + (off - Scale(a.max).off), kLeast);
-    const float db = fmaxf((b.max - max) * kLog2e + (off - Scale(b.max).off), kLeast);
+    const float max = fmaxf(a.max, b.max);
+    const float da = fmaxf((a.max - max) * kLog2e, kLeast), db = fmaxf((b.max - max) * kLog2e, kLeast);
     const float fa = exp2_fast(da), fb = exp2_fast(db);
     return {max, a.total * fa + b.total * fb, (a.inside + da * a.total) * fa + (b.inside + db * b.total) * fb};
 }
@@ -94,13 +107,25 @@ struct Law {
             log_total = entropy = 0.0f;
             return;
         }
-        const float log = logf(t.total);
-        entropy = log - kLn2 * t.inside / t.total;
-        log_total = log - kLn2 * Scale(t.max).off;
-        if (!(log == log)) max = log_total = entropy = log;
+        log_total = logf(t.total);
+        entropy = log_total - kLn2 * t.inside / t.total;
+        if (!(log_total == log_total)) max = entropy = log_total;
     }
     __device__ float lse() const { return max + log_total; }
     __device__ float logp(float x) const { return max == -kInf ? -kInf : (x - max) - log_total; }
+};
+
+// grad_j = -p_j (a + b (ln p_j + entropy)), a more at the target: with z the exponent of a value's power, which is 2^off too
+// large, 2^z (from + slope z).
+struct Descent {
+    float from, slope;
+
+    __device__ Descent(const Scale &scale, float total, float log_total, float entropy, float up, float up_entropy)
+    {
+        const float each = exp2_fast(-scale.off) / total;
+        from = -(up + up_entropy * (entropy - log_total - kLn2 * scale.off)) * each;
+        slope = -up_entropy * kLn2 * each;
+    }
 };
 
 // Where a workgroup, or with kThreads 64 a wavefront by itself, puts side by side what may be among a row's best.
@@ -257,15 +282,18 @@ struct LogitsRow {
         const float max = lanes_reduce<kWithin>(own, MaxFloat());
         const Scale scale(max);
         float total[2] = {0.0f, 0.0f}, inside[2] = {0.0f, 0.0f};
-        for_used(used, [&](int q) {
+        scale.by_power([&](auto apart) {
+            for_used(used, [&](int q) {
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) {
-                const float z = scale.power(x[q][k]), e = exp2_fast(z);
-                total[k & 1] += e;
-                inside[k & 1] = __builtin_fmaf(e, fmaxf(z, kLeast), inside[k & 1]);
-            }
+                for (int k = 0; k < kVec; ++k) {
+                    const float z = scale.power<apart.value>(x[q][k]), e = exp2_fast(z);
+                    total[k & 1] += e;
+                    inside[k & 1] = __builtin_fmaf(e, fmaxf(z, kLeast), inside[k & 1]);
+                }
+            });
         });
-        Tally t = {max, lanes_reduce<kWithin>(total[0] + total[1], Sum()), lanes_reduce<kWithin>(inside[0] + inside[1], Sum())};
+        const float whole = lanes_reduce<kWithin>(total[0] + total[1], Sum()), less = exp2_fast(-scale.off);
+        Tally t = {max, whole * less, (lanes_reduce<kWithin>(inside[0] + inside[1], Sum()) - scale.off * whole) * less};
         if constexpr (kWaves > 1) {
             room += half * kWaves;
             if ((threadIdx.x & 63) == 0) room[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)] = t;
@@ -350,18 +378,17 @@ __device__ __forceinline__ void put_alternative(const LogitsArgs &a, const Law &
     a.top_logp[at] = none ? __builtin_nanf("") : key ? law.logp(value_of(key)) : -kInf;
 }
 
-// The gradient of one pack's values, the first of which is that of symbol `column` and goes to `to`: 2^z (from + slope z), and
-// `up` more at the target.
-template <class T>
-__device__ __forceinline__ void put_gradient(const Raw<T> &x, T *to, uint32_t column, int twice, const Scale &scale, float from, float slope,
+// The gradient of one pack's values, the first of which is that of symbol `column` and goes to `to`; `up` more at the target.
+template <bool kApart, class T>
+__device__ __forceinline__ void put_gradient(const Raw<T> &x, T *to, uint32_t column, int twice, const Scale &scale, const Descent &d_of,
                                              bool in, int64_t t, float up, bool zeros)
 {
     constexpr int kVec = 16 / sizeof(T);
     float d[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-        const float z = fmaxf(scale.power(x[i]), kLeast);
-        d[i] = exp2_fast(z) * __builtin_fmaf(slope, z, from);
+        const float z = fmaxf(scale.power<kApart>(x[i]), kLeast);
+        d[i] = exp2_fast(z) * __builtin_fmaf(d_of.slope, z, d_of.from);
     }
     const uint32_t k = (uint32_t)t - column;
     if (in && k < (uint32_t)kVec)
@@ -437,16 +464,17 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
                 }
             if constexpr (kTrain) {
                 const float up = t < 0 ? 0.0f : up_given;
-                // grad = e (from + slope z), ln p being ln 2 z - ln total
                 const Scale scale(tally.max);
-                float from = -(up + up_entropy * (law.entropy - logf(law.total))) / law.total, slope = -up_entropy * kLn2 / law.total;
+                Descent d(scale, law.total, law.log_total, law.entropy, up, up_entropy);
                 const bool zeros = (up == 0.0f && up_entropy == 0.0f) || law.max == -kInf;
-                if (t >= (int64_t)a.num_sym || !(law.max == law.max)) from = __builtin_nanf("");
+                if (t >= (int64_t)a.num_sym || !(law.max == law.max)) d.from = __builtin_nanf("");
                 T *grad = (T *)a.grad + row * a.grad_stride;
                 r.forget(x);
-                r.for_used(used, [&](int q) {
-                    const uint32_t column = r.column(q, begin, end);
-                    put_gradient(x[q], Row::address(grad, column, begin, end), column, r.twice(q, begin, end), scale, from, slope, in, t, up, zeros);
+                scale.by_power([&](auto apart) {
+                    r.for_used(used, [&](int q) {
+                        const uint32_t column = r.column(q, begin, end);
+                        put_gradient<apart.value>(x[q], Row::address(grad, column, begin, end), column, r.twice(q, begin, end), scale, d, in, t, up, zeros);
+                    });
                 });
             }
         }
@@ -568,20 +596,20 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logi
         const float up = t < 0 ? 0.0f : a.up_logp[row], up_entropy = a.up_entropy ? a.up_entropy[row] : 0.0f;
         const float lse = a.lse_in[row], entropy = a.up_entropy ? a.entropy_in[row] : 0.0f;
         const bool zeros = (up == 0.0f && up_entropy == 0.0f) || lse == -kInf;
-        // p = 2^z 2^-off, ln p = ln 2 (z - off)
         const Scale scale(lse);
-        const float less = exp2_fast(-scale.off);
-        float from = -(up + up_entropy * (entropy - kLn2 * scale.off)) * less, slope = -up_entropy * kLn2 * less;
-        if (t >= (int64_t)a.num_sym || !(lse == lse)) from = __builtin_nanf("");
+        Descent d(scale, 1.0f, 0.0f, entropy, up, up_entropy);
+        if (t >= (int64_t)a.num_sym || !(lse == lse)) d.from = __builtin_nanf("");
         Raw<T> x[kPer];
         r.load((const T *)a.x + row * a.stride, begin, end, x);
         T *grad = (T *)a.grad + row * a.grad_stride;
         const bool in = t >= 0 && t < (int64_t)a.num_sym;
+        scale.by_power([&](auto apart) {
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) {
-            const uint32_t column = r.column(q, begin, end);
-            put_gradient(x[q], Row::address(grad, column, begin, end), column, r.twice(q, begin, end), scale, from, slope, in, t, up, zeros);
-        }
+            for (int q = 0; q < kPer; ++q) {
+                const uint32_t column = r.column(q, begin, end);
+                put_gradient<apart.value>(x[q], Row::address(grad, column, begin, end), column, r.twice(q, begin, end), scale, d, in, t, up, zeros);
+            }
+        });
     }
 }
 
@@ -596,25 +624,24 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitsArgs a)
         const bool in = t >= 0 && t < (int64_t)a.num_sym;
         float largest = -kInf;
         for (uint32_t j = 0; j < a.num_sym; ++j) largest = fmaxf(largest, widen(x[j]));
-        const Scale scale(kGrad ? a.lse_in[row] : largest);
-        float up = 0.0f, up_entropy = 0.0f, from, slope;
+        const float known = kGrad ? a.lse_in[row] : largest, center = known == -kInf ? 0.0f : known;
+        const auto power = [&](float v) { return (v - center) * kLog2e; };
+        float up = 0.0f, up_entropy = 0.0f, total = 1.0f, log_total = 0.0f, entropy = 0.0f;
         if (kTrain || kGrad) {
             up = t < 0 ? 0.0f : a.up_logp[row];
             up_entropy = a.up_entropy ? a.up_entropy[row] : 0.0f;
         }
         bool zeros = up == 0.0f && up_entropy == 0.0f, spoilt = t >= (int64_t)a.num_sym;
         if constexpr (kGrad) {
-            const float less = exp2_fast(-scale.off), entropy = a.up_entropy ? a.entropy_in[row] : 0.0f;
-            from = -(up + up_entropy * (entropy - kLn2 * scale.off)) * less;
-            slope = -up_entropy * kLn2 * less;
-            zeros |= scale.max == -kInf;
-            spoilt |= !(scale.max == scale.max);
+            if (a.up_entropy) entropy = a.entropy_in[row];
+            zeros |= known == -kInf;
+            spoilt |= !(known == known);
         } else {
             Tally tally = {largest, 0.0f, 0.0f};
             float first = 0.0f, rest = 0.0f;  // the largest's power and the others', apart: a nearly certain symbol's ln p is the others'
             bool met = false;
             for (uint32_t j = 0; j < a.num_sym; ++j) {
-                const float v = widen(x[j]), z = scale.power(v), e = exp2_fast(z);
+                const float v = widen(x[j]), z = power(v), e = exp2_fast(z);
                 const bool it = v == largest && !met;
                 met |= it;
                 it ? first = e : rest += e;
@@ -622,7 +649,7 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitsArgs a)
             }
             tally.total = first + rest;
             Law law(tally);
-            if (law.max > -kInf) law.log_total = log1pf(rest / first);
+            if (law.max > -kInf) law.log_total = log1pf(rest);
             if (a.entropy) a.entropy[row] = law.entropy;
             if (a.lse) a.lse[row] = law.lse();
             if (a.logp) a.logp[row] = t < 0 ? 0.0f : spoilt ? __builtin_nanf("") : law.logp(widen(x[t]));
@@ -636,16 +663,16 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitsArgs a)
                 below = best;
                 put_alternative(a, law, row, k, best);
             }
-            from = -(up + up_entropy * (law.entropy - logf(law.total))) / law.total;
-            slope = -up_entropy * kLn2 / law.total;
+            total = law.total, log_total = law.log_total, entropy = law.entropy;
             zeros |= law.max == -kInf;
             spoilt |= !(law.max == law.max);
         }
         if constexpr (kTrain || kGrad) {
+            float from = -(up + up_entropy * (entropy - log_total)) / total, slope = -up_entropy * kLn2 / total;
             if (spoilt) from = __builtin_nanf("");
             T *grad = (T *)a.grad + row * a.grad_stride;
             for (uint32_t j = 0; j < a.num_sym; ++j) {
-                const float z = fmaxf(scale.power(widen(x[j])), kLeast);
+                const float z = fmaxf(power(widen(x[j])), kLeast);
                 float d = exp2_fast(z) * __builtin_fmaf(slope, z, from);
                 if (in && (int64_t)j == t) d += up;
                 grad[j] = (T)(zeros ? 0.0f : d);

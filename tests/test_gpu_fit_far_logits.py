@@ -110,3 +110,40 @@ def test_parts_of_a_row_whose_largest_values_are_far_apart(dtype, rows, n):
     if rows > 100 or n <= 5000:         # rows that one launch takes as a whole
         c.train()
         c.train(with_entropy=False, in_place=True)
+
+
+FAR = {"f32": [1e5, 2.0 ** 20, 3e6, 1e8, 1e9, 1e10, 1e20, 1e30, 9e37, 3e38], "bf16": [1e5, 2.0 ** 20, 3e6, 1e8, 1e9, 1e10, 1e20, 1e30, 9e37, 3e38],
+       "f16": [500.0, 30000.0, 65000.0]}
+
+
+def far_rows(rng, n, sizes):
+    """For each size and sign: a row of that number, one spread about it, one that has it among ordinary logits here and there,
+    one that is half it and half -inf."""
+    rows = []
+    for base in [s * sign for s in sizes for sign in (1, -1)]:
+        rows += [np.full(n, base), base + rng.normal(size=n) * 3, np.where(rng.random(n) < 0.3, rng.normal(size=n) * 3, base),
+                 np.where(np.arange(n) % 2, -np.inf, base)]
+    return np.stack(rows)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n", [2, 3, 5, 7, 64, 256, 999, 5000, 20000, 131073])
+def test_finite_logits_far_from_zero(dtype, n):
+    """Infinities and what is no number come from logits that are so, not from large ones."""
+    rng = np.random.default_rng(n)
+    v = far_rows(rng, n, FAR[dtype])
+    c = Rows(v, 2 * rng.integers(0, (n + 1) // 2, len(v)), TYPES[dtype])
+    c.forward(alternatives=n < 1000)
+    c.gradient()
+    if n <= 5000:                       # rows that one launch takes as a whole
+        c.train()
+        c.train(with_entropy=False, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_training_on_many_long_rows_far_from_zero(dtype):
+    """Rows that a workgroup of sixteen wavefronts takes as a whole, more than half as many as compute units."""
+    rng = np.random.default_rng(1)
+    v = np.concatenate([far_rows(rng, 20001, FAR[dtype]), far_rows(rng, 20001, FAR[dtype])])
+    c = Rows(v, 2 * rng.integers(0, 10000, len(v)), TYPES[dtype])
+    c.train()
