@@ -367,7 +367,9 @@ int pilc_logprobs(const pilc_logits_shape *shape, const void *logits_dev, const 
 /* The gradient of sum_r up_logp[r] logp[r] + up_entropy[r] entropy[r] by the logits:
  *   grad_j = a (1[j = t] - p_j) - b p_j (ln p_j + entropy),  a = up_logp[r] (0 where the target does
  * not count), b = up_entropy[r].
- *   lse_dev, entropy_dev   f32 [rows], from pilc_logprobs
+ *   lse_dev, entropy_dev   f32 [rows], from pilc_logprobs.  p is what this lse, in its 32 bits, says:
+ *                          a |lse| 2^-24th of it is lost, which logits that lie far from zero show;
+ *                          pilc_logprobs_train loses nothing to it
  *   up_logp_dev            f32 [rows]
  *   up_entropy_dev         f32 [rows]; NULL: no such term, entropy_dev is then not read
  *   grad_dev               [rows, num_sym] of the logits' type, row r at r * grad_stride; may be the

@@ -18,6 +18,7 @@ struct LogitsArgs {
     int32_t *top_sym;
     float *top_logp;
     const float *lse_in, *entropy_in, *up_logp, *up_entropy;
+    float4 *law;  // of each row for k_logits_grad: its largest, total, log_total, entropy (see Law)
     void *grad;
     uint64_t stride, grad_stride;
     uint32_t rows, num_sym, top, target_type;
@@ -112,6 +113,7 @@ struct Law {
         if (!(log_total == log_total)) max = entropy = log_total;
     }
     __device__ float lse() const { return max + log_total; }
+    __device__ float4 kept() const { return make_float4(max, total, log_total, entropy); }
     __device__ float logp(float x) const { return max == -kInf ? -kInf : (x - max) - log_total; }
 };
 
@@ -451,6 +453,7 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
             if (r.lane == 0) {
                 if (a.entropy) a.entropy[row] = law.entropy;
                 if (a.lse) a.lse[row] = law.lse();
+                if (!kTrain && a.law) a.law[row] = law.kept();
                 if (a.logp && (t < 0 || t >= (int64_t)a.num_sym)) a.logp[row] = t < 0 ? 0.0f : __builtin_nanf("");
             }
             const bool in = t >= 0 && t < (int64_t)a.num_sym;
@@ -548,6 +551,7 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type
         if (thread == 0) {
             if (a.entropy) a.entropy[row] = law.entropy;
             if (a.lse) a.lse[row] = law.lse();
+            if (a.law) a.law[row] = law.kept();
             if (a.logp) {
                 const int64_t target = target_of(a, (uint32_t)row);
                 float at = 0.0f;
@@ -582,7 +586,8 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type
 }
 
 // The gradient where a row's law is known: run by run, 16 KB at most, read once and written once.  Memory bounds it: 8190 x
-// 50001 f16 275 us (5.9 TB/s).
+// 50001 f16 275 us (5.9 TB/s).  A caller's law is an lse and an entropy; pilc_logprobs_train leaves largest value and total apart,
+// as an lse of 32 bits has a 2^-24th of its size less to say about p.
 template <class T, int kLanes, int kPer>
 __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logits_grad(LogitsArgs a)
 {
@@ -594,11 +599,11 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_logi
         const uint32_t end = min(begin + a.span, a.num_sym);
         const int64_t t = target_of(a, row);
         const float up = t < 0 ? 0.0f : a.up_logp[row], up_entropy = a.up_entropy ? a.up_entropy[row] : 0.0f;
-        const float lse = a.lse_in[row], entropy = a.up_entropy ? a.entropy_in[row] : 0.0f;
-        const bool zeros = (up == 0.0f && up_entropy == 0.0f) || lse == -kInf;
-        const Scale scale(lse);
-        Descent d(scale, 1.0f, 0.0f, entropy, up, up_entropy);
-        if (t >= (int64_t)a.num_sym || !(lse == lse)) d.from = __builtin_nanf("");
+        const float4 law = a.law ? a.law[row] : make_float4(a.lse_in[row], 1.0f, 0.0f, a.up_entropy ? a.entropy_in[row] : 0.0f);
+        const bool zeros = (up == 0.0f && up_entropy == 0.0f) || law.x == -kInf;
+        const Scale scale(law.x);
+        Descent d(scale, law.y, law.z, law.w, up, up_entropy);
+        if (t >= (int64_t)a.num_sym || !(law.x == law.x)) d.from = __builtin_nanf("");
         Raw<T> x[kPer];
         r.load((const T *)a.x + row * a.stride, begin, end, x);
         T *grad = (T *)a.grad + row * a.grad_stride;
@@ -733,8 +738,8 @@ static size_t logits_workspace(const pilc_logits_shape &s)
     size_t most = 256;
     for (uint32_t value : {2u, 4u}) {  // whatever the type, so that a caller need not ask for each
         const LogitsPlan p = logits_plan(s.rows, s.num_sym, value, kWholeRow, kLongestRun, kShortestRun);
-        // pilc_logprobs_train, where it goes two ways, keeps lse and entropy behind the parts
-        const size_t kept = s.top == 0 && !train_by_row(s.rows, s.num_sym, value) ? 2 * sizeof(float) * (size_t)s.rows : 0;
+        // pilc_logprobs_train, where it goes two ways, keeps the rows' laws behind the parts
+        const size_t kept = s.top == 0 && !train_by_row(s.rows, s.num_sym, value) ? sizeof(float4) * (size_t)s.rows : 0;
         most = std::max(most, parts_bytes(p, s.rows, s.top) + kept);
     }
     return most;
@@ -923,16 +928,10 @@ int pilc_logprobs_train(const pilc_logits_shape *shape, const void *logits_dev, 
             return;
         }
         // too few rows to keep the GPU busy one a workgroup, or too long ones: the law first, then the gradient by it
-        LogitsArgs g = a;
-        if (!a.lse || !a.entropy) {  // kept behind the runs' parts where the caller does not want them
-            const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kWholeRow, kLongestRun, kShortestRun);
-            float *kept = (float *)((char *)workspace_dev + parts_bytes(p, a.rows, 0));
-            if (!a.lse) a.lse = kept;
-            if (!a.entropy) a.entropy = kept + a.rows;
-        }
+        const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kWholeRow, kLongestRun, kShortestRun);
+        a.law = (float4 *)((char *)workspace_dev + parts_bytes(p, a.rows, 0));
         launch_law<T>(a, shape->dtype, workspace_dev, stream);
-        g.lse_in = a.lse, g.entropy_in = a.entropy;
-        launch_grad<T>(g, stream);
+        launch_grad<T>(a, stream);
     });
 }
 

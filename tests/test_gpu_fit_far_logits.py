@@ -147,3 +147,22 @@ def test_training_on_many_long_rows_far_from_zero(dtype):
     v = np.concatenate([far_rows(rng, 20001, FAR[dtype]), far_rows(rng, 20001, FAR[dtype])])
     c = Rows(v, 2 * rng.integers(0, 10000, len(v)), TYPES[dtype])
     c.train()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,n", [(3, 40000), (30, 20001), (2, 131073), (130, 140000)])
+def test_training_in_two_launches_has_the_law_in_all_its_bits(dtype, rows, n):
+    """Few long rows, and rows that no workgroup takes as a whole: the same bounds as of those that one does."""
+    rng = np.random.default_rng(n)
+    base = np.array([0.0, 20.0, -1000.0, 30000.0, -65000.0] if dtype == "f16" else [0.0, -20.0, 100.0, 1000.0, 1e5, -1e7, -1e10, 1e30, 3e38])
+    v = rng.normal(size=(rows, n)) * 3 + base[np.arange(rows) % len(base)][:, None]
+    v[1::3] = blocks(rng, n, LOWEST[TYPES[dtype]], base[-1])
+    v[rows - 1] = LOWEST[TYPES[dtype]]
+    c = Rows(v, rng.integers(0, n, rows), TYPES[dtype])
+    c.train()
+    c.train(with_entropy=False, in_place=True)
+    on = lambda x: torch.from_numpy(x).to(DEV)  # noqa: E731
+    logp, grad = torch.empty(rows, device=DEV), torch.empty_like(c.x)
+    pb.pilc_logprobs_train(c.x, c.t, on(c.a), logp, grad, up_entropy=on(c.b), workspace=c.ws_train)       # lse and entropy not wanted
+    want, err = orc.logprobs_grad(c.x64, c.t64, c.a.astype(np.float64), c.b.astype(np.float64), apart=True)
+    close(grad, want, err, c.dtype, "training without lse and entropy: gradient")
