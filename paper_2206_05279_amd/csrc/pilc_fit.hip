@@ -8,6 +8,7 @@
 
 #include "pilc_fit_device.hpp"
 #include "pilc_host.hpp"
+#include "pilc_row_rules.hpp"
 
 #include "pilc_logprobs.hpp"
 #include "pilc_norm.hpp"

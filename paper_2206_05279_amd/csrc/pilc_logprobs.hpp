@@ -708,7 +708,6 @@ struct LogitsPlan {
     uint32_t splits, span;
 };
 constexpr uint32_t kWholeRow = 64 << 10, kLongestRun = 32 << 10, kShortestRun = 8 << 10;
-static uint32_t div_up(uint32_t a, uint32_t b) { return a / b + (a % b != 0); }
 static LogitsPlan logits_plan(uint32_t rows, uint32_t num_sym, uint32_t value, uint32_t whole, uint32_t longest, uint32_t shortest)
 {
     const uint32_t vec = 16 / value, needed = num_sym <= whole / value ? 1 : div_up(num_sym, longest / value), most = div_up(num_sym, shortest / value);

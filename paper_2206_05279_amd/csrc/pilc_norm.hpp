@@ -129,7 +129,7 @@ k_norm_forward_rows(NormArgs a)
     uint32_t row = blockIdx.x * Row::kRows + r.row_in_block;
     const uint32_t step = gridDim.x * Row::kRows, last = a.rows - 1;
     if (Row::kAhead) r.load((const T *)a.x + min(row, last) * a.x_stride, x);
-    for (; row < a.rows; row += step) {
+    for (bool more = row < a.rows; more; more = next_row(row, step, last)) {
         if (Row::kAhead)
             r.load((const T *)a.x + (last - row > step ? row + step : last) * a.x_stride, next);
         else
@@ -190,7 +190,7 @@ k_norm_backward_rows(NormArgs a)
         r.load((const T *)a.dy + of * a.y_stride, to_dy);
     };
     if (Row::kAhead) fetch(min(row, last), mean, rstd, x, dy);
-    for (; row < a.rows; row += step) {
+    for (bool more = row < a.rows; more; more = next_row(row, step, last)) {
         if (Row::kAhead)
             fetch(last - row > step ? row + step : last, next_mean, next_rstd, next_x, next_dy);
         else
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(kNormLongThreads) void k_norm_forward_long(NormArgs
     constexpr int kWaves = kNormLongThreads / 64;
     __shared__ float room[kWaves];
     const W *weight = (const W *)a.weight, *bias = (const W *)a.bias;
-    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *x = (const T *)a.x + row * a.x_stride;
         T *y = (T *)a.y + row * a.y_stride;
         float sum = 0.0f, square = 0.0f;
@@ -422,7 +422,7 @@ __global__ __launch_bounds__(kNormLongThreads) void k_norm_dx_long(NormArgs a)
     constexpr int kWaves = kNormLongThreads / 64;
     __shared__ float room[kWaves];
     const W *weight = (const W *)a.weight;
-    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *x = (const T *)a.x + row * a.x_stride, *dy = (const T *)a.dy + row * a.y_stride;
         T *dx = (T *)a.dx + row * a.dx_stride;
         const float mean = a.mean_in[row], rstd = a.rstd_in[row];
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_parts(NormArgs a)
     const uint32_t column = min(place, a.width - kVec);
     float dw[kVec] = {}, db[kVec] = {};
 #pragma unroll 4
-    for (uint32_t row = blockIdx.y; row < a.rows; row += a.num_parts) {
+    for (uint64_t row = blockIdx.y; row < a.rows; row += a.num_parts) {
         const auto tx = pack_at<kVec>((const T *)a.x + row * a.x_stride + column), td = pack_at<kVec>((const T *)a.dy + row * a.y_stride + column);
         const float mean = a.mean_in[row], rstd = a.rstd_in[row];
 #pragma unroll
@@ -542,7 +542,7 @@ static uint32_t narrow_blocks(uint32_t rows) { return std::min(div_up(rows, kNor
 template <class Row>
 static uint32_t norm_blocks(uint32_t rows, int most_waves)
 {
-    return std::min((rows + Row::kRows - 1) / Row::kRows, compute_units() * (uint32_t)(Row::waves(most_waves) * 256 / Row::kThreads));
+    return std::min(div_up(rows, Row::kRows), compute_units() * (uint32_t)(Row::waves(most_waves) * 256 / Row::kThreads));
 }
 // Workgroups of the backward pass.  With weights' gradients each puts down a part, as much as two rows in 32 bits, so that few
 // rows are shared out by four, once half the compute units have one (4096 columns bf16, us with a row and with four a workgroup:
@@ -550,7 +550,7 @@ static uint32_t norm_blocks(uint32_t rows, int most_waves)
 template <class Row>
 static uint32_t norm_backward_blocks(uint32_t rows, bool with_parts)
 {
-    const uint32_t blocks = (rows + Row::kRows - 1) / Row::kRows, most = norm_blocks<Row>(rows, kNormBackwardWaves);
+    const uint32_t blocks = div_up(rows, Row::kRows), most = norm_blocks<Row>(rows, kNormBackwardWaves);
     return with_parts ? std::min(most, std::max(compute_units() / 2, blocks / 4)) : most;
 }
 // The most parts of any of the ways below: rows too long for kKeep go by kNormLongParts, the others by workgroups that are all
