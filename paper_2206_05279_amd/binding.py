@@ -477,6 +477,21 @@ def _rows(t: torch.Tensor, dtype, rows: int, width: int, device: int, what: str)
     return t.data_ptr(), across
 
 
+def _held(n: int, bits: int, what: str) -> int:
+    """n, which a field of `bits` bits has to hold: ctypes would keep the low ones of a larger number without a word."""
+    if not 0 <= n < 1 << bits:
+        raise PilcError(PILC_E_ARG, "%s = %d" % (what, n))
+    return n
+
+
+def _logits_shape(rows: int, num_sym: int, stride: int, kind: int, target_kind: int, top: int) -> pilc_logits_shape:
+    return pilc_logits_shape(_held(rows, 32, "rows"), _held(num_sym, 32, "num_sym"), stride, kind, target_kind, _held(top, 32, "top"))
+
+
+def _norm_shape(rows: int, width: int, x_stride: int, y_stride: int, dx_stride: int, kind: int, weight_kind: int, eps: float) -> pilc_norm_shape:
+    return pilc_norm_shape(_held(rows, 32, "rows"), _held(width, 32, "width"), x_stride, y_stride, dx_stride, kind, weight_kind, eps)
+
+
 def _raw_stream(stream: Optional[torch.cuda.Stream], device: int) -> int:
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
@@ -488,11 +503,11 @@ def _logits(logits: torch.Tensor, targets: Optional[torch.Tensor], top: int, dev
     rows, num_sym = logits.shape
     ptr, stride = _rows(logits, logits.dtype, rows, num_sym, device, "logits")
     if targets is None:
-        return pilc_logits_shape(rows, num_sym, stride, kind, 0, top), ptr, None
+        return _logits_shape(rows, num_sym, stride, kind, 0, top), ptr, None
     t_kind = _SYMBOLS.get(targets.dtype)
     if t_kind is None:
         _bad("targets", "uint8, int32 or int64")
-    return (pilc_logits_shape(rows, num_sym, stride, kind, t_kind, top), ptr,
+    return (_logits_shape(rows, num_sym, stride, kind, t_kind, top), ptr,
             _vector(targets, targets.dtype, rows, device, "targets"))
 
 
@@ -504,7 +519,7 @@ def _workspace(workspace: torch.Tensor, device: int) -> Tuple[int, int]:
 def pilc_logprobs_workspace_size(rows: int, num_sym: int, top: int = 0) -> int:
     """Bytes of workspace that pilc_logprobs and pilc_logprobs_train need for any type of logits."""
     n = C.c_size_t(0)
-    shape = pilc_logits_shape(int(rows), int(num_sym), int(num_sym), 0, 0, int(top))
+    shape = _logits_shape(int(rows), int(num_sym), int(num_sym), 0, 0, int(top))
     rc = lib().pilc_logprobs_workspace_size(C.byref(shape), C.byref(n))
     if rc != PILC_OK:
         raise PilcError(rc, "pilc_logprobs_workspace_size")
@@ -581,7 +596,7 @@ def pilc_norm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-
     rows, width = x.shape
     xp, xs = _rows(x, own, rows, width, dev, "x")
     yp, ys = _rows(y, own, rows, width, dev, "y")
-    shape = pilc_norm_shape(rows, width, xs, ys, 0, _VALUES[own], _VALUES[kind], eps)
+    shape = _norm_shape(rows, width, xs, ys, 0, _VALUES[own], _VALUES[kind], eps)
     rc = lib().pilc_norm_forward(C.byref(shape), xp, _vector(weight, kind, width, dev, "weight"), _vector(bias, kind, width, dev, "bias"),
                                  yp, _vector(mean, f32, rows, dev, "mean"), _vector(rstd, f32, rows, dev, "rstd"),
                                  _raw_stream(stream, dev))
@@ -593,7 +608,7 @@ def pilc_norm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-
 def pilc_norm_workspace_size(rows: int, width: int) -> int:
     """Bytes of workspace that pilc_norm_backward needs for any types."""
     n = C.c_size_t(0)
-    shape = pilc_norm_shape(int(rows), int(width), int(width), int(width), int(width), 0, 0, 0.0)
+    shape = _norm_shape(int(rows), int(width), int(width), int(width), int(width), 0, 0, 0.0)
     rc = lib().pilc_norm_workspace_size(C.byref(shape), C.byref(n))
     if rc != PILC_OK:
         raise PilcError(rc, "pilc_norm_workspace_size")
@@ -609,7 +624,7 @@ def pilc_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=N
     xp, xs = _rows(x, own, rows, width, dev, "x")
     dyp, dys = _rows(dy, own, rows, width, dev, "dy")
     dxp, dxs = _rows(dx, own, rows, width, dev, "dx") if dx is not None else (None, width)
-    shape = pilc_norm_shape(rows, width, xs, dys, dxs, _VALUES[own], _VALUES[kind], 0.0)
+    shape = _norm_shape(rows, width, xs, dys, dxs, _VALUES[own], _VALUES[kind], 0.0)
     rc = lib().pilc_norm_backward(C.byref(shape), dyp, xp, _vector(weight, kind, width, dev, "weight"),
                                   _vector(mean, f32, rows, dev, "mean"), _vector(rstd, f32, rows, dev, "rstd"), dxp,
                                   _vector(dweight, kind, width, dev, "dweight"), _vector(dbias, kind, width, dev, "dbias"),
@@ -660,7 +675,7 @@ def pilc_adamw_step(tensors: AdamwTensors, lr: float, beta1: float, beta2: float
     dev = tensors.device
     if dev != torch.cuda.current_device():
         _bad("tensors", "those of a list made")
-    par = pilc_adamw_params(lr, beta1, beta2, eps, grad_scale, step, tensors.param_type, tensors.grad_type, tensors.state_bits,
+    par = pilc_adamw_params(lr, beta1, beta2, eps, grad_scale, _held(step, 64, "step"), tensors.param_type, tensors.grad_type, tensors.state_bits,
                             dither & 0xFFFFFFFF)
     rc = lib().pilc_adamw_step(C.byref(par), tensors.records, len(tensors.records), _raw_stream(stream, dev))
     if check and rc != PILC_OK:
