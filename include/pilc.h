@@ -448,7 +448,8 @@ typedef struct {
 /* One step over `num_tensors` tensors (tensors_host is read before the call returns):
  *   g = grad grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *   param = param (1 - lr decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
- * with the new m and v as they are before they are put into 8 bits.
+ * with the new m and v as they are before they are put into 8 bits.  PILC_E_ARG for numbers that 32 bits
+ * do not hold: eps, grad_scale, lr lr_mult / (1 - beta1^step), 1 - lr lr_mult decay.
  *
  * State in 8 bits: 256 values in a row share a scale 2^(e-126), e the exponent field of the
  * largest of them (at least 1), held as a byte; e = 255 says that the block is not finite, its

@@ -249,14 +249,18 @@ static uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
 static bool adamw_ok(const pilc_adamw_params *h, const pilc_adamw_tensor *t, uint32_t num)
 {
-    const auto fine = [](double v) { return v >= 0.0 && v < (double)kInf; };
+    constexpr double kMost = 3.4028234663852886e38;  // of 32 bits, in which the kernels have them
+    const auto held = [](double v) { return v >= -kMost && v <= kMost; };
+    const auto fine = [](double v) { return v >= 0.0 && v <= kMost; };
     if (!h || (num && !t) || !fine(h->lr) || !fine(h->eps) || !(h->beta1 >= 0.0 && h->beta1 < 1.0) || !(h->beta2 >= 0.0 && h->beta2 < 1.0) ||
-        !std::isfinite(h->grad_scale) || h->step < 1 || h->param_type > PILC_F16 || h->grad_type > PILC_F16 ||
+        !held(h->grad_scale) || h->step < 1 || h->param_type > PILC_F16 || h->grad_type > PILC_F16 ||
         (h->state_bits != 32 && h->state_bits != 8))
         return false;
+    const double c1 = 1.0 - std::pow(h->beta1, (double)h->step);
     for (uint32_t k = 0; k < num; ++k) {
         const pilc_adamw_tensor &x = t[k];
-        if (!std::isfinite(x.lr_mult) || !std::isfinite(x.decay)) return false;
+        const double lr = h->lr * x.lr_mult;
+        if (!std::isfinite(x.lr_mult) || !std::isfinite(x.decay) || !held(lr / c1) || !held(1.0 - lr * x.decay)) return false;
         if (x.count == 0) continue;
         const size_t state = h->state_bits == 32 ? 4 : 1;
         if (!x.param || !x.grad || !x.m || !x.v || !aligned_to(x.param, value_bytes(h->param_type)) ||
