@@ -437,7 +437,7 @@ typedef struct {
 } pilc_adamw_tensor;
 
 typedef struct {
-    double lr, beta1, beta2, eps; /* 0 <= beta < 1, eps >= 0                                */
+    double lr, beta1, beta2, eps; /* 0 <= beta < 1, eps >= 0 (above 0 it counts as 2^-126 at least) */
     double grad_scale;            /* the gradients are multiplied by it                     */
     uint64_t step;                /* of this step, from 1                                   */
     uint32_t param_type, grad_type;

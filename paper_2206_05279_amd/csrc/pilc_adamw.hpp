@@ -282,7 +282,8 @@ int pilc_adamw_step(const pilc_adamw_params *params_host, const pilc_adamw_tenso
     const pilc_adamw_params &h = *params_host;
     AdamwArgs a = {};
     a.b1 = (float)h.beta1, a.b1_rest = (float)(1.0 - h.beta1), a.b2 = (float)h.beta2, a.b2_rest = (float)(1.0 - h.beta2);
-    a.grad_scale = (float)h.grad_scale, a.eps = (float)h.eps, a.dither = h.dither;
+    a.grad_scale = (float)h.grad_scale, a.dither = h.dither;
+    a.eps = h.eps > 0.0 ? std::max((float)h.eps, 0x1p-126f) : 0.0f;  // the hardware's reciprocal of less is infinite
     const double c1 = 1.0 - std::pow(h.beta1, (double)h.step), c2 = 1.0 - std::pow(h.beta2, (double)h.step);
     a.root_scale = (float)(1.0 / std::sqrt(c2));
     uint64_t blocks = 0;
