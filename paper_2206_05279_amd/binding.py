@@ -477,19 +477,19 @@ def _rows(t: torch.Tensor, dtype, rows: int, width: int, device: int, what: str)
     return t.data_ptr(), across
 
 
-def _held(n: int, bits: int, what: str) -> int:
-    """n, which a field of `bits` bits has to hold: ctypes would keep the low ones of a larger number without a word."""
-    if not 0 <= n < 1 << bits:
-        raise PilcError(PILC_E_ARG, "%s = %d" % (what, n))
-    return n
+_OVER = 1 << 32     # a field of 32 bits; ctypes would keep the low ones of a larger number without a word
 
 
 def _logits_shape(rows: int, num_sym: int, stride: int, kind: int, target_kind: int, top: int) -> pilc_logits_shape:
-    return pilc_logits_shape(_held(rows, 32, "rows"), _held(num_sym, 32, "num_sym"), stride, kind, target_kind, _held(top, 32, "top"))
+    if not (0 <= rows < _OVER and 0 <= num_sym < _OVER and 0 <= top < _OVER):
+        raise PilcError(PILC_E_ARG, "%d rows of %d logits with %d alternatives" % (rows, num_sym, top))
+    return pilc_logits_shape(rows, num_sym, stride, kind, target_kind, top)
 
 
 def _norm_shape(rows: int, width: int, x_stride: int, y_stride: int, dx_stride: int, kind: int, weight_kind: int, eps: float) -> pilc_norm_shape:
-    return pilc_norm_shape(_held(rows, 32, "rows"), _held(width, 32, "width"), x_stride, y_stride, dx_stride, kind, weight_kind, eps)
+    if not (0 <= rows < _OVER and 0 <= width < _OVER):
+        raise PilcError(PILC_E_ARG, "%d rows of %d values" % (rows, width))
+    return pilc_norm_shape(rows, width, x_stride, y_stride, dx_stride, kind, weight_kind, eps)
 
 
 def _raw_stream(stream: Optional[torch.cuda.Stream], device: int) -> int:
@@ -675,7 +675,9 @@ def pilc_adamw_step(tensors: AdamwTensors, lr: float, beta1: float, beta2: float
     dev = tensors.device
     if dev != torch.cuda.current_device():
         _bad("tensors", "those of a list made")
-    par = pilc_adamw_params(lr, beta1, beta2, eps, grad_scale, _held(step, 64, "step"), tensors.param_type, tensors.grad_type, tensors.state_bits,
+    if not 0 <= step < 1 << 64:
+        raise PilcError(PILC_E_ARG, "step %d" % step)
+    par = pilc_adamw_params(lr, beta1, beta2, eps, grad_scale, step, tensors.param_type, tensors.grad_type, tensors.state_bits,
                             dither & 0xFFFFFFFF)
     rc = lib().pilc_adamw_step(C.byref(par), tensors.records, len(tensors.records), _raw_stream(stream, dev))
     if check and rc != PILC_OK:

@@ -247,7 +247,8 @@ __global__ __launch_bounds__(256) void k_adamw_values(const uint8_t *__restrict_
 constexpr uint32_t kAdamwMostChunks = 1u << 20;  // a launch has fewer than 2^32 threads
 static uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-static bool adamw_ok(const pilc_adamw_params *h, const pilc_adamw_tensor *t, uint32_t num)
+// c1 to be: 1 - beta1^step
+static bool adamw_ok(const pilc_adamw_params *h, const pilc_adamw_tensor *t, uint32_t num, double &c1)
 {
     constexpr double kMost = 3.4028234663852886e38;  // of 32 bits, in which the kernels have them
     const auto held = [](double v) { return v >= -kMost && v <= kMost; };
@@ -256,11 +257,12 @@ static bool adamw_ok(const pilc_adamw_params *h, const pilc_adamw_tensor *t, uin
         !held(h->grad_scale) || h->step < 1 || h->param_type > PILC_F16 || h->grad_type > PILC_F16 ||
         (h->state_bits != 32 && h->state_bits != 8))
         return false;
-    const double c1 = 1.0 - std::pow(h->beta1, (double)h->step);
+    c1 = 1.0 - std::pow(h->beta1, (double)h->step);
+    const double most_lr = kMost * c1;
     for (uint32_t k = 0; k < num; ++k) {
         const pilc_adamw_tensor &x = t[k];
         const double lr = h->lr * x.lr_mult;
-        if (!std::isfinite(x.lr_mult) || !std::isfinite(x.decay) || !held(lr / c1) || !held(1.0 - lr * x.decay)) return false;
+        if (!(std::fabs(lr) <= most_lr) || !held(1.0 - lr * x.decay)) return false;  // nor where a factor is not finite
         if (x.count == 0) continue;
         const size_t state = h->state_bits == 32 ? 4 : 1;
         if (!x.param || !x.grad || !x.m || !x.v || !aligned_to(x.param, value_bytes(h->param_type)) ||
@@ -278,13 +280,14 @@ using namespace pilc;
 
 int pilc_adamw_step(const pilc_adamw_params *params_host, const pilc_adamw_tensor *tensors_host, uint32_t num_tensors, void *hip_stream)
 {
-    if (!adamw_ok(params_host, tensors_host, num_tensors)) return PILC_E_ARG;
+    double c1;
+    if (!adamw_ok(params_host, tensors_host, num_tensors, c1)) return PILC_E_ARG;
     const pilc_adamw_params &h = *params_host;
     AdamwArgs a = {};
     a.b1 = (float)h.beta1, a.b1_rest = (float)(1.0 - h.beta1), a.b2 = (float)h.beta2, a.b2_rest = (float)(1.0 - h.beta2);
     a.grad_scale = (float)h.grad_scale, a.dither = h.dither;
     a.eps = h.eps > 0.0 ? std::max((float)h.eps, 0x1p-126f) : 0.0f;  // the hardware's reciprocal of less is infinite
-    const double c1 = 1.0 - std::pow(h.beta1, (double)h.step), c2 = 1.0 - std::pow(h.beta2, (double)h.step);
+    const double c2 = 1.0 - std::pow(h.beta2, (double)h.step);
     a.root_scale = (float)(1.0 / std::sqrt(c2));
     uint64_t blocks = 0;
     const uint32_t chunk = h.state_bits == 32 ? kAdamwChunk : kAdamwBytesChunk;
