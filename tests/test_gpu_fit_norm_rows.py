@@ -1,11 +1,12 @@
-"""Layer norm over numbers of rows at the end of what the entry points take."""
+"""Layer norm over widths between those of test_gpu_fit_norm.py, over many narrow rows, and over as many rows as are counted."""
 import numpy as np
 import pytest
 import torch
 
-from fit_util import close, up
+from fit_util import TYPES, close, up
 from oracle import fit_oracle as orc
 from paper_2206_05279_amd import binding as pb
+from test_gpu_fit_norm import backward, forward, values
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -32,3 +33,35 @@ def test_as_many_rows_as_32_bits_count():
         assert all(bool((t[a:a + step] == t[-1]).all()) for a in range(0, rows, step))
     del x, dy, mean, rstd, ws
     torch.cuda.empty_cache()
+
+
+# rows that sixteen wavefronts hold as 32 values a lane, their weights read anew for each; 600: more than there are workgroups
+LONG = [(3, 16385, 0, 0), (2, 20000, 3, 5), (1, 24576, 0, 1), (2, 32767, 1, 0), (2, 32768, 0, 0), (600, 17001, 0, 0)]
+KINDS = [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32")]
+
+
+@pytest.mark.parametrize("dtype,wtype", KINDS)
+@pytest.mark.parametrize("rows,n,pad,shift", LONG)
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rows_of_sixteen_wavefronts(dtype, wtype, rows, n, pad, shift, in_place):
+    rng = np.random.default_rng(rows + n)
+    x, w = values(rng, rows, n), 1 + rng.normal(size=n) * 0.3
+    forward(x, w, rng.normal(size=n), TYPES[dtype], TYPES[wtype], pad=pad, shift=shift, in_place=in_place)
+    backward(rng.normal(size=(rows, n)), x, w, TYPES[dtype], TYPES[wtype], pad, shift, in_place=in_place)
+
+
+@pytest.mark.parametrize("wanted", [(True, False, False), (False, True, True), (False, False, True)])
+@pytest.mark.parametrize("n", [5, 20001])
+def test_what_is_wanted_of_narrow_and_of_long_rows(n, wanted):
+    rng = np.random.default_rng(n)
+    backward(rng.normal(size=(300, n)), values(rng, 300, n), None, torch.bfloat16, torch.bfloat16, wanted=wanted)
+
+
+@pytest.mark.parametrize("dtype,wtype", KINDS)
+@pytest.mark.parametrize("rows,n", [(100000, 5), (70000, 7), (66000, 1)])
+def test_many_rows_of_less_than_a_pack(dtype, wtype, rows, n):
+    """More rows than a workgroup a compute unit has threads: each goes on to another, and there is more than one part."""
+    rng = np.random.default_rng(n)
+    x, w = values(rng, rows, n), 1 + rng.normal(size=n) * 0.3
+    forward(x, w, rng.normal(size=n), TYPES[dtype], TYPES[wtype], in_place=n == 7)
+    backward(rng.normal(size=(rows, n)), x, w, TYPES[dtype], TYPES[wtype], in_place=n == 7)
