@@ -124,7 +124,7 @@ struct Descent {
 
     __device__ Descent(const Scale &scale, float total, float log_total, float entropy, float up, float up_entropy)
     {
-        const float each = exp2_fast(-scale.off) / total;
+        const float each = 1.0f / (exp2_fast(scale.off) * total);
         from = -(up + up_entropy * (entropy - log_total - kLn2 * scale.off)) * each;
         slope = -up_entropy * kLn2 * each;
     }
@@ -294,8 +294,9 @@ struct LogitsRow {
                 }
             });
         });
-        const float whole = lanes_reduce<kWithin>(total[0] + total[1], Sum()), less = exp2_fast(-scale.off);
-        Tally t = {max, whole * less, (lanes_reduce<kWithin>(inside[0] + inside[1], Sum()) - scale.off * whole) * less};
+        // the largest value's power is 2^off to the last bit, and by itself makes a total of 1
+        const float whole = lanes_reduce<kWithin>(total[0] + total[1], Sum()), first = exp2_fast(scale.off);
+        Tally t = {max, whole / first, (lanes_reduce<kWithin>(inside[0] + inside[1], Sum()) - scale.off * whole) * __builtin_amdgcn_rcpf(first)};
         if constexpr (kWaves > 1) {
             room += half * kWaves;
             if ((threadIdx.x & 63) == 0) room[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)] = t;

@@ -166,3 +166,27 @@ def test_training_in_two_launches_has_the_law_in_all_its_bits(dtype, rows, n):
     pb.pilc_logprobs_train(c.x, c.t, on(c.a), logp, grad, up_entropy=on(c.b), workspace=c.ws_train)       # lse and entropy not wanted
     want, err = orc.logprobs_grad(c.x64, c.t64, c.a.astype(np.float64), c.b.astype(np.float64), apart=True)
     close(grad, want, err, c.dtype, "training without lse and entropy: gradient")
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,n", [(300, 3), (300, 9), (100, 500), (20, 9000), (130, 40000), (4, 150000)])
+def test_the_only_symbol_that_can_occur_is_certain(dtype, rows, n):
+    """Its power over itself is 1, whatever the logit: ln p is 0 and lse the logit, to the last bit."""
+    rng = np.random.default_rng(n)
+    v, t = np.full((rows, n), -np.inf), rng.integers(0, n, rows)
+    size = np.exp(rng.uniform(-3, 10 if dtype == "f16" else 80, rows))
+    v[np.arange(rows), t] = size * rng.choice([-1, 1], rows)
+    x, _ = placed(v, TYPES[dtype])
+    want = up(x)[np.arange(rows), t]
+    ws = torch.empty(pb.pilc_logprobs_workspace_size(rows, n), dtype=torch.uint8, device=DEV)
+    logp, entropy, lse, a = (torch.ones(rows, device=DEV) for _ in range(4))
+    on = torch.from_numpy(t).to(DEV)
+    for k in range(2):
+        if k:
+            grad = torch.empty_like(x)
+            pb.pilc_logprobs_train(x, on, a, logp, grad, entropy=entropy, lse=lse, workspace=ws)
+            # a power, a product and a quotient
+            assert float(grad.abs().max()) <= 4 * orc.U and int((grad != 0).sum()) <= rows
+        else:
+            pb.pilc_logprobs(x, on, logp, entropy=entropy, lse=lse, workspace=ws)
+        assert (logp == 0).all() and np.array_equal(up(lse), want) and float(entropy.abs().max()) < 16 * orc.U
