@@ -65,3 +65,19 @@ def test_many_rows_of_less_than_a_pack(dtype, wtype, rows, n):
     x, w = values(rng, rows, n), 1 + rng.normal(size=n) * 0.3
     forward(x, w, rng.normal(size=n), TYPES[dtype], TYPES[wtype], in_place=n == 7)
     backward(rng.normal(size=(rows, n)), x, w, TYPES[dtype], TYPES[wtype], in_place=n == 7)
+
+
+def test_weights_gradients_of_the_widest_rows():
+    """More columns than one launch has threads for: 64 of them take 1024 threads."""
+    torch.cuda.empty_cache()
+    n = (1 << 28) + 72
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x, dy = (torch.randint(-8, 9, (1, n), generator=g, device=DEV, dtype=torch.int8).to(torch.bfloat16) for _ in range(2))
+    mean, rstd = torch.full((1,), 0.5, device=DEV), torch.full((1,), 2.0, device=DEV)
+    dw, db = torch.full((n,), 77.0, dtype=torch.bfloat16, device=DEV), torch.full((n,), 77.0, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(pb.pilc_norm_workspace_size(1, n), dtype=torch.uint8, device=DEV)
+    pb.pilc_norm_backward(dy, x, None, mean, rstd, None, dw, db, workspace=ws)
+    assert torch.equal(db, dy[0])
+    assert torch.equal(dw, (dy[0].float() * (2 * x[0].float() - 1)).to(torch.bfloat16))     # whole numbers up to 136
+    del x, dy, dw, db, ws
+    torch.cuda.empty_cache()
