@@ -474,6 +474,132 @@ int pilc_adamw_step(const pilc_adamw_params *params_host, const pilc_adamw_tenso
 int pilc_adamw_values(const uint8_t *code_dev, const uint8_t *scale_dev, uint64_t count, int is_signed,
                       float *values_dev, void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------
+ * From a network's last states to its logits, in 8 bits: matrices whose values share scales in
+ * blocks of 128, their product, the norm that answers in them, and the loss that teaches a small
+ * network a large one's laws.  What is said above of streams, alignment and rounding holds here.
+ * ------------------------------------------------------------------------------------------ */
+enum { PILC_E4M3 = 0, PILC_E5M2 = 1 }; /* types of 8-bit values: 4 bits of exponent, up to 448, no infinity; 5, up to 57344 */
+
+/* A matrix of 8-bit values, their rows dense.  A row's values 128 b .. 128 b + 127 (the last ones
+ * maybe fewer) are its block b, under a scale of its own with block_rows 1; with block_rows 128
+ * rows 128 a .. 128 a + 127 share theirs.  A scale is a byte e that stands for 2^(e - 127); e = 255
+ * says that the block is not finite, its values are NaN. */
+typedef struct {
+    void *code;            /* device, row r at r * stride bytes                               */
+    uint8_t *scale;        /* device, of row r and block b at r / block_rows * scale_stride + b */
+    uint64_t stride;       /* >= the row's values                                             */
+    uint64_t scale_stride; /* >= the row's blocks                                             */
+    uint32_t type;         /* PILC_E4M3, PILC_E5M2                                            */
+    uint32_t block_rows;   /* 1, 128                                                          */
+} pilc_block8;
+
+/* A matrix x [rows, width] into 8 bits: `out` [rows, width], `out_t` [width, rows] from its
+ * transpose, whose blocks go along x's columns (both hold the same values with block_rows 128);
+ * either may be NULL.  A block's scale is the smallest under which its largest value is 448 or
+ * 57344 at most (2^-127 at least); its values are rounded to the nearest under it, ties to even.  A
+ * block with a NaN or an infinity: e = 255, every code 0x7F.
+ * rows, width: 0: the call does nothing; up to 2^31 - 1.  Errors: PILC_E_ARG, PILC_E_HIP. */
+int pilc_block8_quantize(uint32_t rows, uint32_t width, const void *x_dev, uint64_t x_stride, uint32_t dtype,
+                         const pilc_block8 *out, const pilc_block8 *out_t, void *hip_stream);
+
+/* The values that a matrix in 8 bits stands for, [rows, width] of `dtype`, row r at r * stride.  Those
+ * beyond the type's range are infinities.  Errors: PILC_E_ARG, PILC_E_HIP. */
+int pilc_block8_values(uint32_t rows, uint32_t width, const pilc_block8 *in, void *values_dev, uint64_t stride,
+                       uint32_t dtype, void *hip_stream);
+
+/* Device workspace of pilc_block8_product for any types (at least 256).  Errors: PILC_E_ARG. */
+int pilc_block8_product_workspace_size(uint32_t rows, uint32_t cols, uint32_t depth, size_t *workspace_bytes_host);
+
+/* c = a b^T: c_ij = sum over k of a_ik b_jk, a [rows, depth], b [cols, depth], c [rows, cols] of `c_type`, row i at i *
+ * c_stride.  So a layer is states times weights [outputs, inputs]; its way back takes the weights
+ * transposed, and the weights' gradient both sides transposed (pilc_block8_quantize's out_t).
+ * Products are exact and sums go by 32 bits, in an order that the shape and the GPU's number of compute
+ * units fix, with one exception: where c is of 16 bits and rows are more than 64, products are added up in groups
+ * of eight with 13 bits below the largest one's power of two (up to 2^-13 of the sum of the products'
+ * sizes; a c of 16 bits is rounded by 2^-9 or 2^-12 of itself).  Products under 2^-126 may be lost.
+ * depth 0: c is 0.  Each of rows, cols, depth: up to 2^31 - 1.
+ * Errors: PILC_E_ARG, PILC_E_WORKSPACE, PILC_E_HIP. */
+int pilc_block8_product(uint32_t rows, uint32_t cols, uint32_t depth, const pilc_block8 *a, const pilc_block8 *b,
+                        void *c_dev, uint64_t c_stride, uint32_t c_type, void *workspace_dev, size_t workspace_bytes,
+                        void *hip_stream);
+
+/* rows x width values; strides between rows in elements, >= width. */
+typedef struct {
+    uint32_t rows;        /* 0: forward does nothing, backward's weight gradient is 0       */
+    uint32_t width;       /* 1 .. 2^31 - 1                                                  */
+    uint64_t x_stride;    /* of x; in the backward pass of h                                */
+    uint64_t add_stride;  /* of add; in the backward pass of dsum; looked at if there is one */
+    uint64_t sum_stride;  /* of sum; in the backward pass of dx; looked at if there is one  */
+    uint64_t y_stride;    /* of y; in the backward pass of dy; looked at if there is one    */
+    uint32_t dtype;       /* of all of them: PILC_F32, PILC_BF16, PILC_F16                  */
+    uint32_t weight_type; /* of weight and its gradient: dtype or PILC_F32                  */
+    float eps;            /* >= 0                                                           */
+} pilc_rms_shape;
+
+/* h = x + add, rounded to dtype (add_dev NULL: x), y = h rstd weight, rstd = 1 / sqrt(mean of h^2 + eps), over each row.
+ *   sum_dev     h; NULL: not wanted.  May be x_dev or add_dev (same stride)
+ *   y_dev       NULL: not wanted.  May be x_dev, where that is not sum_dev (same stride)
+ *   y8          y in 8 bits, [rows, width] with block_rows 1, by pilc_block8_quantize's rule from its 32
+ *               bits; NULL: not wanted
+ *   rstd_dev    f32 [rows]; NULL: not wanted
+ *   weight_dev  [width]; NULL: 1
+ * One of sum, y, y8, rstd at least is wanted.  Errors: PILC_E_ARG, PILC_E_HIP. */
+int pilc_rms_forward(const pilc_rms_shape *shape, const void *x_dev, const void *add_dev, const void *weight_dev,
+                     void *sum_dev, void *y_dev, const pilc_block8 *y8, float *rstd_dev, void *hip_stream);
+
+/* Device workspace of pilc_rms_backward (at least 256).  Errors: PILC_E_ARG. */
+int pilc_rms_workspace_size(const pilc_rms_shape *shape, size_t *workspace_bytes_host);
+
+/* With hh = h rstd and q = dy weight:
+ *   dx = rstd (q - hh mean of (q hh)) + dsum over each row, dweight = sum over rows of dy hh.
+ * dx is the gradient by x, and by add the same.  dsum_dev: what comes back through sum, NULL: nothing does.
+ * rstd_dev f32 [rows] from the forward pass; weight_dev NULL: 1.  dx_dev, dweight_dev: NULL: not wanted, one
+ * at least is.  dx_dev may be dy_dev or dsum_dev (same stride).  The sum over rows is taken in an order that the shape and
+ * the GPU's number of compute units fix.  Errors: PILC_E_ARG, PILC_E_WORKSPACE, PILC_E_HIP. */
+int pilc_rms_backward(const pilc_rms_shape *shape, const void *dy_dev, const void *h_dev, const void *weight_dev,
+                      const float *rstd_dev, const void *dsum_dev, void *dx_dev, void *dweight_dev,
+                      void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* rows x num_sym logits of a student, row r at r * stride elements, and what a teacher names for each row. */
+typedef struct {
+    uint32_t rows;      /* 0: the calls do nothing                                          */
+    uint32_t num_sym;   /* 1 .. 2^31 - 1                                                    */
+    uint64_t stride;    /* >= num_sym, in elements                                          */
+    uint32_t dtype;     /* of logits and gradient: PILC_F32, PILC_BF16, PILC_F16            */
+    uint32_t top;       /* symbols that the teacher names a row, 1 .. 128                   */
+    uint32_t rest;      /* 0, 1: see below                                                  */
+    float temperature;  /* > 0                                                              */
+} pilc_distill_shape;
+
+/* Device workspace of pilc_distill (at least 256).  Errors: PILC_E_ARG. */
+int pilc_distill_workspace_size(const pilc_distill_shape *shape, size_t *workspace_bytes_host);
+
+/* What a student's law p, the softmax of x / temperature over a row of logits x, loses against the laws q of a teacher who
+ * names some symbols only, in nats a row, and the gradient by x of sum_r up[r] loss[r].
+ *   sym_dev    int32 [rows, top] symbols; a negative one is no entry
+ *   value_dev  f32 [rows, top]; -inf: named, with q = 0
+ * rest 0: values are the teacher's logits (or ln p), q is the softmax of value / temperature over the row's entries:
+ *   loss = sum_i q_i (ln q_i - ln p_i), gradient up / temperature (p_j - q_j)
+ * rest 1: values are ln q as they are (as pilc_logprobs answers in top_logp), and what the entries leave of 1, Q = max(0, 1 -
+ *   sum q), stands against what the student leaves, P = the sum of p over symbols that are not named:
+ *   loss = sum_i q_i (ln q_i - ln p_i) + Q (ln Q - ln P), gradient up / temperature (p_j - q_j) where
+ *   symbol j is named, up / temperature p_j (1 - Q / P) where not
+ *   Q counts as 0 where the student has no other symbol.
+ * q ln q is 0 for q = 0.  A symbol named twice has both q's, and its two terms in the loss.
+ * A row without entries: loss and gradient are 0 whatever its logits are.  A symbol with q > 0 whose logit is -inf: loss +inf,
+ * the gradient as above.  A row whose logits are all -inf: gradient 0, loss +inf if there is a q > 0, else 0.  A row
+ * with entries and a NaN or +inf among its logits, among the entries' values or with a symbol >= num_sym: loss and gradient
+ * NaN, but where up is 0 the gradient is 0 whatever the row is.
+ *   loss_dev   f32 [rows]
+ *   up_dev     f32 [rows]; NULL if grad_dev is
+ *   grad_dev   [rows, num_sym] of the logits' type, row r at r * grad_stride; NULL: not wanted; may be the logits
+ *              themselves (same address and stride)
+ * Errors: PILC_E_ARG, PILC_E_WORKSPACE, PILC_E_HIP. */
+int pilc_distill(const pilc_distill_shape *shape, const void *logits_dev, const int32_t *sym_dev, const float *value_dev,
+                 const float *up_dev, float *loss_dev, void *grad_dev, uint64_t grad_stride, void *workspace_dev,
+                 size_t workspace_bytes, void *hip_stream);
+
 const char *pilc_strerror(int code);
 const char *pilc_last_hip_error(void); /* text of the last HIP failure on this thread */
 uint32_t pilc_version(void);

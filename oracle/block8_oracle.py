@@ -1,0 +1,222 @@
+"""Plain references in numpy for what lies between a network's last states and its laws: values in 8 bits under scales for blocks
+of 128, their product, the root-mean-square norm, distillation.
+
+Codes and scales are exact, from a table of what the codes stand for; the rest is computed in 64 bits from the definitions,
+and each function that a rounding analysis is made for also returns the bounds of what 32-bit arithmetic may be off.
+"""
+from __future__ import annotations
+
+import numpy as np
+
+from oracle.fit_oracle import U, chain
+
+BLOCK = 128
+
+
+def _table(kind):
+    """What codes 0 .. 127 stand for, NaN and inf among them."""
+    digits, bias = (3, 7) if kind == "e4m3" else (2, 15)
+    out = np.zeros(128)
+    for c in range(128):
+        e, m = c >> digits, c & ((1 << digits) - 1)
+        out[c] = (m / 2 ** digits) * 2.0 ** (1 - bias) if e == 0 else (1 + m / 2 ** digits) * 2.0 ** (e - bias)
+    if kind == "e4m3":
+        out[127] = np.nan
+    else:
+        out[124], out[125:] = np.inf, np.nan
+    return out
+
+
+TABLE = {k: _table(k) for k in ("e4m3", "e5m2")}
+MOST = {"e4m3": 448.0, "e5m2": 57344.0}
+
+
+def encode(v, kind):
+    """Codes of the values nearest to v (|v| <= MOST), the even code where two are as near."""
+    t = TABLE[kind][: 127 if kind == "e4m3" else 124]
+    size = np.abs(v)
+    hi = np.clip(np.searchsorted(t, size), 1, t.size - 1)
+    below, above = size - t[hi - 1], t[hi] - size
+    code = np.where((below < above) | ((below == above) & ((hi - 1) % 2 == 0)), hi - 1, hi)
+    return (code | np.where(np.signbit(v), 128, 0)).astype(np.uint8)
+
+
+def decode(codes, kind):
+    v = TABLE[kind][codes & 127]
+    return np.where(codes & 128, -v, v)
+
+
+def scale_of(largest, kind):
+    """The byte for a block whose largest value, by size, this is."""
+    if not np.isfinite(largest):
+        return 255
+    e = 0
+    while largest > MOST[kind] * 2.0 ** (e - 127):
+        e += 1
+    return e
+
+
+def _blocks(rows, width, block_rows):
+    for i in range(0, rows, block_rows):
+        for j in range(0, width, BLOCK):
+            yield i // block_rows, j // BLOCK, (slice(i, min(i + block_rows, rows)), slice(j, min(j + BLOCK, width)))
+
+
+def quantize(x, kind, block_rows):
+    """(codes, scales) of x [rows, width] in 64 bits."""
+    rows, width = x.shape
+    codes, scales = np.zeros(x.shape, np.uint8), np.zeros((-(-rows // block_rows), -(-width // BLOCK)), np.uint8)
+    for a, b, at in _blocks(rows, width, block_rows):
+        with np.errstate(invalid="ignore"):
+            scales[a, b] = scale_of(np.abs(x[at]).max(), kind)
+        codes[at] = 0x7F if scales[a, b] == 255 else encode(np.ldexp(x[at], 127 - int(scales[a, b])), kind)
+    return codes, scales
+
+
+def powers(scales, shape, block_rows):
+    """What each value's scale stands for."""
+    e = np.repeat(np.repeat(scales, block_rows, 0)[: shape[0]], BLOCK, 1)[:, : shape[1]]
+    return np.where(e == 255, np.nan, np.ldexp(1.0, e.astype(np.int64) - 127))
+
+
+def values(codes, scales, kind, block_rows):
+    return decode(codes, kind) * powers(scales, codes.shape, block_rows)
+
+
+def held_by(codes, scales, y, y_rel, kind):
+    """Whether codes and scales [rows, ..] are what 8 bits hold of numbers that are y but for a share y_rel [rows] of themselves:
+    each block's scale that of a largest value so near, each value within half a step."""
+    for a, b, at in _blocks(*y.shape, 1):
+        rel = float(y_rel[a])
+        largest = np.abs(y[at]).max()
+        byte = int(scales[a, b])
+        if byte not in (scale_of(largest * (1 - rel), kind), scale_of(largest * (1 + rel), kind)):
+            return False
+        z = np.abs(np.ldexp(y[at], 127 - byte)) * (1 + rel)
+        digits, low = (3, -6) if kind == "e4m3" else (2, -14)
+        step = 2.0 ** (np.maximum(np.floor(np.log2(np.maximum(z, 1e-300))), low) - digits)
+        if (np.abs(decode(codes[at], kind) - np.ldexp(y[at], 127 - byte)) > 0.5 * step + rel * z).any():
+            return False
+    return True
+
+
+def product(a, b, groups):
+    """(a b^T, bound of its error) of values in 64 bits.  Products of 8-bit values have 8 bits and are exact; sums in 32 bits by
+    the matrix unit, 32 products at a time, may lose a unit of all their sizes at each of depth / 32 steps and 40 more.  With
+    `groups`, products of each eight are cut 2^-13 below the power of two of the largest before that."""
+    depth = a.shape[1]
+    c = a @ b.T
+    sizes = np.abs(a) @ np.abs(b).T
+    err = 2 * U * (depth / 32 + 40) * sizes + 2.0 ** -126 * depth
+    if groups:
+        a8 = np.pad(np.abs(a), ((0, 0), (0, -depth % 8))).reshape(a.shape[0], -1, 8)
+        b8 = np.pad(np.abs(b), ((0, 0), (0, -depth % 8))).reshape(b.shape[0], -1, 8)
+        for i in range(a.shape[0]):
+            err[i] += 8 * 2.0 ** -13 * (a8[i][None] * b8).max(2).sum(1)
+    return c, err
+
+
+def rms_forward(h, weight, eps):
+    """(y, rstd, share of y, of rstd that they may be off)."""
+    n = h.shape[1]
+    mean = (h * h).mean(1)
+    rstd = 1 / np.sqrt(mean + eps)
+    w = np.ones(n) if weight is None else weight
+    rel = np.full(h.shape[0], 0.5 * U * (chain(n) + 8) + 6 * U)
+    return h * rstd[:, None] * w, rstd, rel + 4 * U, rel
+
+
+def rms_backward(dy, h, weight, rstd, dsum):
+    """(dx, dweight, bounds of their errors)."""
+    rows, n = h.shape
+    w = np.ones(n) if weight is None else weight
+    hh, q = h * rstd[:, None], dy * w
+    along = (q * hh).mean(1, keepdims=True)
+    core = rstd[:, None] * (q - hh * along)
+    extra = 0 if dsum is None else dsum
+    along_err = U * (chain(n) + 8) * np.abs(q * hh).mean(1, keepdims=True)
+    err = np.abs(rstd[:, None]) * (8 * U * (np.abs(q) + np.abs(hh * along)) + np.abs(hh) * along_err) + U * np.abs(core + extra)
+    return core + extra, (dy * hh).sum(0), err, U * (rows + 12) * np.abs(dy * hh).sum(0)
+
+
+def distill(x, sym, value, up, temperature, rest):
+    """(loss, gradient, bounds of their errors) a row; up None: no gradient."""
+    rows, n = x.shape
+    loss, loss_err, g, g_err = np.zeros(rows), np.zeros(rows), np.zeros((rows, n)), np.zeros((rows, n))
+    for r in range(rows):
+        s, v = sym[r][sym[r] >= 0], value[r][sym[r] >= 0]
+        a = 0.0 if up is None else float(up[r])
+        if s.size == 0:
+            continue
+        bad = (s >= n).any() or np.isnan(v).any() or (v == np.inf).any() or np.isnan(x[r]).any() or (x[r] == np.inf).any()
+        if bad:
+            loss[r] = np.nan
+            g[r] = np.nan if a != 0 else 0.0
+            continue
+        z = x[r] / temperature
+        big = z.max()
+        lawless = big == -np.inf
+        there = z > -np.inf
+        far = np.where(there, big - np.where(there, z, 0), 0)        # sizes of the distances to the largest
+        e = np.where(there, np.exp(-far), 0.0)
+        log_total = np.log(e.sum()) if not lawless else 0.0
+        p = e / max(e.sum(), 1e-300)
+        log_p = np.where(there, -far - log_total, -np.inf)
+        top_v = v[v > -np.inf].max() if (v > -np.inf).any() else 0.0
+        t = np.where(v > -np.inf, v if rest else (v - top_v) / temperature, -np.inf)
+        q = np.exp(t)
+        log_q = t
+        # of a power: its exponent's subtraction, its factor and what that rounds, four units of the exponent, and two of its own
+        q_rel = U * (6 * np.where(q > 0, np.abs(t), 0) + 10)
+        q_sum_rel = U * (chain(s.size) + 4) + (q * q_rel).sum() / max(q.sum(), 1e-300)
+        if not rest and q.sum() > 0:
+            log_q = t - np.log(q.sum())
+            q = q / q.sum()
+            q_rel = q_rel + q_sum_rel + 3 * U
+        p_rel = U * (6 * far + 4)
+        total_rel = U * (chain(n) + 8) + (p * p_rel).sum()
+        p_rel = p_rel + total_rel + 3 * U
+        mass = np.zeros(n)
+        mass_err = np.zeros(n)
+        np.add.at(mass, s, q)
+        np.add.at(mass_err, s, q * (q_rel + 8 * U))
+        named = np.zeros(n, bool)
+        named[s] = True
+        on = q > 0
+        with np.errstate(invalid="ignore"):
+            terms = np.where(on, q * (log_q - log_p[s]), 0.0)
+        loss[r] = terms.sum()
+        # (t - z) each with its factor's rounding, times a q that is off; the logarithms of both totals; the final rounding
+        apart = np.where(on & there[s], np.abs(t - (-far[s])), 0)
+        loss_err[r] = (q * (apart * (q_rel + 4 * U) + 2 * U * (np.where(on, np.abs(t), 0) + far[s]))).sum() + total_rel + 2 * U * abs(log_total)
+        loss_err[r] += q_sum_rel * (1 if not rest else 2 * (abs(log_total) + 1))
+        if rest:
+            out = p[~named].sum()
+            left = max(0.0, 1 - q.sum()) if out > 0 else 0.0
+            left_err = q.sum() * q_sum_rel + 2 * U
+            if out > 0 and not lawless:
+                o = z[~named]
+                out_big = o.max()
+                log_out = out_big - big + np.log(np.exp(o - out_big).sum()) - log_total
+                out_rel = 2 * total_rel + U * (8 * (big - out_big) + 8)
+                if left > 0:
+                    loss[r] += left * (np.log(left) - log_out)
+                loss_err[r] += left_err * (40 + abs(log_out)) + left * (out_rel + 4 * U * abs(log_out))
+                share = 1 - left / np.exp(log_out)
+            else:
+                log_out, out_rel, share = 0.0, 0.0, 0.0
+        if lawless or (on & ~there[s]).any():
+            loss[r] = np.inf if on.any() else 0.0
+        loss_err[r] += 2 * U * abs(loss[r]) if np.isfinite(loss[r]) else 0
+        if a == 0.0 or lawless:
+            continue
+        by = a / temperature
+        if rest:
+            g[r] = by * np.where(named, p - mass, p * share)
+            ratio = left / np.exp(log_out) if out > 0 else 0.0
+            bulk = p * (p_rel + out_rel + 4 * U) * (1 + ratio) + p * (ratio * (out_rel + 4 * U) + left_err / np.exp(log_out))
+            g_err[r] = abs(by) * np.where(named, p * p_rel + mass_err, bulk) + 4 * U * np.abs(g[r])
+        else:
+            g[r] = by * (p * (1.0 if on.any() else 0.0) - mass)
+            g_err[r] = abs(by) * (p * p_rel + mass_err) + 4 * U * np.abs(g[r])
+    return loss, g, loss_err, g_err

@@ -36,6 +36,8 @@ EXPORTS = [
     "pilc_logprobs_workspace_size", "pilc_logprobs", "pilc_logprobs_grad", "pilc_logprobs_train",
     "pilc_norm_workspace_size", "pilc_norm_forward", "pilc_norm_backward",
     "pilc_adamw_step", "pilc_adamw_values",
+    "pilc_block8_quantize", "pilc_block8_values", "pilc_block8_product_workspace_size", "pilc_block8_product",
+    "pilc_rms_forward", "pilc_rms_workspace_size", "pilc_rms_backward", "pilc_distill_workspace_size", "pilc_distill",
 ]
 
 
@@ -82,6 +84,21 @@ class pilc_adamw_params(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("grad_scale", C.c_double), ("step", C.c_uint64), ("param_type", C.c_uint32), ("grad_type", C.c_uint32),
                 ("state_bits", C.c_uint32), ("dither", C.c_uint32)]
+
+
+class pilc_block8(C.Structure):
+    _fields_ = [("code", C.c_void_p), ("scale", C.c_void_p), ("stride", C.c_uint64), ("scale_stride", C.c_uint64),
+                ("type", C.c_uint32), ("block_rows", C.c_uint32)]
+
+
+class pilc_rms_shape(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("width", C.c_uint32), ("x_stride", C.c_uint64), ("add_stride", C.c_uint64),
+                ("sum_stride", C.c_uint64), ("y_stride", C.c_uint64), ("dtype", C.c_uint32), ("weight_type", C.c_uint32), ("eps", C.c_float)]
+
+
+class pilc_distill_shape(C.Structure):
+    _fields_ = [("rows", C.c_uint32), ("num_sym", C.c_uint32), ("stride", C.c_uint64), ("dtype", C.c_uint32), ("top", C.c_uint32),
+                ("rest", C.c_uint32), ("temperature", C.c_float)]
 
 
 class PilcError(RuntimeError):
@@ -183,6 +200,17 @@ def lib():
                   L.pilc_norm_workspace_size, L.pilc_norm_forward, L.pilc_norm_backward, L.pilc_adamw_step,
                   L.pilc_adamw_values):
             f.restype = C.c_int
+        bp, rp, dp, W = C.POINTER(pilc_block8), C.POINTER(pilc_rms_shape), C.POINTER(pilc_distill_shape), C.c_uint32
+        for f, args in ((L.pilc_block8_quantize, [W, W, V, C.c_uint64, W, bp, bp, V]),
+                        (L.pilc_block8_values, [W, W, bp, V, C.c_uint64, W, V]),
+                        (L.pilc_block8_product_workspace_size, [W, W, W, C.POINTER(Z)]),
+                        (L.pilc_block8_product, [W, W, W, bp, bp, V, C.c_uint64, W, V, Z, V]),
+                        (L.pilc_rms_forward, [rp, V, V, V, V, V, bp, V, V]),
+                        (L.pilc_rms_workspace_size, [rp, C.POINTER(Z)]),
+                        (L.pilc_rms_backward, [rp, V, V, V, V, V, V, V, V, Z, V]),
+                        (L.pilc_distill_workspace_size, [dp, C.POINTER(Z)]),
+                        (L.pilc_distill, [dp, V, V, V, V, V, V, C.c_uint64, V, Z, V])):
+            f.restype, f.argtypes = C.c_int, args
         _lib = L
     return _lib
 
@@ -694,4 +722,181 @@ def pilc_adamw_values(codes, scales, values, signed: bool, stream: Optional[torc
                                  n, 1 if signed else 0, _vector(values, torch.float32, n, dev, "values"), _raw_stream(stream, dev))
     if check and rc != PILC_OK:
         raise PilcError(rc, "pilc_adamw_values")
+    return rc
+
+
+# ---- from a network's last states to its logits, in 8 bits -------------------------------------
+_CODES = {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
+
+
+class Block8:
+    """A matrix in 8 bits as the calls below take it; holds its tensors, so that they stay where they are."""
+
+    def __init__(self, record, rows: int, width: int, device: int, codes, scales):
+        self.record, self.rows, self.width, self.device, self.codes, self.scales = record, rows, width, device, codes, scales
+        self.ref = C.byref(record)
+
+
+def make_block8(codes: torch.Tensor, scales: torch.Tensor, block_rows: int = 1) -> Block8:
+    """codes [rows, width] of float8_e4m3fn or float8_e5m2, rows dense; scales uint8 [rows / block_rows, width / 128], both rounded
+    up: byte e stands for 2^(e - 127), 255 for a block that is not finite.  Made once and used as long as the tensors stay
+    the same ones."""
+    dev = _device_of(codes, "codes")
+    if codes.dtype not in _CODES or codes.dim() != 2:
+        _bad("codes", "a matrix of float8_e4m3fn or float8_e5m2")
+    if block_rows not in (1, 128):
+        raise PilcError(PILC_E_ARG, "blocks of %s rows" % block_rows)
+    rows, width = codes.shape
+    if not (rows < 1 << 31 and width < 1 << 31):
+        raise PilcError(PILC_E_ARG, "%d rows of %d values" % (rows, width))
+    code, stride = _rows(codes, codes.dtype, rows, width, dev, "codes")
+    scale, scale_stride = _rows(scales, torch.uint8, -(-rows // block_rows), -(-width // 128), dev, "scales")
+    return Block8(pilc_block8(code, scale, stride, scale_stride, _CODES[codes.dtype], block_rows), rows, width, dev, codes, scales)
+
+
+def _block8(m: Optional[Block8], rows: int, width: int, device: int, what: str):
+    if m is None:
+        return None
+    if not isinstance(m, Block8) or m.rows != rows or m.width != width or m.device != device:
+        _bad(what, "a Block8 of %d x %d values" % (rows, width))
+    return m.ref
+
+
+def _matrix(x: torch.Tensor, what: str) -> Tuple[int, int]:
+    if x.dim() != 2 or x.dtype not in _VALUES:
+        _bad(what, "a matrix of float32, bfloat16 or float16")
+    rows, width = x.shape
+    if not (rows < _OVER and width < _OVER):
+        raise PilcError(PILC_E_ARG, "%d rows of %d values" % (rows, width))
+    return rows, width
+
+
+def pilc_block8_quantize(x, out: Optional[Block8] = None, out_t: Optional[Block8] = None, stream: Optional[torch.cuda.Stream] = None,
+                         check: bool = True) -> int:
+    """x [rows, width] into `out` of the same shape, and its transpose into `out_t` [width, rows]; either may be None."""
+    dev = _device_of(x, "x")
+    rows, width = _matrix(x, "x")
+    ptr, stride = _rows(x, x.dtype, rows, width, dev, "x")
+    rc = lib().pilc_block8_quantize(rows, width, ptr, stride, _VALUES[x.dtype], _block8(out, rows, width, dev, "out"),
+                                    _block8(out_t, width, rows, dev, "out_t"), _raw_stream(stream, dev))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_block8_quantize")
+    return rc
+
+
+def pilc_block8_values(held: Block8, values, stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """values [rows, width] = what a matrix in 8 bits stands for."""
+    dev = _device_of(values, "values")
+    rows, width = _matrix(values, "values")
+    ptr, stride = _rows(values, values.dtype, rows, width, dev, "values")
+    rc = lib().pilc_block8_values(rows, width, _block8(held, rows, width, dev, "held"), ptr, stride, _VALUES[values.dtype], _raw_stream(stream, dev))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_block8_values")
+    return rc
+
+
+def pilc_block8_product_workspace_size(rows: int, cols: int, depth: int) -> int:
+    """Bytes of workspace that pilc_block8_product needs for any types."""
+    n = C.c_size_t(0)
+    if not all(0 <= k < _OVER for k in (rows, cols, depth)):
+        raise PilcError(PILC_E_ARG, "%d x %d x %d" % (rows, cols, depth))
+    rc = lib().pilc_block8_product_workspace_size(rows, cols, depth, C.byref(n))
+    if rc != PILC_OK:
+        raise PilcError(rc, "pilc_block8_product_workspace_size")
+    return int(n.value)
+
+
+def pilc_block8_product(a: Block8, b: Block8, c, *, workspace, stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """c [rows, cols] = a [rows, depth] times the transpose of b [cols, depth]."""
+    dev = _device_of(c, "c")
+    rows, cols = _matrix(c, "c")
+    ptr, stride = _rows(c, c.dtype, rows, cols, dev, "c")
+    depth = a.width if isinstance(a, Block8) else 0
+    rc = lib().pilc_block8_product(rows, cols, depth, _block8(a, rows, depth, dev, "a"), _block8(b, cols, depth, dev, "b"), ptr, stride,
+                                   _VALUES[c.dtype], *_workspace(workspace, dev), _raw_stream(stream, dev))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_block8_product")
+    return rc
+
+
+def _strided(t: Optional[torch.Tensor], dtype, rows: int, width: int, device: int, what: str) -> Tuple[Optional[int], int]:
+    return (None, width) if t is None else _rows(t, dtype, rows, width, device, what)
+
+
+def pilc_rms_forward(x, weight, y=None, y8: Optional[Block8] = None, add=None, sum=None, rstd=None, eps: float = 1e-5,
+                     stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """sum = x + add, and of it y = sum * rstd * weight over each row [rows, width], in x's type (y) or in 8 bits (y8); what is
+    None is not wanted, add None: nothing is added, weight None: 1.  sum may be x or add, y may be x."""
+    dev = _device_of(x, "x")
+    own, kind = _norm_types(x, weight)
+    rows, width = _matrix(x, "x")
+    (xp, xs), (ap, a_s), (sp, ss), (yp, ys) = (_strided(t, own, rows, width, dev, n) for t, n in ((x, "x"), (add, "add"), (sum, "sum"), (y, "y")))
+    shape = pilc_rms_shape(rows, width, xs, a_s, ss, ys, _VALUES[own], _VALUES[kind], eps)
+    rc = lib().pilc_rms_forward(C.byref(shape), xp, ap, _vector(weight, kind, width, dev, "weight"), sp, yp, _block8(y8, rows, width, dev, "y8"),
+                                _vector(rstd, torch.float32, rows, dev, "rstd"), _raw_stream(stream, dev))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_rms_forward")
+    return rc
+
+
+def pilc_rms_workspace_size(rows: int, width: int) -> int:
+    """Bytes of workspace that pilc_rms_backward needs for any types."""
+    n = C.c_size_t(0)
+    if not (0 <= rows < _OVER and 0 <= width < _OVER):
+        raise PilcError(PILC_E_ARG, "%d rows of %d values" % (rows, width))
+    rc = lib().pilc_rms_workspace_size(C.byref(pilc_rms_shape(rows, width, width, width, width, width, 0, 0, 0.0)), C.byref(n))
+    if rc != PILC_OK:
+        raise PilcError(rc, "pilc_rms_workspace_size")
+    return int(n.value)
+
+
+def pilc_rms_backward(dy, h, weight, rstd, dx=None, dweight=None, dsum=None, *, workspace, stream: Optional[torch.cuda.Stream] = None,
+                      check: bool = True) -> int:
+    """Gradients of pilc_rms_forward by x (and add) and by weight; h is its sum, dsum what comes back through that.  What is None
+    is not wanted.  dx may be dy or dsum."""
+    dev = _device_of(h, "h")
+    own, kind = _norm_types(h, weight, dweight)
+    rows, width = _matrix(h, "h")
+    (hp, hs), (gp, gs), (sp, ss), (xp, xs) = (_strided(t, own, rows, width, dev, n) for t, n in ((h, "h"), (dy, "dy"), (dsum, "dsum"), (dx, "dx")))
+    shape = pilc_rms_shape(rows, width, hs, ss, xs, gs, _VALUES[own], _VALUES[kind], 0.0)
+    rc = lib().pilc_rms_backward(C.byref(shape), gp, hp, _vector(weight, kind, width, dev, "weight"), _vector(rstd, torch.float32, rows, dev, "rstd"),
+                                 sp, xp, _vector(dweight, kind, width, dev, "dweight"), *_workspace(workspace, dev), _raw_stream(stream, dev))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_rms_backward")
+    return rc
+
+
+def _distill_shape(rows: int, num_sym: int, stride: int, kind: int, top: int, rest: bool, temperature: float) -> pilc_distill_shape:
+    if not (0 <= rows < _OVER and 0 <= num_sym < _OVER and 0 <= top < _OVER):
+        raise PilcError(PILC_E_ARG, "%d rows of %d logits with %d named" % (rows, num_sym, top))
+    return pilc_distill_shape(rows, num_sym, stride, kind, top, 1 if rest else 0, temperature)
+
+
+def pilc_distill_workspace_size(rows: int, num_sym: int, top: int) -> int:
+    """Bytes of workspace that pilc_distill needs for any type of logits."""
+    n = C.c_size_t(0)
+    rc = lib().pilc_distill_workspace_size(C.byref(_distill_shape(rows, num_sym, num_sym, 0, top, False, 1.0)), C.byref(n))
+    if rc != PILC_OK:
+        raise PilcError(rc, "pilc_distill_workspace_size")
+    return int(n.value)
+
+
+def pilc_distill(logits, sym, value, loss, up=None, grad=None, temperature: float = 1.0, rest: bool = False, *, workspace,
+                 stream: Optional[torch.cuda.Stream] = None, check: bool = True) -> int:
+    """loss [rows] of a student's logits [rows, num_sym] against the symbols that a teacher names, sym int32 and value float32
+    [rows, top], and with grad the gradient of sum(up * loss) by the logits; grad may be the logits.  rest: values are the
+    teacher's ln p, and what is left of 1 counts as one more symbol."""
+    dev, f32 = _device_of(logits, "logits"), torch.float32
+    rows, num_sym = _matrix(logits, "logits")
+    ptr, stride = _rows(logits, logits.dtype, rows, num_sym, dev, "logits")
+    if sym.dim() != 2:
+        _bad("sym", "a matrix of int32")
+    top = sym.shape[1]
+    g, g_stride = _strided(grad, logits.dtype, rows, num_sym, dev, "grad")
+    shape = _distill_shape(rows, num_sym, stride, _VALUES[logits.dtype], top, rest, temperature)
+    rc = lib().pilc_distill(C.byref(shape), ptr, _vector(sym, torch.int32, rows * top, dev, "sym"), _vector(value, f32, rows * top, dev, "value"),
+                            _vector(up, f32, rows, dev, "up"), _vector(loss, f32, rows, dev, "loss"), g, g_stride,
+                            *_workspace(workspace, dev), _raw_stream(stream, dev))
+    if check and rc != PILC_OK:
+        raise PilcError(rc, "pilc_distill")
     return rc

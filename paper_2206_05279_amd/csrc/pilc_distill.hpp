@@ -1,0 +1,536 @@
+// What a student's laws lose against those of a teacher who names some symbols of each row, and the gradient.
+#pragma once
+
+namespace pilc {
+
+// Per row of logits x, f = 1 / temperature: M = max x and S = sum of e^(f (x - M)) over the bulk, which is all symbols, or with `rest`
+// those that are not named.  The gradient of a bulk symbol is e^(f (x - M)) times one number of the row's, and the named symbols,
+// at most 128, are looked at one by one: their logits are fetched by themselves, and their gradients put in their places after the
+// bulk's.  So a row is read once, into registers, and gone through as in pilc_logprobs.  A loss is a small difference
+// of large logarithms where student and teacher agree: the named symbols' terms are added up in 64 bits, of differences
+// that are taken first.
+
+constexpr int kMaxNamed = 128;
+
+struct DistillArgs {
+    const void *x;
+    const int32_t *sym;
+    const float *value, *up;
+    float *loss;
+    void *grad;
+    uint64_t stride, grad_stride;
+    uint32_t rows, num_sym, top;
+    float turn;             // 1 / temperature
+    uint32_t splits, span;  // see LogitsArgs
+    float2 *part;           // of each run: its largest value and sum
+    float4 *record;         // of each row for k_distill_grad: see Moves
+    float *named;           // of each entry: its gradient
+};
+
+// What is known of the bulk of a row or of a run: its largest value and the sum of the powers of the others' distances to it.
+struct Bulk {
+    float max, total;
+};
+__device__ __forceinline__ float distill_factor(const DistillArgs &a) { return a.turn * kLog2e; }
+__device__ __forceinline__ float center_of(float max) { return max == -kInf ? 0.0f : max; }
+__device__ __forceinline__ Bulk both(Bulk a, Bulk b, float factor)
+{
+    const float max = fmaxf(a.max, b.max), c = center_of(max);
+    return {max, a.total * exp2_fast((a.max - c) * factor) + b.total * exp2_fast((b.max - c) * factor)};
+}
+
+// What a row's bulk moves by: `each` times a value's power; nothing at all with `zeros`.
+struct Moves {
+    float max, each;
+    bool zeros;
+};
+
+struct Or {
+    __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a | b; }
+};
+template <int kLanes>
+__device__ __forceinline__ double lanes_sum(double v)
+{
+    for (int d = 1; d < kLanes; d *= 2) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+// The entries of a row, in LDS, gone through by kLanes lanes of a wavefront.
+template <int kLanes>
+struct Named {
+    static constexpr uint32_t kAny = 1, kSpoilt = 2;
+    int32_t *sym;
+    float *value, *x;  // `value` becomes q, `x` the entry's gradient
+    uint32_t lane, top, flags;
+
+    __device__ Named(void *room, uint32_t t) : sym((int32_t *)room), value((float *)room + t), x((float *)room + 2 * t), lane(threadIdx.x % kLanes), top(t), flags(0) {}
+    __device__ static size_t bytes(uint32_t top) { return 12 * (size_t)top; }
+
+    template <class T>
+    __device__ void load(const DistillArgs &a, uint32_t row)
+    {
+        const T *logits = (const T *)a.x + (uint64_t)row * a.stride;
+        uint32_t own = 0;
+        for (uint32_t i = lane; i < top; i += kLanes) {
+            const int32_t s = a.sym[(uint64_t)row * top + i];
+            const float v = a.value[(uint64_t)row * top + i];
+            const bool in = s >= 0 && (uint32_t)s < a.num_sym;
+            const float at = in ? widen(logits[s]) : 0.0f;
+            if (s >= 0) own |= in && v < kInf && at < kInf ? kAny : kAny | kSpoilt;
+            sym[i] = in ? s : -1, value[i] = v, x[i] = at;
+        }
+        flags = lanes_reduce<kLanes>(own, Or());
+    }
+    template <class F>
+    __device__ void each(F f) const
+    {
+        for (uint32_t i = lane; i < top; i += kLanes)
+            if (sym[i] >= 0) f(i);
+    }
+
+    // The row's loss, and what moves its bulk and its entries.  Entries of the same symbol have their q's together.
+    template <bool kRest>
+    __device__ Moves settle(const DistillArgs &a, Bulk bulk, float up, float &loss)
+    {
+        if (!(flags & kAny)) {
+            loss = 0.0f;
+            each([&](uint32_t i) { x[i] = 0.0f; });
+            return {bulk.max, 0.0f, true};
+        }
+        const float factor = distill_factor(a);
+        const bool spoilt = (flags & kSpoilt) || !(bulk.total == bulk.total);
+        float max = bulk.max, most = -kInf;
+        each([&](uint32_t i) {
+            if (kRest) max = fmaxf(max, x[i]);
+            most = fmaxf(most, value[i]);
+        });
+        if (kRest) max = lanes_reduce<kLanes>(max, MaxFloat());
+        most = center_of(lanes_reduce<kLanes>(most, MaxFloat()));
+        const float center = center_of(max);
+        const bool lawless = max == -kInf;
+        // q, and with kRest the student's sum over named symbols, each once
+        float weight = 0.0f, mass = 0.0f;
+        each([&](uint32_t i) {
+            const float q = kRest ? expf(value[i]) : expf((value[i] - most) * a.turn);
+            weight += q;
+            if constexpr (kRest) {
+                bool first = true;
+                for (uint32_t j = 0; j < i; ++j) first &= sym[j] != sym[i];
+                if (first) mass += exp2_fast((x[i] - center) * factor);
+            }
+        });
+        double all = lanes_sum<kLanes>((double)weight);
+        const float norm = kRest || all == 0.0 ? 1.0f : 1.0f / (float)all;
+        const float beside = kRest ? bulk.total * exp2_fast((bulk.max - center) * factor) : 0.0f;  // the bulk's share of the sum
+        const float total = kRest ? beside + lanes_reduce<kLanes>(mass, Sum()) : bulk.total;
+        double sum = 0.0;
+        bool never = false;  // a symbol with q > 0 that the student rules out
+        each([&](uint32_t i) {
+            const float q = (kRest ? expf(value[i]) : expf((value[i] - most) * a.turn)) * norm;
+            if (q > 0.0f) {
+                never |= x[i] == -kInf;
+                const double mine = ((double)x[i] - center) * a.turn;
+                sum += q * ((kRest ? (double)value[i] : ((double)value[i] - most) * a.turn) - (x[i] == -kInf ? 0.0 : mine));
+            }
+            value[i] = q;
+        });
+        sum = lanes_sum<kLanes>(sum);
+        never = lanes_reduce<kLanes>((uint32_t)never, Or());
+        const bool weighted = all > 0.0;
+        const double log_total = log((double)total);
+        float share;  // of the bulk's powers, before up / temperature
+        if constexpr (kRest) {
+            const double left = bulk.total > 0.0f ? fmax(0.0, 1.0 - all) : 0.0;
+            sum += all * log_total;
+            if (left > 0.0) sum += left * (log(left) - (((double)bulk.max - center) * a.turn + log((double)bulk.total) - log_total));
+            share = bulk.total > 0.0f ? (beside / total - (float)left) / bulk.total : 0.0f;
+        } else {
+            if (weighted) sum += log_total - log(all);
+            share = weighted ? 1.0f / total : 0.0f;
+        }
+        loss = spoilt ? __builtin_nanf("") : lawless || never ? (weighted && (lawless || never) ? kInf : 0.0f) : (float)sum;
+        const float by = up * a.turn;
+        const bool zeros = up == 0.0f || (lawless && !spoilt);
+        if (a.grad) {
+            meet<64>();
+            for (uint32_t i = lane; i < top; i += kLanes) {
+                if (sym[i] < 0) continue;
+                float q = 0.0f;
+                for (uint32_t j = 0; j < top; ++j) q += sym[j] == sym[i] ? value[j] : 0.0f;
+                const float p = kRest || weighted ? exp2_fast((x[i] - center) * factor) / total : 0.0f;
+                x[i] = zeros ? 0.0f : spoilt ? __builtin_nanf("") : by * (p - q);
+            }
+        }
+        return {bulk.max, spoilt ? __builtin_nanf("") : by * share, zeros};
+    }
+};
+
+// The values whose bit is set become -inf.
+template <class T>
+__device__ __forceinline__ void rule_out_bits(Raw<T> &x, uint32_t bits)
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x.bits[k] = bits >> k & 1 ? 0xFF800000u : x.bits[k];
+    } else {
+        constexpr uint32_t kNone = __is_same(T, __bf16) ? 0xFF80u : 0xFC00u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t w = x.bits[i];
+            if (bits >> (2 * i) & 1) w = (w & 0xFFFF0000u) | kNone;
+            if (bits >> (2 * i + 1) & 1) w = (w & 0xFFFFu) | kNone << 16;
+            x.bits[i] = w;
+        }
+    }
+}
+
+template <class T, int kLanes, int kPer>
+struct DistillRow : LogitsRow<T, kLanes, kPer> {
+    using Row = LogitsRow<T, kLanes, kPer>;
+    using Row::kVec;
+    static constexpr int kEntryLanes = kLanes < 64 ? kLanes : 64;
+    static constexpr size_t kMarks = (size_t)kLanes * kPer;  // bytes, one a pack
+
+    // Named symbols of columns begin .. end-1 are ruled out: a byte a pack says which of its values are.
+    __device__ void leave_out(const Named<kEntryLanes> &named, bool mine, uint8_t *marks, uint32_t begin, uint32_t end, Raw<T> (&x)[kPer], int used) const
+    {
+        const uint32_t lane = this->lane;
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) marks[q * kLanes + lane] = 0;
+        meet<kLanes>();
+        if (mine)
+            named.each([&](uint32_t i) {
+                const uint32_t s = (uint32_t)named.sym[i];
+                if (s < begin || s >= end) return;
+                const uint32_t pack = (s - begin) / kVec, column = min(begin + pack * kVec, end - kVec);
+                atomicOr((uint32_t *)marks + pack / 4, 1u << (pack % 4 * 8 + (s - column)));
+            });
+        meet<kLanes>();
+        Row::for_used(used, [&](int q) {
+            const uint32_t bits = marks[q * kLanes + lane];
+            if (bits) rule_out_bits(x[q], bits);
+        });
+    }
+    // The bulk of all lanes' values, in all lanes.  `room` holds 2 * kWaves, its halves are used in turn.
+    __device__ Bulk bulk(const Raw<T> (&x)[kPer], int used, float own, float factor, Bulk *room, int half) const
+    {
+        const float max = lanes_reduce<Row::kWithin>(own, MaxFloat()), center = center_of(max);
+        float total[2] = {0.0f, 0.0f};
+        Row::for_used(used, [&](int q) {
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) total[k & 1] += exp2_fast((x[q][k] - center) * factor);
+        });
+        Bulk t = {max, lanes_reduce<Row::kWithin>(total[0] + total[1], Sum())};
+        if constexpr (Row::kWaves > 1) {
+            room += half * Row::kWaves;
+            if ((threadIdx.x & 63) == 0) room[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)] = t;
+            __syncthreads();
+            t = room[threadIdx.x & (Row::kWaves - 1)];
+#pragma unroll
+            for (int d = 1; d < Row::kWaves; d *= 2) t = both(t, Bulk{__shfl_xor(t.max, d, 64), __shfl_xor(t.total, d, 64)}, factor);
+        }
+        return t;
+    }
+    __device__ void put(const Raw<T> &x, T *to, int twice, float center, float factor, const Moves &m) const
+    {
+        float d[kVec];
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) d[k] = m.zeros ? 0.0f : exp2_fast((x[k] - center) * factor) * m.each;
+        if (twice == 0) {
+            Raw<T>::of(d).store(to);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kVec; ++k)
+                if (k >= twice) to[k] = (T)d[k];
+        }
+    }
+};
+
+// A row a workgroup or a part of it, with kGrad its gradient from the same registers.
+template <class T, int kLanes, int kPer, bool kRest, bool kGrad>
+__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::kResident)) void k_distill(DistillArgs a)
+{
+    using Row = DistillRow<T, kLanes, kPer>;
+    __shared__ Bulk room[2 * Row::kWaves];
+    __shared__ Moves shared_moves;
+    extern __shared__ uint32_t more_room[];  // the rows' marks, then their entries
+    Row r;
+    const uint64_t step = (uint64_t)gridDim.x * Row::kRows;
+    const float factor = distill_factor(a);
+    uint8_t *marks = (uint8_t *)more_room + (kRest ? r.row_in_block * Row::kMarks : 0);
+    Named<Row::kEntryLanes> named((uint8_t *)more_room + (kRest ? Row::kRows * Row::kMarks : 0) + r.row_in_block * 12 * a.top, a.top);
+    const bool mine = Row::kWaves <= 1 || threadIdx.x < 64;  // of a row's wavefronts the first sees to the entries
+    int half = 0;
+    for (uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block; item < a.rows; item += step) {
+        const uint32_t row = (uint32_t)item;
+        const float up = kGrad ? a.up[row] : 0.0f;
+        Raw<T> x[kPer];
+        if (mine) named.template load<T>(a, row);
+        r.load((const T *)a.x + (uint64_t)row * a.stride, 0, a.num_sym, x);
+        r.rule_out(0, a.num_sym, x);
+        const int used = r.used(0, a.num_sym);
+        meet<64>();
+        if constexpr (kRest) r.leave_out(named, mine, marks, 0, a.num_sym, x, used);
+        float of[kPer];
+        const float own = r.largest(x, used, of);
+        r.forget(x);
+        const Bulk bulk = r.bulk(x, used, own, factor, room, half);
+        r.forget(x);
+        half ^= 1;
+        Moves moves = {};
+        if (mine) {
+            float loss;
+            moves = named.template settle<kRest>(a, bulk, up, loss);
+            if (r.lane == 0) {
+                a.loss[row] = loss;
+                if (Row::kWaves > 1) shared_moves = moves;
+            }
+        }
+        if constexpr (kGrad) {
+            if constexpr (Row::kWaves > 1) {
+                __syncthreads();
+                moves = shared_moves;
+            }
+            const float center = center_of(moves.max);
+            T *grad = (T *)a.grad + (uint64_t)row * a.grad_stride;
+            Row::for_used(used, [&](int q) { r.put(x[q], Row::address(grad, r.column(q, 0, a.num_sym), 0, a.num_sym), r.twice(q, 0, a.num_sym), center, factor, moves); });
+            // the bulk's stores are done before the entries take their places
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            meet<kLanes>();
+            if (mine) named.each([&](uint32_t i) { grad[named.sym[i]] = (T)named.x[i]; });
+        }
+        meet<kLanes>();
+    }
+}
+
+// Rows in runs: the bulk of each run,
+template <class T, int kLanes, int kPer, bool kRest>
+__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::kResident)) void k_distill_runs(DistillArgs a)
+{
+    using Row = DistillRow<T, kLanes, kPer>;
+    __shared__ Bulk room[2 * Row::kWaves];
+    extern __shared__ uint32_t more_room[];
+    Row r;
+    const uint64_t items = (uint64_t)a.rows * a.splits, step = (uint64_t)gridDim.x * Row::kRows;
+    const float factor = distill_factor(a);
+    uint8_t *marks = (uint8_t *)more_room + r.row_in_block * Row::kMarks;
+    const bool mine = Row::kWaves <= 1 || threadIdx.x < 64;
+    int half = 0;
+    for (uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block; item < items; item += step) {
+        const uint32_t row = (uint32_t)(item / a.splits), begin = (uint32_t)(item - (uint64_t)row * a.splits) * a.span;
+        const uint32_t end = min(begin + a.span, a.num_sym);
+        Raw<T> x[kPer];
+        r.load((const T *)a.x + (uint64_t)row * a.stride, begin, end, x);
+        r.rule_out(begin, end, x);
+        const int used = r.used(begin, end);
+        if constexpr (kRest) {
+            // the entries' symbols are looked at where they lie
+            Named<Row::kEntryLanes> named(nullptr, a.top);
+            named.sym = (int32_t *)a.sym + (uint64_t)row * a.top;
+            r.leave_out(named, mine, marks, begin, end, x, used);
+        }
+        float of[kPer];
+        const float own = r.largest(x, used, of);
+        r.forget(x);
+        const Bulk bulk = r.bulk(x, used, own, factor, room, half);
+        half ^= 1;
+        if (r.lane == 0) a.part[item] = make_float2(bulk.max, bulk.total);
+        meet<kLanes>();
+    }
+}
+// the runs put together, a wavefront a row, with the row's loss and moves,
+template <class T, bool kRest>
+__global__ __launch_bounds__(256) void k_distill_join(DistillArgs a)
+{
+    extern __shared__ uint32_t more_room[];
+    Named<64> named((uint8_t *)more_room + (threadIdx.x >> 6) * 12 * a.top, a.top);
+    const uint32_t lane = threadIdx.x & 63;
+    for (uint64_t row = blockIdx.x * 4ull + (threadIdx.x >> 6); row < a.rows; row += gridDim.x * 4ull) {
+        named.template load<T>(a, (uint32_t)row);
+        Bulk bulk = {-kInf, 0.0f};
+        for (uint32_t s = lane; s < a.splits; s += 64) {
+            const float2 p = a.part[row * a.splits + s];
+            bulk = both(bulk, Bulk{p.x, p.y}, distill_factor(a));
+        }
+        for (int d = 1; d < 64; d *= 2) bulk = both(bulk, Bulk{__shfl_xor(bulk.max, d, 64), __shfl_xor(bulk.total, d, 64)}, distill_factor(a));
+        meet<64>();
+        float loss;
+        const Moves moves = named.template settle<kRest>(a, bulk, a.grad ? a.up[row] : 0.0f, loss);
+        if (lane == 0) {
+            a.loss[row] = loss;
+            if (a.grad) a.record[row] = make_float4(moves.max, moves.each, moves.zeros ? 1.0f : 0.0f, 0.0f);
+        }
+        if (a.grad)
+            for (uint32_t i = lane; i < a.top; i += 64) a.named[row * a.top + i] = named.x[i];
+        meet<64>();
+    }
+}
+// the bulk's gradient run by run,
+template <class T, int kLanes, int kPer>
+__global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_distill_grad(DistillArgs a)
+{
+    using Row = DistillRow<T, kLanes, kPer>;
+    const Row r;
+    const uint64_t items = (uint64_t)a.rows * a.splits, step = (uint64_t)gridDim.x * Row::kRows;
+    const float factor = distill_factor(a);
+    for (uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block; item < items; item += step) {
+        const uint32_t row = (uint32_t)(item / a.splits), begin = (uint32_t)(item - (uint64_t)row * a.splits) * a.span;
+        const uint32_t end = min(begin + a.span, a.num_sym);
+        const float4 record = a.record[row];
+        const Moves moves = {record.x, record.y, record.z != 0.0f};
+        Raw<T> x[kPer];
+        r.load((const T *)a.x + (uint64_t)row * a.stride, begin, end, x);
+        T *grad = (T *)a.grad + (uint64_t)row * a.grad_stride;
+#pragma unroll
+        for (int q = 0; q < kPer; ++q)
+            r.put(x[q], Row::address(grad, r.column(q, begin, end), begin, end), r.twice(q, begin, end), center_of(moves.max), factor, moves);
+    }
+}
+// and the entries' in their places.
+template <class T>
+__global__ __launch_bounds__(256) void k_distill_named(DistillArgs a)
+{
+    const uint64_t count = (uint64_t)a.rows * a.top;
+    for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < count; i += gridDim.x * 256ull) {
+        const int32_t s = a.sym[i];
+        if (s >= 0 && (uint32_t)s < a.num_sym) ((T *)a.grad)[i / a.top * a.grad_stride + s] = (T)a.named[i];
+    }
+}
+
+// Rows shorter than a pack: a wavefront a row, each value a lane's.
+template <class T, bool kRest>
+__global__ __launch_bounds__(256) void k_distill_short(DistillArgs a)
+{
+    extern __shared__ uint32_t more_room[];
+    Named<64> named((uint8_t *)more_room + (threadIdx.x >> 6) * 12 * a.top, a.top);
+    const uint32_t lane = threadIdx.x & 63;
+    const float factor = distill_factor(a);
+    for (uint64_t row = blockIdx.x * 4ull + (threadIdx.x >> 6); row < a.rows; row += gridDim.x * 4ull) {
+        named.template load<T>(a, (uint32_t)row);
+        float x = lane < a.num_sym ? widen(((const T *)a.x)[row * a.stride + lane]) : -kInf;
+        meet<64>();
+        bool is_named = false;
+        for (uint32_t i = 0; i < a.top; ++i) is_named |= named.sym[i] == (int32_t)lane;
+        if (kRest && is_named) x = -kInf;
+        const float max = wave_reduce(x, MaxFloat());
+        const Bulk bulk = {max, wave_reduce(exp2_fast((x - center_of(max)) * factor), Sum())};
+        float loss;
+        const Moves moves = named.template settle<kRest>(a, bulk, a.grad ? a.up[row] : 0.0f, loss);
+        if (lane == 0) a.loss[row] = loss;
+        if (a.grad) {
+            T *grad = (T *)a.grad + row * a.grad_stride;
+            if (lane < a.num_sym && !is_named) grad[lane] = (T)(moves.zeros ? 0.0f : exp2_fast((x - center_of(max)) * factor) * moves.each);
+            meet<64>();
+            named.each([&](uint32_t i) { grad[named.sym[i]] = (T)named.x[i]; });
+        }
+        meet<64>();
+    }
+}
+
+static bool distill_shape_ok(const pilc_distill_shape *s)
+{
+    return s && s->num_sym >= 1 && s->num_sym <= 0x7FFFFFFFu && s->stride >= s->num_sym && s->stride <= (1ull << 48) && s->dtype <= PILC_F16 &&
+           s->top >= 1 && s->top <= (uint32_t)kMaxNamed && s->rest <= 1 && s->temperature >= 1e-30f && s->temperature <= 1e30f;
+}
+
+// Whole rows as pilc_logprobs and pilc_logprobs_train keep them, by the same figures.
+static bool distill_by_row(uint32_t rows, uint32_t num_sym, uint32_t value, bool grad)
+{
+    return grad ? train_by_row(rows, num_sym, value) : logits_plan(rows, num_sym, value, kWholeRow, kLongestRun, kShortestRun).splits == 1;
+}
+static size_t distill_workspace(const pilc_distill_shape &s)
+{
+    size_t most = 256;
+    for (uint32_t value : {2u, 4u}) {
+        const LogitsPlan p = logits_plan(s.rows, s.num_sym, value, kWholeRow, kLongestRun, kShortestRun);
+        if (!distill_by_row(s.rows, s.num_sym, value, true) || !distill_by_row(s.rows, s.num_sym, value, false))
+            most = std::max(most, (size_t)s.rows * (sizeof(float4) + sizeof(float2) * p.splits + sizeof(float) * s.top));
+    }
+    return most;
+}
+
+template <class T, bool kRest, bool kGrad>
+static void launch_distill_rows(DistillArgs a, hipStream_t stream)
+{
+    logits_row<kGrad ? kTrainRows : kLaw>(a.num_sym * (uint32_t)sizeof(T), 0, true, [&](auto lanes, auto per) {
+        using Row = DistillRow<T, decltype(lanes)::value, decltype(per)::value>;
+        const size_t lds = Row::kRows * ((kRest ? Row::kMarks : 0) + 12 * a.top);
+        k_distill<T, decltype(lanes)::value, decltype(per)::value, kRest, kGrad><<<logits_blocks(a.rows, Row::kRows), Row::kThreads, lds, stream>>>(a);
+    });
+}
+
+template <class T, bool kRest>
+static void launch_distill(DistillArgs a, void *workspace, hipStream_t stream)
+{
+    const uint32_t quarter = std::min(div_up(a.rows, 4), 1u << 20);
+    const size_t entries = 4 * 12 * (size_t)a.top;
+    if (a.num_sym < 16 / sizeof(T)) {
+        k_distill_short<T, kRest><<<quarter, 256, entries, stream>>>(a);
+        return;
+    }
+    if (distill_by_row(a.rows, a.num_sym, sizeof(T), a.grad != nullptr)) {
+        a.grad ? launch_distill_rows<T, kRest, true>(a, stream) : launch_distill_rows<T, kRest, false>(a, stream);
+        return;
+    }
+    const LogitsPlan p = logits_plan(a.rows, a.num_sym, sizeof(T), kWholeRow, kLongestRun, kShortestRun);
+    a.splits = p.splits, a.span = std::min(p.span, a.num_sym);
+    a.record = (float4 *)workspace;
+    a.part = (float2 *)(a.record + a.rows);
+    a.named = (float *)(a.part + (size_t)a.rows * a.splits);
+    logits_row<kLaw>(a.span * (uint32_t)sizeof(T), 0, false, [&](auto lanes, auto per) {
+        using Row = DistillRow<T, decltype(lanes)::value, decltype(per)::value>;
+        k_distill_runs<T, decltype(lanes)::value, decltype(per)::value, kRest>
+            <<<logits_blocks((uint64_t)a.rows * a.splits, Row::kRows), Row::kThreads, kRest ? Row::kRows * Row::kMarks : 0, stream>>>(a);
+    });
+    k_distill_join<T, kRest><<<quarter, 256, entries, stream>>>(a);
+    if (!a.grad) return;
+    constexpr uint32_t kRun = 16 << 10;
+    const LogitsPlan g = logits_plan(a.rows, a.num_sym, sizeof(T), kRun, kRun, kShortestRun);
+    a.splits = g.splits, a.span = std::min(g.span, a.num_sym);
+    using std::integral_constant;
+    const auto with = [&](auto per) {
+        using Row = DistillRow<T, 256, decltype(per)::value>;
+        if (a.span > Row::kValues) return false;
+        k_distill_grad<T, 256, decltype(per)::value><<<logits_blocks((uint64_t)a.rows * a.splits, 1), 256, 0, stream>>>(a);
+        return true;
+    };
+    (void)(with(integral_constant<int, 2>()) || with(integral_constant<int, 4>()));
+    k_distill_named<T><<<(uint32_t)std::min<uint64_t>(((uint64_t)a.rows * a.top + 255) / 256, 1u << 20), 256, 0, stream>>>(a);
+}
+
+}  // namespace pilc
+
+extern "C" {
+using namespace pilc;
+
+int pilc_distill_workspace_size(const pilc_distill_shape *shape, size_t *workspace_bytes_host)
+{
+    if (!distill_shape_ok(shape) || !workspace_bytes_host) return PILC_E_ARG;
+    *workspace_bytes_host = distill_workspace(*shape);
+    return PILC_OK;
+}
+
+int pilc_distill(const pilc_distill_shape *shape, const void *logits_dev, const int32_t *sym_dev, const float *value_dev, const float *up_dev,
+                 float *loss_dev, void *grad_dev, uint64_t grad_stride, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    if (!distill_shape_ok(shape) || (grad_dev && (grad_stride < shape->num_sym || grad_stride > (1ull << 48)))) return PILC_E_ARG;
+    if (shape->rows == 0) return PILC_OK;
+    const size_t bytes = value_bytes(shape->dtype);
+    if (!logits_dev || !sym_dev || !value_dev || !loss_dev || (grad_dev != nullptr) != (up_dev != nullptr) || !aligned_to(logits_dev, bytes) ||
+        !aligned_to(grad_dev, bytes) || !aligned_to(sym_dev, 4) || !aligned_to(value_dev, 4) || !aligned_to(up_dev, 4) || !aligned_to(loss_dev, 4) ||
+        !workspace_dev || !aligned_to(workspace_dev, 256) || (grad_dev == logits_dev && grad_stride != shape->stride))
+        return PILC_E_ARG;
+    if (workspace_bytes < distill_workspace(*shape)) return PILC_E_WORKSPACE;
+    DistillArgs a = {};
+    a.x = logits_dev, a.sym = sym_dev, a.value = value_dev, a.up = up_dev, a.loss = loss_dev, a.grad = grad_dev, a.stride = shape->stride;
+    a.grad_stride = grad_stride, a.rows = shape->rows, a.num_sym = shape->num_sym, a.top = shape->top, a.turn = 1.0f / shape->temperature;
+    return by_type(shape->dtype, [&](auto *t) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        if (shape->rest)
+            launch_distill<T, true>(a, workspace_dev, (hipStream_t)hip_stream);
+        else
+            launch_distill<T, false>(a, workspace_dev, (hipStream_t)hip_stream);
+    });
+}
+
+}  // extern "C"

@@ -691,14 +691,11 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitsArgs a)
     }
 }
 
-static size_t value_bytes(uint32_t type) { return type == PILC_F32 ? 4 : 2; }
-
 static bool logits_shape_ok(const pilc_logits_shape *s)
 {
     return s && s->num_sym >= 1 && s->num_sym <= 0x7FFFFFFFu && s->stride >= s->num_sym && s->stride <= (1ull << 48) && s->dtype <= PILC_F16 &&
            s->target_type <= PILC_I64 && s->top <= (uint32_t)kMaxTop;
 }
-static bool aligned_to(const void *p, size_t bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
 
 static bool logits_in_ok(const pilc_logits_shape *s, const void *logits, const void *target)
 {
@@ -842,23 +839,6 @@ static void launch_grad(LogitsArgs a, hipStream_t stream)
            with(integral_constant<int, 16>(), integral_constant<int, 4>()) || with(integral_constant<int, 32>(), integral_constant<int, 4>()) ||
            with(integral_constant<int, 64>(), integral_constant<int, 4>()) || with(integral_constant<int, 256>(), integral_constant<int, 2>()) ||
            with(integral_constant<int, 256>(), integral_constant<int, 4>()));
-}
-
-template <class Launch>
-static void by_value_type(uint32_t type, Launch launch)
-{
-    switch (type) {
-    case PILC_F32: launch((float *)nullptr); break;
-    case PILC_BF16: launch((bf16_t *)nullptr); break;
-    default: launch((f16_t *)nullptr); break;
-    }
-}
-template <class Launch>
-static int by_type(uint32_t type, Launch launch)
-{
-    by_value_type(type, launch);
-    HIP_TRY(hipGetLastError());
-    return PILC_OK;
 }
 
 }  // namespace pilc

@@ -583,17 +583,6 @@ static bool norm_shape_ok(const pilc_norm_shape *s, bool backward)
            (s->weight_type == s->dtype || s->weight_type == PILC_F32) && s->eps >= 0.0f && s->eps < kInf;
 }
 
-template <class Launch>
-static int by_types(uint32_t type, uint32_t weight_type, Launch launch)
-{
-    return by_type(type, [&](auto *t) {
-        if (weight_type == type)
-            launch(t, t);
-        else
-            launch(t, (float *)nullptr);
-    });
-}
-
 }  // namespace pilc
 
 extern "C" {

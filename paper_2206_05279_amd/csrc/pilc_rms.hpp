@@ -1,0 +1,627 @@
+// Root-mean-square norm of a sum, in values or in 8 bits under scales, and its backward pass.
+#pragma once
+
+namespace pilc {
+
+struct RmsArgs {
+    const void *x, *add, *weight, *dy, *dsum;
+    void *sum, *y, *dx, *dweight;
+    float *rstd;
+    const float *rstd_in;
+    float *parts;  // [parts][width]
+    Block8 y8;
+    uint64_t x_stride, add_stride, sum_stride, y_stride;  // backward: of h, dsum, dx, dy
+    uint32_t rows, width, num_parts;
+    float eps;
+};
+
+constexpr int kRmsLongThreads = 1024;
+// Wavefronts a SIMD that the kernels' registers are kept down to, and that are launched: all at once, each going from row to row.
+constexpr int kRmsForwardWaves = 4, kRmsBackwardWaves = 2;
+
+// Rows held in registers: kLanes lanes of a wavefront, or a whole workgroup of kLanes threads, hold kEach values of a row each, as
+// packs of 16 bytes, and go from row to row.  A pack that would reach over the row's end is loaded from further ahead and
+// shifted, and one that lies behind it is zeros: neither adds anything to sums or to a block's largest value.
+template <class T, class W, int kLanes, int kEach>
+struct RmsRow {
+    static constexpr int kVec = 16 / sizeof(T), kPer = kEach / kVec;
+    static constexpr bool kAhead = kLanes < 1024;  // the next row is asked for early; the largest workgroups lack the registers
+    static constexpr bool kKeep = kEach <= 16;     // the weights stay in registers; the longest rows' come from the caches
+    static constexpr int kThreads = kLanes > 256 ? kLanes : 256;
+    static constexpr int kRows = kThreads / kLanes;  // that a workgroup has in hand
+    static constexpr int kWaves = kLanes / 64;       // that share a row
+    static constexpr int kWithin = kLanes < 64 ? kLanes : 64;
+    static constexpr int kBlockLanes = (int)kBlock8 / kVec;  // that hold a block
+    static constexpr int waves(int most) { return kThreads == 1024 ? 4 : most * 256 / kThreads * kThreads / 256; }
+    static_assert(kLanes % kBlockLanes == 0 || kLanes * kEach <= (int)kBlock8);
+
+    uint32_t width, lane, row_in_block;
+
+    __device__ explicit RmsRow(uint32_t w) : width(w), lane(threadIdx.x % kLanes), row_in_block(kRows > 1 ? threadIdx.x / kLanes : 0) {}
+    __device__ uint32_t place(int q) const { return (q * kLanes + lane) * kVec; }
+    __device__ int valid(int q) const { return (int)min(width - min(place(q), width), (uint32_t)kVec); }
+
+    __device__ void load(const T *p, Raw<T> (&out)[kPer]) const
+    {
+        if (width == (uint32_t)(kLanes * kEach)) {
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) out[q] = Raw<T>::load(p + place(q));
+        } else if (width >= (uint32_t)kVec) {
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) out[q] = Raw<T>::load(p + min(place(q), width - kVec));
+        } else {
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) out[q].bits = __builtin_bit_cast(u32x4_t, load_pack<kVec>(p + min(place(q), width), valid(q)));
+        }
+    }
+    // What has been loaded, each value in its place
+    __device__ void settle(Raw<T> (&x)[kPer]) const
+    {
+        if (width == (uint32_t)(kLanes * kEach) || width < (uint32_t)kVec) return;
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) {
+            const uint32_t off = min(place(q) - min(place(q), width - kVec), (uint32_t)kVec) * (uint32_t)(8 * sizeof(T));
+            uint64_t lo = (uint64_t)x[q].bits[1] << 32 | x[q].bits[0], hi = (uint64_t)x[q].bits[3] << 32 | x[q].bits[2];
+            const uint32_t part = off & 63;
+            const uint64_t carried = part ? hi << (64 - part) : 0;
+            const uint64_t low = off >= 128 ? 0 : off >= 64 ? hi >> part : lo >> part | carried;
+            const uint64_t high = off >= 64 ? 0 : hi >> part;
+            x[q].bits = u32x4_t{(uint32_t)low, (uint32_t)(low >> 32), (uint32_t)high, (uint32_t)(high >> 32)};
+        }
+    }
+    __device__ void store(T *p, int q, const Raw<T> &v) const
+    {
+        const int n = valid(q);
+        if (n == kVec)
+            v.store(p + place(q));
+        else if (n > 0)
+            store_pack<kVec>(p + place(q), n, __builtin_bit_cast(Pack<T, kVec>, v.bits));
+    }
+    __device__ Pack<W, kVec> weights(const W *p, int q) const
+    {
+        const int n = valid(q);
+        if (p && n > 0) return load_pack<kVec>(p + place(q), n);
+        Pack<W, kVec> t;
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) t.v[k] = (W)1.0f;
+        return t;
+    }
+    // The row's sum in all its lanes; `room`'s halves are used in turn, so that the workgroup meets once a sum.
+    __device__ float sum(float v, float *room, int half) const
+    {
+        v = lanes_reduce<kWithin>(v, Sum());
+        if constexpr (kWaves > 1) {
+            room += half * kWaves;
+            if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+            __syncthreads();
+            v = room[0];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) v += room[w];
+        }
+        return v;
+    }
+};
+
+// Codes of kVec values whose place is `at` of row `row`, under the block's scale.
+template <int kVec>
+__device__ __forceinline__ void put_codes(const Block8 &y8, uint32_t row, uint32_t at, int valid, const float (&v)[kVec], uint32_t largest, bool first)
+{
+    const uint32_t byte = scale_byte(largest, y8.type);
+    const float f = scale_inverse(byte);
+    if (valid > 0) {
+        uint32_t words[kVec / 4];
+#pragma unroll
+        for (int i = 0; i < kVec / 4; ++i)
+            words[i] = codes_of(v[4 * i] * f, v[4 * i + 1] * f, v[4 * i + 2] * f, v[4 * i + 3] * f, y8.type, byte);
+        Pack<uint8_t, kVec> codes;
+        __builtin_memcpy(&codes, words, kVec);
+        store_pack<kVec>(y8.code + (uint64_t)row * y8.stride + at, valid, codes);
+        if (first) y8.scale[(uint64_t)row * y8.scale_stride + at / kBlock8] = (uint8_t)byte;
+    }
+}
+
+template <class T>
+__device__ __forceinline__ Raw<T> added(const Raw<T> &x, const Raw<T> &add)
+{
+    float v[Raw<T>::kVec];
+#pragma unroll
+    for (int k = 0; k < Raw<T>::kVec; ++k) v[k] = x[k] + add[k];
+    return Raw<T>::of(v);
+}
+
+template <class T, class W, int kLanes, int kEach>
+__global__ __launch_bounds__((RmsRow<T, W, kLanes, kEach>::kThreads), (RmsRow<T, W, kLanes, kEach>::waves(kRmsForwardWaves))) void
+k_rms_forward_rows(RmsArgs a)
+{
+    using Row = RmsRow<T, W, kLanes, kEach>;
+    constexpr int kVec = Row::kVec, kPer = Row::kPer;
+    __shared__ float room[2 * (Row::kWaves > 1 ? Row::kWaves : 1)];
+    const Row r(a.width);
+    const float per_value = 1.0f / (float)a.width;
+    Pack<W, kVec> weight[kPer];
+    if (Row::kKeep)
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) weight[q] = r.weights((const W *)a.weight, q);
+    Raw<T> x[kPer], add[kPer], next_x[kPer], next_add[kPer];
+    uint32_t row = blockIdx.x * Row::kRows + r.row_in_block;
+    const uint32_t step = gridDim.x * Row::kRows, last = a.rows - 1;
+    int half = 0;
+    const auto fetch = [&](uint32_t of, Raw<T>(&to)[kPer], Raw<T>(&to_add)[kPer]) {
+        r.load((const T *)a.x + (uint64_t)of * a.x_stride, to);
+        if (a.add) r.load((const T *)a.add + (uint64_t)of * a.add_stride, to_add);
+    };
+    if (Row::kAhead) fetch(min(row, last), x, add);
+    for (bool more = row < a.rows; more; more = next_row(row, step, last)) {
+        if (Row::kAhead)
+            fetch(last - row > step ? row + step : last, next_x, next_add);
+        else
+            fetch(row, x, add);
+        r.settle(x);
+        if (a.add) {
+            r.settle(add);
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) {
+                x[q] = added(x[q], add[q]);
+                if (a.sum) r.store((T *)a.sum + (uint64_t)row * a.sum_stride, q, x[q]);
+            }
+        } else if (a.sum) {
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) r.store((T *)a.sum + (uint64_t)row * a.sum_stride, q, x[q]);
+        }
+        float square[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int q = 0; q < kPer; ++q)
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) square[k & 1] = __builtin_fmaf(x[q][k], x[q][k], square[k & 1]);
+        const float rstd = 1.0f / sqrtf(r.sum(square[0] + square[1], room, half) * per_value + a.eps);
+        half ^= 1;
+        if (r.lane == 0 && a.rstd) a.rstd[row] = rstd;
+        const auto out = [&](int q, float(&v)[kVec]) {
+            if (!Row::kKeep) weight[q] = r.weights((const W *)a.weight, q);
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) v[k] = x[q][k] * rstd * widen(weight[q].v[k]);
+        };
+        const auto largest_of = [&](const float(&v)[kVec]) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) m = max(m, size_bits(v[k]));
+            return m;
+        };
+        uint32_t whole = 0;  // a block that is all of the row
+        if constexpr (kLanes % Row::kBlockLanes != 0)
+            if (a.y8.code) {
+#pragma unroll
+                for (int q = 0; q < kPer; ++q) {
+                    float v[kVec];
+                    out(q, v);
+                    whole = max(whole, largest_of(v));
+                }
+                whole = lanes_reduce<Row::kWithin>(whole, Max());
+            }
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) {
+            float v[kVec];
+            out(q, v);
+            if (a.y) r.store((T *)a.y + (uint64_t)row * a.y_stride, q, Raw<T>::of(v));
+            if (a.y8.code) {
+                uint32_t m = whole;
+                if constexpr (kLanes % Row::kBlockLanes == 0) m = lanes_reduce<Row::kBlockLanes>(largest_of(v), Max());
+                put_codes<kVec>(a.y8, row, r.place(q), r.valid(q), v, m, r.place(q) % kBlock8 == 0);
+            }
+        }
+        if (Row::kAhead)
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) x[q] = next_x[q], add[q] = next_add[q];
+    }
+}
+
+// dx row by row as above, and what the rows a workgroup meets add to the weight's gradient, in registers; at the end the workgroup's
+// rows are added up and put down as one part.  The longest rows leave no room for that: k_rms_parts.
+template <class T, class W, int kLanes, int kEach>
+__global__ __launch_bounds__((RmsRow<T, W, kLanes, kEach>::kThreads), (RmsRow<T, W, kLanes, kEach>::waves(kRmsBackwardWaves))) void
+k_rms_backward_rows(RmsArgs a)
+{
+    using Row = RmsRow<T, W, kLanes, kEach>;
+    constexpr int kVec = Row::kVec, kPer = Row::kPer;
+    __shared__ float room[2 * (Row::kWaves > 1 ? Row::kWaves : 1)];
+    __shared__ float joined[Row::kRows > 1 ? Row::kThreads * kEach : 1];
+    const Row r(a.width);
+    const float per_value = 1.0f / (float)a.width;
+    Pack<W, kVec> weight[kPer];
+    float dw[kPer][kVec] = {};
+    if (Row::kKeep)
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) weight[q] = r.weights((const W *)a.weight, q);
+    Raw<T> h[kPer], dy[kPer], ds[kPer], next_h[kPer], next_dy[kPer], next_ds[kPer];
+    uint32_t row = blockIdx.x * Row::kRows + r.row_in_block;
+    const uint32_t step = gridDim.x * Row::kRows, last = a.rows - 1;
+    int half = 0;
+    // a row's rstd is asked for before its values: loads come back in order, and what was asked for late would make the
+    // values of the next row be waited for with it
+    float rstd = 0.0f, next_rstd = 0.0f;
+    const bool with_sum = a.dsum && a.dx;
+    const auto fetch = [&](uint32_t of, float &s, Raw<T>(&to_h)[kPer], Raw<T>(&to_dy)[kPer], Raw<T>(&to_ds)[kPer]) {
+        s = a.rstd_in[of];
+        r.load((const T *)a.x + (uint64_t)of * a.x_stride, to_h);
+        r.load((const T *)a.dy + (uint64_t)of * a.y_stride, to_dy);
+        if (with_sum) r.load((const T *)a.dsum + (uint64_t)of * a.add_stride, to_ds);
+    };
+    if (Row::kAhead) fetch(min(row, last), rstd, h, dy, ds);
+    for (bool more = row < a.rows; more; more = next_row(row, step, last)) {
+        if (Row::kAhead)
+            fetch(last - row > step ? row + step : last, next_rstd, next_h, next_dy, next_ds);
+        else
+            fetch(row, rstd, h, dy, ds);
+        r.settle(h);
+        r.settle(dy);
+        if (!Row::kKeep)
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) weight[q] = r.weights((const W *)a.weight, q);
+        float along = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kPer; ++q)
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) {
+                const float d = dy[q][k] * (h[q][k] * rstd);
+                if (Row::kKeep) dw[q][k] += d;
+                along = __builtin_fmaf(d, widen(weight[q].v[k]), along);
+            }
+        if (a.dx) {
+            const float c = r.sum(along, room, half) * per_value;
+            half ^= 1;
+            if (with_sum) r.settle(ds);
+            T *dx = (T *)a.dx + (uint64_t)row * a.sum_stride;
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) {
+                float out[kVec];
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    out[k] = rstd * (dy[q][k] * widen(weight[q].v[k]) - h[q][k] * rstd * c);
+                    if (with_sum) out[k] += ds[q][k];
+                }
+                r.store(dx, q, Raw<T>::of(out));
+            }
+        }
+        if (Row::kAhead) {
+            rstd = next_rstd;
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) h[q] = next_h[q], dy[q] = next_dy[q], ds[q] = next_ds[q];
+        }
+    }
+    if (!Row::kKeep || !a.parts) return;
+    float *part = a.parts + (size_t)blockIdx.x * a.width;
+    if constexpr (Row::kRows > 1) {
+        // value v of lane l of row g at (g * kEach + v) * kLanes + l
+#pragma unroll
+        for (int v = 0; v < kEach; ++v) joined[(r.row_in_block * kEach + v) * kLanes + r.lane] = dw[v / kVec][v % kVec];
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < (uint32_t)(kEach * kLanes); i += Row::kThreads) {
+            const uint32_t v = i / kLanes, l = i % kLanes, j = (v / kVec * kLanes + l) * kVec + v % kVec;
+            float sum = 0.0f;
+            for (int g = 0; g < Row::kRows; ++g) sum += joined[g * kEach * kLanes + i];
+            if (j < a.width) part[j] = sum;
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) {
+            Pack<float, kVec> out;
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) out.v[k] = dw[q][k];
+            if (r.valid(q) > 0) store_pack<kVec>(part + r.place(q), r.valid(q), out);
+        }
+    }
+}
+
+// Rows too long for registers, over 32768 values: a workgroup goes through them twice and finds them in the caches the second
+// time.  kLongEach packs a thread at a time, so that as many loads are on their way; f(pack numbers, valid counts).
+constexpr int kRmsLongEach = 4;
+template <int kVec, class F>
+__device__ __forceinline__ void for_long(uint32_t width, F f)
+{
+    const uint32_t step = kRmsLongThreads * kVec;
+    for (uint32_t begin = 0; begin < width; begin += std::min(step * kRmsLongEach, width - begin)) {
+        uint32_t at[kRmsLongEach];
+        int valid[kRmsLongEach];
+#pragma unroll
+        for (int q = 0; q < kRmsLongEach; ++q) {
+            at[q] = begin + q * step + threadIdx.x * kVec;
+            valid[q] = (int)min(width - min(at[q], width), (uint32_t)kVec);
+        }
+        f(at, valid);
+    }
+}
+template <int kVec, class T>
+__device__ __forceinline__ Pack<T, kVec> long_pack(const T *p, uint32_t at, int valid)
+{
+    return load_pack<kVec>(p + (valid > 0 ? at : 0), valid);
+}
+
+template <class T, class W>
+__global__ __launch_bounds__(kRmsLongThreads) void k_rms_forward_long(RmsArgs a)
+{
+    constexpr int kVec = 16 / sizeof(T), kWaves = kRmsLongThreads / 64;
+    __shared__ float room[kWaves];
+    const W *weight = (const W *)a.weight;
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *x = (const T *)a.x + row * a.x_stride, *add = a.add ? (const T *)a.add + row * a.add_stride : nullptr;
+        T *sum = a.sum ? (T *)a.sum + row * a.sum_stride : nullptr;
+        float square = 0.0f;
+        for_long<kVec>(a.width, [&](const auto &at, const auto &valid) {
+            Pack<T, kVec> t[kRmsLongEach], u[kRmsLongEach];
+#pragma unroll
+            for (int q = 0; q < kRmsLongEach; ++q) {
+                t[q] = long_pack<kVec>(x, at[q], valid[q]);
+                if (add) u[q] = long_pack<kVec>(add, at[q], valid[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < kRmsLongEach; ++q) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    if (add) t[q].v[k] = (T)(widen(t[q].v[k]) + widen(u[q].v[k]));
+                    square = __builtin_fmaf(widen(t[q].v[k]), widen(t[q].v[k]), square);
+                }
+                if (sum && valid[q] > 0) store_pack<kVec>(sum + at[q], valid[q], t[q]);
+            }
+        });
+        const float rstd = 1.0f / sqrtf(block_reduce<kWaves>(square, Sum(), room) / (float)a.width + a.eps);
+        if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
+        // what a thread has put down as the sum it finds there itself; the sum may have taken x's or add's place
+        const T *again = sum ? sum : x, *more = sum ? nullptr : add;
+        if (a.y || a.y8.code)
+            for_long<kVec>(a.width, [&](const auto &at, const auto &valid) {
+                Pack<T, kVec> t[kRmsLongEach], u[kRmsLongEach];
+                Pack<W, kVec> w[kRmsLongEach];
+#pragma unroll
+                for (int q = 0; q < kRmsLongEach; ++q) {
+                    t[q] = long_pack<kVec>(again, at[q], valid[q]);
+                    if (more) u[q] = long_pack<kVec>(more, at[q], valid[q]);
+                    if (weight) w[q] = long_pack<kVec>(weight, at[q], valid[q]);
+                }
+#pragma unroll
+                for (int q = 0; q < kRmsLongEach; ++q) {
+                    float v[kVec];
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int k = 0; k < kVec; ++k) {
+                        if (more) t[q].v[k] = (T)(widen(t[q].v[k]) + widen(u[q].v[k]));
+                        v[k] = widen(t[q].v[k]) * rstd * (weight ? widen(w[q].v[k]) : 1.0f);
+                        t[q].v[k] = (T)v[k];
+                        m = max(m, size_bits(v[k]));
+                    }
+                    if (a.y && valid[q] > 0) store_pack<kVec>((T *)a.y + row * a.y_stride + at[q], valid[q], t[q]);
+                    if (a.y8.code)
+                        put_codes<kVec>(a.y8, (uint32_t)row, at[q], valid[q], v, lanes_reduce<(int)kBlock8 / kVec>(m, Max()), at[q] % kBlock8 == 0);
+                }
+            });
+        __syncthreads();
+    }
+}
+
+template <class T, class W>
+__global__ __launch_bounds__(kRmsLongThreads) void k_rms_dx_long(RmsArgs a)
+{
+    constexpr int kVec = 16 / sizeof(T), kWaves = kRmsLongThreads / 64;
+    __shared__ float room[kWaves];
+    const W *weight = (const W *)a.weight;
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *h = (const T *)a.x + row * a.x_stride, *dy = (const T *)a.dy + row * a.y_stride;
+        const T *ds = a.dsum ? (const T *)a.dsum + row * a.add_stride : nullptr;
+        T *dx = (T *)a.dx + row * a.sum_stride;
+        const float rstd = a.rstd_in[row];
+        float along = 0.0f;
+        for_long<kVec>(a.width, [&](const auto &at, const auto &valid) {
+            Pack<T, kVec> th[kRmsLongEach], td[kRmsLongEach];
+            Pack<W, kVec> w[kRmsLongEach];
+#pragma unroll
+            for (int q = 0; q < kRmsLongEach; ++q) {
+                th[q] = long_pack<kVec>(h, at[q], valid[q]), td[q] = long_pack<kVec>(dy, at[q], valid[q]);
+                if (weight) w[q] = long_pack<kVec>(weight, at[q], valid[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < kRmsLongEach; ++q)
+#pragma unroll
+                for (int k = 0; k < kVec; ++k)
+                    along = __builtin_fmaf(widen(td[q].v[k]) * (widen(th[q].v[k]) * rstd), weight ? widen(w[q].v[k]) : 1.0f, along);
+        });
+        const float c = block_reduce<kWaves>(along, Sum(), room) / (float)a.width;
+        for_long<kVec>(a.width, [&](const auto &at, const auto &valid) {
+            Pack<T, kVec> th[kRmsLongEach], td[kRmsLongEach], ts[kRmsLongEach];
+            Pack<W, kVec> w[kRmsLongEach];
+#pragma unroll
+            for (int q = 0; q < kRmsLongEach; ++q) {
+                th[q] = long_pack<kVec>(h, at[q], valid[q]), td[q] = long_pack<kVec>(dy, at[q], valid[q]);
+                if (weight) w[q] = long_pack<kVec>(weight, at[q], valid[q]);
+                if (ds) ts[q] = long_pack<kVec>(ds, at[q], valid[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < kRmsLongEach; ++q) {
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    float v = rstd * (widen(td[q].v[k]) * (weight ? widen(w[q].v[k]) : 1.0f) - widen(th[q].v[k]) * rstd * c);
+                    if (ds) v += widen(ts[q].v[k]);
+                    td[q].v[k] = (T)v;
+                }
+                if (valid[q] > 0) store_pack<kVec>(dx + at[q], valid[q], td[q]);
+            }
+        });
+        __syncthreads();
+    }
+}
+
+// A pack of columns a thread, the rows in num_parts runs; before dx, which may take dy's place.
+template <class T>
+__global__ __launch_bounds__(256) void k_rms_parts(RmsArgs a)
+{
+    constexpr int kVec = 16 / sizeof(T);
+    const uint64_t place = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * kVec;
+    if (place >= a.width) return;
+    const uint32_t column = std::min((uint32_t)place, a.width - kVec);
+    float dw[kVec] = {};
+#pragma unroll 4
+    for (uint64_t row = blockIdx.y; row < a.rows; row += a.num_parts) {
+        const auto th = *(const Pack<T, kVec> *)((const T *)a.x + row * a.x_stride + column), td = *(const Pack<T, kVec> *)((const T *)a.dy + row * a.y_stride + column);
+        const float rstd = a.rstd_in[row];
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) dw[k] += widen(td.v[k]) * (widen(th.v[k]) * rstd);
+    }
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) a.parts[(size_t)blockIdx.y * a.width + column + k] = dw[k];
+}
+
+// The parts added up: 64 columns a workgroup at a time, each by sixteen threads that take every sixteenth part.
+template <class W>
+__global__ __launch_bounds__(1024) void k_rms_join(RmsArgs a)
+{
+    __shared__ float room[16][64];
+    const uint32_t column = threadIdx.x & 63, run = threadIdx.x >> 6;
+    for (uint64_t first = blockIdx.x * 64ull; first < a.width; first += gridDim.x * 64ull) {
+        const uint64_t j = first + column;
+        const float *part = a.parts + j;
+        float sum = 0.0f;
+        if (j < a.width) {
+#pragma unroll 8
+            for (uint32_t p = run; p < a.num_parts; p += 16) sum += part[(size_t)p * a.width];
+        }
+        room[run][column] = sum;
+        __syncthreads();
+        if (run == 0 && j < a.width) {
+            for (int i = 1; i < 16; ++i) sum += room[i][column];
+            ((W *)a.dweight)[j] = (W)sum;
+        }
+        __syncthreads();
+    }
+}
+
+// Calls `go` with the lanes and values a lane that a row of `width` values goes into, or returns false where it is too long: the
+// fewest that it fits, as lanes without values cost as much as others.
+template <class Go>
+static bool rms_row(uint32_t width, Go go)
+{
+    using std::integral_constant;
+    const auto with = [&](auto lanes, auto each) {
+        if (width > (uint32_t)(lanes.value * each.value)) return false;
+        go(lanes, each);
+        return true;
+    };
+    return with(integral_constant<int, 8>(), integral_constant<int, 8>()) || with(integral_constant<int, 32>(), integral_constant<int, 8>()) ||
+           with(integral_constant<int, 64>(), integral_constant<int, 16>()) || with(integral_constant<int, 256>(), integral_constant<int, 8>()) ||
+           with(integral_constant<int, 256>(), integral_constant<int, 16>()) || with(integral_constant<int, 512>(), integral_constant<int, 16>()) ||
+           with(integral_constant<int, 1024>(), integral_constant<int, 16>()) || with(integral_constant<int, 1024>(), integral_constant<int, 32>());
+}
+
+constexpr uint32_t kRmsLongParts = 64, kRmsLongestKept = 16384;
+template <class Row>
+static uint32_t rms_blocks(uint32_t rows, int most_waves)
+{
+    return std::min(div_up(rows, Row::kRows), compute_units() * (uint32_t)(Row::waves(most_waves) * 256 / Row::kThreads));
+}
+// Workgroups of the backward pass: with the weight's gradient each puts down a part, as much as two rows in 32 bits, so that few
+// rows are shared out by four, once half the compute units have one.
+template <class Row>
+static uint32_t rms_backward_blocks(uint32_t rows, bool with_parts)
+{
+    const uint32_t blocks = div_up(rows, Row::kRows), most = rms_blocks<Row>(rows, kRmsBackwardWaves);
+    return with_parts ? std::min(most, std::max(compute_units() / 2, blocks / 4)) : most;
+}
+static size_t rms_workspace(const pilc_rms_shape &s)
+{
+    const uint32_t most = s.width > kRmsLongestKept ? kRmsLongParts : std::max(kRmsLongParts, (uint32_t)kRmsBackwardWaves * compute_units());
+    return std::max<size_t>(256, sizeof(float) * (size_t)std::max(1u, std::min(s.rows, most)) * s.width);
+}
+
+static bool rms_shape_ok(const pilc_rms_shape *s)
+{
+    return s && s->width >= 1 && s->width <= 0x7FFFFFFFu && s->dtype <= PILC_F16 && (s->weight_type == s->dtype || s->weight_type == PILC_F32) &&
+           s->eps >= 0.0f && s->eps < kInf;
+}
+
+}  // namespace pilc
+
+extern "C" {
+using namespace pilc;
+
+int pilc_rms_forward(const pilc_rms_shape *shape, const void *x_dev, const void *add_dev, const void *weight_dev, void *sum_dev, void *y_dev,
+                     const pilc_block8 *y8, float *rstd_dev, void *hip_stream)
+{
+    if (!rms_shape_ok(shape)) return PILC_E_ARG;
+    const auto stride_ok = [&](uint64_t stride) { return stride >= shape->width && stride <= (1ull << 48); };
+    if (!stride_ok(shape->x_stride) || (add_dev && !stride_ok(shape->add_stride)) || (sum_dev && !stride_ok(shape->sum_stride)) ||
+        (y_dev && !stride_ok(shape->y_stride)) || (y8 && (!block8_ok(y8, shape->width) || y8->block_rows != 1)))
+        return PILC_E_ARG;
+    if (shape->rows == 0) return PILC_OK;
+    const size_t bytes = value_bytes(shape->dtype);
+    if (!x_dev || (!sum_dev && !y_dev && !y8 && !rstd_dev) || (y8 && (!y8->code || !y8->scale)) || !aligned_to(x_dev, bytes) ||
+        !aligned_to(add_dev, bytes) || !aligned_to(sum_dev, bytes) || !aligned_to(y_dev, bytes) || !aligned_to(rstd_dev, 4) ||
+        !aligned_to(weight_dev, value_bytes(shape->weight_type)) || (sum_dev && sum_dev == x_dev && shape->sum_stride != shape->x_stride) ||
+        (sum_dev && sum_dev == add_dev && shape->sum_stride != shape->add_stride) || (y_dev && y_dev == x_dev && shape->y_stride != shape->x_stride) ||
+        (y_dev && (y_dev == sum_dev || y_dev == add_dev)))
+        return PILC_E_ARG;
+    RmsArgs a = {};
+    a.x = x_dev, a.add = add_dev, a.weight = weight_dev, a.sum = sum_dev, a.y = y_dev, a.rstd = rstd_dev;
+    if (y8) a.y8 = block8_of(*y8);
+    a.x_stride = shape->x_stride, a.add_stride = shape->add_stride, a.sum_stride = shape->sum_stride, a.y_stride = shape->y_stride;
+    a.rows = shape->rows, a.width = shape->width, a.eps = shape->eps;
+    return by_types(shape->dtype, shape->weight_type, [&](auto *t, auto *w) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        using W = std::remove_pointer_t<decltype(w)>;
+        if (!rms_row(a.width, [&](auto lanes, auto each) {
+                using Row = RmsRow<T, W, decltype(lanes)::value, decltype(each)::value>;
+                k_rms_forward_rows<T, W, decltype(lanes)::value, decltype(each)::value>
+                    <<<rms_blocks<Row>(a.rows, kRmsForwardWaves), Row::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+            }))
+            k_rms_forward_long<T, W><<<std::min(a.rows, 1u << 20), kRmsLongThreads, 0, (hipStream_t)hip_stream>>>(a);
+    });
+}
+
+int pilc_rms_workspace_size(const pilc_rms_shape *shape, size_t *workspace_bytes_host)
+{
+    if (!rms_shape_ok(shape) || !workspace_bytes_host) return PILC_E_ARG;
+    *workspace_bytes_host = rms_workspace(*shape);
+    return PILC_OK;
+}
+
+int pilc_rms_backward(const pilc_rms_shape *shape, const void *dy_dev, const void *h_dev, const void *weight_dev, const float *rstd_dev,
+                      const void *dsum_dev, void *dx_dev, void *dweight_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    if (!rms_shape_ok(shape) || (!dx_dev && !dweight_dev)) return PILC_E_ARG;
+    const auto stride_ok = [&](uint64_t stride) { return stride >= shape->width && stride <= (1ull << 48); };
+    if (!stride_ok(shape->x_stride) || !stride_ok(shape->y_stride) || (dsum_dev && !stride_ok(shape->add_stride)) || (dx_dev && !stride_ok(shape->sum_stride)))
+        return PILC_E_ARG;
+    const size_t bytes = value_bytes(shape->dtype), weight_bytes = value_bytes(shape->weight_type);
+    if ((shape->rows && (!dy_dev || !h_dev || !rstd_dev)) || !aligned_to(dy_dev, bytes) || !aligned_to(h_dev, bytes) || !aligned_to(dsum_dev, bytes) ||
+        !aligned_to(dx_dev, bytes) || !aligned_to(weight_dev, weight_bytes) || !aligned_to(dweight_dev, weight_bytes) || !aligned_to(rstd_dev, 4) ||
+        !workspace_dev || !aligned_to(workspace_dev, 256) || (dx_dev && dx_dev == dy_dev && shape->sum_stride != shape->y_stride) ||
+        (dx_dev && dx_dev == dsum_dev && shape->sum_stride != shape->add_stride) || (dx_dev && dx_dev == h_dev))
+        return PILC_E_ARG;
+    if (workspace_bytes < rms_workspace(*shape)) return PILC_E_WORKSPACE;
+    RmsArgs a = {};
+    a.dy = dy_dev, a.x = h_dev, a.weight = weight_dev, a.rstd_in = rstd_dev, a.dsum = dsum_dev, a.dx = dx_dev, a.dweight = dweight_dev;
+    a.x_stride = shape->x_stride, a.add_stride = shape->add_stride, a.sum_stride = shape->sum_stride, a.y_stride = shape->y_stride;
+    a.rows = shape->rows, a.width = shape->width;
+    if (dweight_dev) a.parts = (float *)workspace_dev;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    return by_types(shape->dtype, shape->weight_type, [&](auto *t, auto *w) {
+        using T = std::remove_pointer_t<decltype(t)>;
+        using W = std::remove_pointer_t<decltype(w)>;
+        const auto parts = [&] {
+            a.num_parts = std::min(a.rows, kRmsLongParts);
+            if (a.parts && a.rows) k_rms_parts<T><<<dim3(div_up(a.width, 256 * 16 / sizeof(T)), a.num_parts), 256, 0, stream>>>(a);
+        };
+        if (!rms_row(a.width, [&](auto lanes, auto each) {
+                using Row = RmsRow<T, W, decltype(lanes)::value, decltype(each)::value>;
+                if (!Row::kKeep) parts();
+                const uint32_t blocks = rms_backward_blocks<Row>(a.rows, Row::kKeep && a.parts);
+                static_assert(Row::waves(kRmsBackwardWaves) * 256 / Row::kThreads <= kRmsBackwardWaves &&
+                              Row::kKeep == (decltype(lanes)::value * decltype(each)::value <= (int)kRmsLongestKept));
+                if (Row::kKeep) a.num_parts = blocks;
+                if (a.rows && (Row::kKeep || a.dx))
+                    k_rms_backward_rows<T, W, decltype(lanes)::value, decltype(each)::value><<<blocks, Row::kThreads, 0, stream>>>(a);
+            })) {
+            parts();
+            if (a.dx && a.rows) k_rms_dx_long<T, W><<<std::min(a.rows, 1u << 20), kRmsLongThreads, 0, stream>>>(a);
+        }
+        if (a.parts) k_rms_join<W><<<std::min(div_up(a.width, 64), 1u << 20), 1024, 0, stream>>>(a);
+    });
+}
+
+}  // extern "C"

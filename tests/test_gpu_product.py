@@ -1,0 +1,180 @@
+"""pilc_block8_product against 64 bits: products of 8-bit values are exact, so only the sums may be off."""
+import numpy as np
+import pytest
+import torch
+
+from block8_util import DEV, holding, room, workspace
+from fit_util import TYPES, UNIT, close, placed, up
+from oracle import block8_oracle as orc
+from paper_2206_05279_amd import binding as pb
+
+pytestmark = pytest.mark.gpu
+
+#        rows cols depth
+SIZES = [(1, 1, 1), (1, 16, 128), (1, 256, 130), (2, 1000, 4096), (3, 5, 17), (16, 16, 128), (17, 33, 257), (31, 512, 1024), (33, 100, 96), (64, 64, 640),
+         (65, 129, 384), (100, 300, 1000), (128, 128, 4100), (130, 127, 2048), (200, 520, 128), (257, 260, 144), (300, 1, 999), (512, 512, 512), (5, 40, 20000)]
+
+
+def inputs(rows, depth, seed):
+    rng = np.random.default_rng(seed)
+    x = rng.normal(size=(rows, depth)) * np.exp(rng.normal(size=(1, depth)))
+    x[:, rng.integers(0, depth, max(1, depth // 300))] *= 30
+    return x * np.exp(rng.normal(size=(rows, 1)) * 2)
+
+
+def beyond_or_within(c, want, err, dtype, what):
+    """As `close`, but for sums at the border of the type's range.  A number turns into an infinity from `most` and half its last
+    step on, most (1 + UNIT / 2); a sum that may be off by err may lie on either side of that if it is not further than err
+    and a rounding from it.  There either answer is right: an infinity of its sign, or a number within the bound."""
+    got, most = up(c), float(torch.finfo(dtype).max)
+    border = most * (1 + UNIT[dtype][0] / 2)
+    near = np.isfinite(want) & (np.abs(np.abs(want) - border) <= err + 2 * UNIT[dtype][0] * most)
+    right = np.where(np.isinf(got), np.sign(got) == np.sign(want), np.abs(got - want) <= err + 1.01 * UNIT[dtype][0] * np.abs(want))
+    assert right[near].all(), what
+    close(torch.where(torch.from_numpy(near).to(c.device), 0, c), np.where(near, 0.0, want), err, dtype, what)
+
+
+def run(rows, cols, depth, ka, kb, shared, out, pad=0, shift=0, scale_pad=0, seed=0):
+    a, va = holding(inputs(rows, depth, seed), ka, 1, pad, shift, scale_pad)
+    b, vb = holding(inputs(cols, depth, seed + 1), kb, shared, pad, shift, scale_pad)
+    c, whole = placed(np.full((rows, cols), 55.0), TYPES[out], pad, shift)
+    gaps = torch.isnan(whole)
+    pb.pilc_block8_product(a, b, c, workspace=workspace(pb.pilc_block8_product_workspace_size(rows, cols, depth)))
+    want, err = orc.product(va, vb, out != "f32" and rows > 64)
+    beyond_or_within(c, want, err, TYPES[out], "%s" % ((rows, cols, depth, ka, kb, shared, out),))
+    assert torch.isnan(whole[gaps]).all()
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,cols,depth", SIZES)
+def test_sizes(out, rows, cols, depth):
+    run(rows, cols, depth, "e4m3", "e4m3", 128, out)
+    run(rows, cols, depth, "e5m2", "e4m3", 1, out, pad=5, shift=3, scale_pad=1)
+
+
+@pytest.mark.parametrize("ka", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("kb", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("rows,cols,depth", [(3, 70, 300), (80, 70, 304), (300, 290, 272)])
+def test_types_and_alignment(ka, kb, rows, cols, depth):
+    for pad, shift in ((0, 0), (16, 16), (0, 8), (1, 0)):
+        run(rows, cols, depth, ka, kb, 128, "bf16", pad=pad, shift=shift)
+        run(rows, cols, depth, ka, kb, 1, "f32", pad=pad, shift=shift)
+
+
+def test_both_sides_may_share_scales():
+    x, y = inputs(300, 500, 1), inputs(200, 500, 2)
+    a, va = holding(x, "e4m3", 128)
+    b, vb = holding(y, "e4m3", 128)
+    for out in ("f32", "bf16"):
+        c = torch.empty(300, 200, dtype=TYPES[out], device=DEV)
+        pb.pilc_block8_product(a, b, c, workspace=workspace(pb.pilc_block8_product_workspace_size(300, 200, 500)))
+        want, err = orc.product(va, vb, out != "f32")
+        close(c, want, err, TYPES[out], out)
+
+
+@pytest.mark.parametrize("rows", [2, 100])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_what_is_not_a_number_stays_in_its_row_and_column(rows, out):
+    x, y = inputs(rows, 400, 3), inputs(90, 400, 4)
+    x[1, 130], y[7, 399] = np.nan, np.inf
+    a, va = holding(x, "e4m3")
+    b, vb = holding(y, "e4m3")
+    c = torch.empty(rows, 90, dtype=TYPES[out], device=DEV)
+    pb.pilc_block8_product(a, b, c, workspace=workspace(pb.pilc_block8_product_workspace_size(rows, 90, 400)))
+    bad = torch.isnan(c).cpu().numpy()
+    want = np.zeros((rows, 90), bool)
+    want[1], want[:, 7] = True, True
+    assert np.array_equal(bad, want) and torch.isfinite(c[0, 0])
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows", [1, 70])
+def test_scales_at_their_ends(out, rows):
+    """The largest and smallest scales on one side against the other's opposite: products are of ordinary size."""
+    rng = np.random.default_rng(9)
+    depth, cols = 256, 20
+    a, codes_a, scales_a, _ = room(rows, depth, "e4m3")
+    b, codes_b, scales_b, _ = room(cols, depth, "e4m3")
+    ca, cb = (rng.integers(0x30, 0x48, s).astype(np.uint8) for s in ((rows, depth), (cols, depth)))
+    sa, sb = np.full((rows, 2), 127, np.uint8), np.full((cols, 2), 127, np.uint8)
+    sa[:, 0], sb[:, 0], sa[:, 1], sb[:, 1] = 127 + 100, 127 - 100, 127 - 90, 127 + 90
+    for t, v in ((codes_a, ca), (codes_b, cb), (scales_a, sa), (scales_b, sb)):
+        t.copy_(torch.from_numpy(v))
+    c = torch.empty(rows, cols, dtype=TYPES[out], device=DEV)
+    pb.pilc_block8_product(a, b, c, workspace=workspace(pb.pilc_block8_product_workspace_size(rows, cols, depth)))
+    want, err = orc.product(orc.values(ca, sa, "e4m3", 1), orc.values(cb, sb, "e4m3", 1), out != "f32" and rows > 64)
+    close(c, want, err, TYPES[out], out)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 70])
+def test_a_scale_of_255_is_no_number_whatever_the_codes(out, rows):
+    a, va = holding(inputs(rows, 300, 3), "e4m3")
+    b, codes, scales, _ = room(40, 300, "e5m2")
+    codes.fill_(0x3C)
+    scales.fill_(127)
+    scales[5, 1] = 255
+    c = torch.empty(rows, 40, dtype=TYPES[out], device=DEV)
+    pb.pilc_block8_product(a, b, c, workspace=workspace(pb.pilc_block8_product_workspace_size(rows, 40, 300)))
+    bad = torch.isnan(c).all(0).cpu().numpy()
+    assert bad[5] and bad.sum() == 1 and torch.isfinite(c[:, :5]).all()
+
+
+def test_no_depth_is_zero_and_nothing_is_no_error():
+    for rows, cols in ((3, 5), (200, 130)):
+        a, b = room(rows, 0, "e4m3")[0], room(cols, 0, "e4m3")[0]
+        c = torch.full((rows, cols), 3.0, device=DEV)
+        pb.pilc_block8_product(a, b, c, workspace=workspace(256))
+        assert (c == 0).all()
+    pb.pilc_block8_product(room(0, 128, "e4m3")[0], room(4, 128, "e4m3")[0], torch.empty(0, 4, device=DEV), workspace=workspace(256))
+
+
+def test_codes_beyond_32_bits():
+    """Rows whose first code lies over 2^32 bytes in, on both sides."""
+    depth, rows, cols = 65536, 66000, 3
+    a = torch.zeros(rows, depth, dtype=torch.uint8, device=DEV)
+    sa = torch.full((rows, depth // 128), 127, dtype=torch.uint8, device=DEV)
+    rng = np.random.default_rng(3)
+    some = [0, 65536, 65999]
+    v = rng.integers(0x28, 0x40, (3, depth)).astype(np.uint8)
+    a[some] = torch.from_numpy(v).to(DEV)
+    y = inputs(cols, depth, 5)
+    b, vb = holding(y, "e4m3")
+    held = pb.make_block8(a.view(torch.float8_e4m3fn), sa)
+    want, err = orc.product(orc.decode(v, "e4m3"), vb, True)
+    for left, right, c in ((held, b, torch.empty(rows, cols, dtype=torch.bfloat16, device=DEV)), (b, held, torch.empty(cols, rows, dtype=torch.bfloat16, device=DEV))):
+        pb.pilc_block8_product(left, right, c, workspace=workspace(pb.pilc_block8_product_workspace_size(left.rows, right.rows, depth)))
+        got = c if c.shape[0] == rows else c.t()
+        close(got[some].contiguous(), want, err, torch.bfloat16, "far rows")
+        assert (got[1:65536] == 0).all()
+
+
+@pytest.mark.parametrize("rows,cols,depth,out", [(1, 300, 5000, "bf16"), (40, 70, 20000, "f32"), (300, 300, 4096, "bf16"), (520, 780, 1024, "f16"), (256, 256, 32768, "f32")])
+def test_same_bits_every_time_on_other_streams_and_in_a_graph(rows, cols, depth, out):
+    a, codes_a, scales_a, _ = room(rows, depth, "e4m3")
+    b, _, _, _ = room(cols, depth, "e4m3", 128)
+    ws = workspace(pb.pilc_block8_product_workspace_size(rows, cols, depth))
+    c = torch.empty(rows, cols, dtype=TYPES[out], device=DEV)
+    x = torch.randn(rows, depth, device=DEV)
+    pb.pilc_block8_quantize(torch.randn(cols, depth, device=DEV), b)
+    pb.pilc_block8_quantize(x, a)
+    pb.pilc_block8_product(a, b, c, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = torch.empty_like(c)
+    pb.pilc_block8_product(a, b, other, workspace=workspace(ws.numel()), stream=side)
+    side.synchronize()
+    assert torch.equal(c, other)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        pb.pilc_block8_product(a, b, c, workspace=ws)
+    for _ in range(4):
+        pb.pilc_block8_quantize(x.normal_(), a)
+        pb.pilc_block8_product(a, b, c, workspace=ws)
+        torch.cuda.synchronize()
+        first = c.clone()
+        ws.fill_(0x77)
+        c.fill_(3)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(first, c)
