@@ -9,7 +9,7 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libpilc.so")
-SOURCES = [os.path.join(CSRC, name) for name in ("pilc.hip", "pilc_fit.hip", "pilc_block8.hip")]
+SOURCES = [os.path.join(CSRC, name) for name in ("pilc.hip", "pilc_fit.hip", "pilc_block8.hip", "pilc_product.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
