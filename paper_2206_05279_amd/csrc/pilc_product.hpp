@@ -450,12 +450,12 @@ __global__ __launch_bounds__(256, kTile == 256 ? 1 : 2) void k_product_singles(P
     }
 }
 
-// Few rows: b is read once, from memory to registers, and that bounds it.  A workgroup takes 32 columns and shares their depth out
+// Few rows: b is read once, from memory to registers, and that bounds it.  A workgroup takes 16 or 32 columns and shares their depth out
 // among its wavefronts, whose sums meet in LDS.
-template <int kTypeA, int kTypeB, int kRowTiles>
+template <int kTypeA, int kTypeB, int kRowTiles, int kColTiles>
 __global__ __launch_bounds__(512) void k_product_few(ProductArgs p)
 {
-    constexpr int kWaves = 8, kColTiles = 2;
+    constexpr int kWaves = 8;
     __shared__ f32x4_t room[kWaves][kRowTiles * kColTiles][64];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const uint32_t across = div_up(p.cols, 16 * kColTiles);
@@ -466,54 +466,68 @@ __global__ __launch_bounds__(512) void k_product_few(ProductArgs p)
         f32x4_t sum[kRowTiles][kColTiles] = {};
         const uint8_t *a[kRowTiles], *b[kColTiles], *sa[kRowTiles], *sb[kColTiles];
 #pragma unroll
-        for (int i = 0; i < kRowTiles; ++i) a[i] = code_row(p.a, min(i * 16 + r, p.rows - 1)) + g * 32, sa[i] = scale_row(p.a, min(i * 16 + r, p.rows - 1));
+        for (int i = 0; i < kRowTiles; ++i) a[i] = code_row(p.a, min(i * 16 + r, p.rows - 1)) + g * 16, sa[i] = scale_row(p.a, min(i * 16 + r, p.rows - 1));
 #pragma unroll
-        for (int j = 0; j < kColTiles; ++j) b[j] = code_row(p.b, min(col0 + j * 16 + r, p.cols - 1)) + g * 32, sb[j] = scale_row(p.b, min(col0 + j * 16 + r, p.cols - 1));
-        const auto add = [&](const u32x4_t (&ca)[kRowTiles][2], const u32x4_t (&cb)[kColTiles][2], const uint32_t (&ea)[kRowTiles], const uint32_t (&eb)[kColTiles]) {
+        for (int j = 0; j < kColTiles; ++j) b[j] = code_row(p.b, min(col0 + j * 16 + r, p.cols - 1)) + g * 16, sb[j] = scale_row(p.b, min(col0 + j * 16 + r, p.cols - 1));
+        struct Held {
+            u32x4_t a[kRowTiles][2], b[kColTiles][2];
+            uint32_t ea[kRowTiles], eb[kColTiles];
+        };
+        const auto add = [&](const Held &h) {
 #pragma unroll
             for (int part = 0; part < 4; ++part) {
                 bf16x8_t wb[kColTiles];
 #pragma unroll
-                for (int j = 0; j < kColTiles; ++j) wb[j] = widen8<kTypeB>(cb[j][part / 2], part % 2, scale_value(eb[j]));
+                for (int j = 0; j < kColTiles; ++j) wb[j] = widen8<kTypeB>(h.b[j][part / 2], part % 2, scale_value(h.eb[j]));
 #pragma unroll
                 for (int i = 0; i < kRowTiles; ++i) {
-                    const bf16x8_t wa = widen8<kTypeA>(ca[i][part / 2], part % 2, scale_value(ea[i]));
+                    const bf16x8_t wa = widen8<kTypeA>(h.a[i][part / 2], part % 2, scale_value(h.ea[i]));
 #pragma unroll
                     for (int j = 0; j < kColTiles; ++j) sum[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j], wa, sum[i][j], 0, 0, 0);
                 }
             }
         };
         const uint32_t whole = min(last, p.depth / kBlock8);
-        u32x4_t ca[kRowTiles][2], cb[kColTiles][2];
-        uint32_t ea[kRowTiles], eb[kColTiles];
-        for (uint32_t block = first + wave; block < whole; block += kWaves) {
+        const auto fetch = [&](Held &h, uint32_t block) {
             const uint64_t at = (uint64_t)block * kBlock8;
 #pragma unroll
             for (int j = 0; j < kColTiles; ++j) {
-                cb[j][0] = Raw<uint8_t>::load(b[j] + at).bits, cb[j][1] = Raw<uint8_t>::load(b[j] + at + 16).bits;
-                eb[j] = sb[j][block];
+                h.eb[j] = sb[j][block];
+                h.b[j][0] = Raw<uint8_t>::load(b[j] + at).bits, h.b[j][1] = Raw<uint8_t>::load(b[j] + at + 64).bits;
             }
 #pragma unroll
             for (int i = 0; i < kRowTiles; ++i) {
-                ca[i][0] = Raw<uint8_t>::load(a[i] + at).bits, ca[i][1] = Raw<uint8_t>::load(a[i] + at + 16).bits;
-                ea[i] = sa[i][block];
+                h.ea[i] = sa[i][block];
+                h.a[i][0] = Raw<uint8_t>::load(a[i] + at).bits, h.a[i][1] = Raw<uint8_t>::load(a[i] + at + 64).bits;
             }
-            add(ca, cb, ea, eb);
+        };
+        // the next block is on its way while one is worked on
+        Held h[2];
+        uint32_t block = first + wave;
+        if (block < whole) fetch(h[0], block);
+        while (block < whole) {
+            fetch(h[1], min(block + kWaves, whole - 1));
+            add(h[0]);
+            block += kWaves;
+            if (block >= whole) break;
+            fetch(h[0], min(block + kWaves, whole - 1));
+            add(h[1]);
+            block += kWaves;
         }
         if (whole < last && wave == (whole - first) % kWaves) {
 #pragma unroll
             for (int j = 0; j < kColTiles; ++j) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) cb[j][h] = product_chunk(b[j] - g * 32, whole * kBlock8 + g * 32 + h * 16, p.depth);
-                eb[j] = sb[j][whole];
+                for (int n = 0; n < 2; ++n) h[0].b[j][n] = product_chunk(b[j] - g * 16, whole * kBlock8 + g * 16 + n * 64, p.depth);
+                h[0].eb[j] = sb[j][whole];
             }
 #pragma unroll
             for (int i = 0; i < kRowTiles; ++i) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) ca[i][h] = product_chunk(a[i] - g * 32, whole * kBlock8 + g * 32 + h * 16, p.depth);
-                ea[i] = sa[i][whole];
+                for (int n = 0; n < 2; ++n) h[0].a[i][n] = product_chunk(a[i] - g * 16, whole * kBlock8 + g * 16 + n * 64, p.depth);
+                h[0].ea[i] = sa[i][whole];
             }
-            add(ca, cb, ea, eb);
+            add(h[0]);
         }
 #pragma unroll
         for (int i = 0; i < kRowTiles; ++i)
@@ -552,23 +566,29 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs p)
 // not fill the GPU.
 constexpr uint32_t kFewRows = 64;
 struct ProductPlan {
-    uint32_t tile, splits, blocks_each;  // tile 0: few rows
+    uint32_t tile, width, splits, blocks_each;  // tile 0: few rows, `width` columns a workgroup
 };
 static ProductPlan product_plan(uint32_t rows, uint32_t cols, uint32_t depth)
 {
     const uint32_t blocks = div_up(depth, kBlock8), units = compute_units();
-    uint64_t groups;
-    uint32_t tile = 0, least;  // blocks that a split takes at least
+    const auto in_splits = [&](uint32_t tile, uint32_t width, uint64_t groups, uint32_t least) {
+        const uint32_t wanted = (uint32_t)std::max<uint64_t>(1, units / std::max<uint64_t>(groups, 1)), splits = std::max(1u, std::min(wanted, blocks / least));
+        const uint32_t each = std::max(4u, div_up(div_up(blocks, splits), 4) * 4);
+        return ProductPlan{tile, width, std::max(1u, div_up(blocks, each)), each};
+    };
     if (rows <= kFewRows) {
-        groups = div_up(cols, 32), least = 32;
-    } else {
-        tile = (uint64_t)div_up(rows, 256) * div_up(cols, 256) * 2 >= units ? 256 : 128;
-        groups = (uint64_t)div_up(rows, tile) * div_up(cols, tile), least = 8;
-        if (tile == 128) groups = (groups + 1) / 2;  // two on a compute unit
+        const uint32_t width = div_up(cols, 32) >= units ? 32 : 16;
+        return in_splits(0, width, div_up(cols, width), 32);
     }
-    const uint32_t wanted = (uint32_t)std::max<uint64_t>(1, units / std::max<uint64_t>(groups, 1)), splits = std::max(1u, std::min(wanted, blocks / least));
-    const uint32_t each = std::max(4u, div_up(div_up(blocks, splits), 4) * 4);
-    return {tile, std::max(1u, div_up(blocks, each)), each};
+    // what share of the GPU works on what is wanted
+    const auto worth = [&](const ProductPlan &p) {
+        const double groups = (double)div_up(rows, p.tile) * div_up(cols, p.tile) * p.splits, room = p.tile == 256 ? units : 2.0 * units;
+        const double full = groups / (room * std::ceil(groups / room));
+        return full * rows / ((double)div_up(rows, p.tile) * p.tile) * cols / ((double)div_up(cols, p.tile) * p.tile);
+    };
+    const ProductPlan large = in_splits(256, 256, (uint64_t)div_up(rows, 256) * div_up(cols, 256), 8);
+    const ProductPlan small = in_splits(128, 128, ((uint64_t)div_up(rows, 128) * div_up(cols, 128) + 1) / 2, 8);
+    return worth(large) >= 0.6 * worth(small) ? large : small;
 }
 // Whether codes and scales of a matrix can go to LDS without registers.
 static bool product_direct(const pilc_block8 &m, uint32_t blocks)
@@ -620,17 +640,21 @@ int pilc_block8_product(uint32_t rows, uint32_t cols, uint32_t depth, const pilc
     p.rows = rows, p.cols = cols, p.depth = depth, p.c_type = c_type, p.blocks = div_up(depth, kBlock8);
     p.splits = plan.splits, p.blocks_each = plan.blocks_each;
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const uint64_t groups = plan.tile ? (uint64_t)div_up(cols, plan.tile) * div_up(rows, plan.tile) : div_up(cols, 32);
+    const uint64_t groups = plan.tile ? (uint64_t)div_up(cols, plan.tile) * div_up(rows, plan.tile) : div_up(cols, plan.width);
     const uint32_t grid = (uint32_t)std::min<uint64_t>(groups * plan.splits, 1u << 20);
     const bool direct = product_direct(*a, p.blocks) && product_direct(*b, p.blocks);
     by_types8(a->type, b->type, [&](auto ta, auto tb) {
         constexpr int kA = decltype(ta)::value, kB = decltype(tb)::value;
         if (plan.tile == 0) {
+            const auto few = [&](auto row_tiles) {
+                constexpr int kRowTiles = decltype(row_tiles)::value;
+                plan.width == 32 ? k_product_few<kA, kB, kRowTiles, 2><<<grid, 512, 0, stream>>>(p) : k_product_few<kA, kB, kRowTiles, 1><<<grid, 512, 0, stream>>>(p);
+            };
             switch (div_up(rows, 16)) {
-            case 1: k_product_few<kA, kB, 1><<<grid, 512, 0, stream>>>(p); break;
-            case 2: k_product_few<kA, kB, 2><<<grid, 512, 0, stream>>>(p); break;
-            case 3: k_product_few<kA, kB, 3><<<grid, 512, 0, stream>>>(p); break;
-            default: k_product_few<kA, kB, 4><<<grid, 512, 0, stream>>>(p); break;
+            case 1: few(std::integral_constant<int, 1>()); break;
+            case 2: few(std::integral_constant<int, 2>()); break;
+            case 3: few(std::integral_constant<int, 3>()); break;
+            default: few(std::integral_constant<int, 4>()); break;
             }
         } else if (c_type == PILC_F32) {
             plan.tile == 256 ? k_product_singles<kA, kB, 256><<<grid, 256, 0, stream>>>(p) : k_product_singles<kA, kB, 128><<<grid, 256, 0, stream>>>(p);
