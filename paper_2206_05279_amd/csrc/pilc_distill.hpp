@@ -5,8 +5,8 @@ namespace pilc {
 
 // Per row of logits x, f = 1 / temperature: M = max x and S = sum of e^(f (x - M)) over the bulk, which is all symbols, or with `rest`
 // those that are not named.  The gradient of a bulk symbol is e^(f (x - M)) times one number of the row's, and the named symbols,
-// at most 128, are looked at one by one: their logits are fetched by themselves, and their gradients put in their places after the
-// bulk's.  So a row is read once, into registers, and gone through as in pilc_logprobs.  A loss is a small difference
+// at most 128, are looked at one by one: their logits are fetched by themselves, and their gradients put in the places of the
+// bulk's before those are stored.  So a row is read once, into registers, and gone through as in pilc_logprobs.  A loss is a small difference
 // of large logarithms where student and teacher agree: the named symbols' terms are added up in 64 bits, of differences
 // that are taken first.
 
@@ -48,122 +48,24 @@ struct Moves {
 struct Or {
     __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a | b; }
 };
+// As lanes_reduce, in 64 bits.
+template <int kDpp>
+__device__ __forceinline__ double from_partner64(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)from_partner<kDpp>((uint32_t)(b >> 32)) << 32 | from_partner<kDpp>((uint32_t)b));
+}
 template <int kLanes>
 __device__ __forceinline__ double lanes_sum(double v)
 {
-    for (int d = 1; d < kLanes; d *= 2) v += __shfl_xor(v, d, 64);
+    if constexpr (kLanes >= 2) v += from_partner64<0xB1>(v);
+    if constexpr (kLanes >= 4) v += from_partner64<0x4E>(v);
+    if constexpr (kLanes >= 8) v += from_partner64<0x141>(v);
+    if constexpr (kLanes >= 16) v += from_partner64<0x140>(v);
+    if constexpr (kLanes >= 32) v += __shfl_xor(v, 16, 64);
+    if constexpr (kLanes >= 64) v += __shfl_xor(v, 32, 64);
     return v;
 }
-
-// The entries of a row, in LDS, gone through by kLanes lanes of a wavefront.
-template <int kLanes>
-struct Named {
-    static constexpr uint32_t kAny = 1, kSpoilt = 2;
-    int32_t *sym;
-    float *value, *x;  // `value` becomes q, `x` the entry's gradient
-    uint32_t lane, top, flags;
-
-    __device__ Named(void *room, uint32_t t) : sym((int32_t *)room), value((float *)room + t), x((float *)room + 2 * t), lane(threadIdx.x % kLanes), top(t), flags(0) {}
-    __device__ static size_t bytes(uint32_t top) { return 12 * (size_t)top; }
-
-    template <class T>
-    __device__ void load(const DistillArgs &a, uint32_t row)
-    {
-        const T *logits = (const T *)a.x + (uint64_t)row * a.stride;
-        uint32_t own = 0;
-        for (uint32_t i = lane; i < top; i += kLanes) {
-            const int32_t s = a.sym[(uint64_t)row * top + i];
-            const float v = a.value[(uint64_t)row * top + i];
-            const bool in = s >= 0 && (uint32_t)s < a.num_sym;
-            const float at = in ? widen(logits[s]) : 0.0f;
-            if (s >= 0) own |= in && v < kInf && at < kInf ? kAny : kAny | kSpoilt;
-            sym[i] = in ? s : -1, value[i] = v, x[i] = at;
-        }
-        flags = lanes_reduce<kLanes>(own, Or());
-    }
-    template <class F>
-    __device__ void each(F f) const
-    {
-        for (uint32_t i = lane; i < top; i += kLanes)
-            if (sym[i] >= 0) f(i);
-    }
-
-    // The row's loss, and what moves its bulk and its entries.  Entries of the same symbol have their q's together.
-    template <bool kRest>
-    __device__ Moves settle(const DistillArgs &a, Bulk bulk, float up, float &loss)
-    {
-        if (!(flags & kAny)) {
-            loss = 0.0f;
-            each([&](uint32_t i) { x[i] = 0.0f; });
-            return {bulk.max, 0.0f, true};
-        }
-        const float factor = distill_factor(a);
-        const bool spoilt = (flags & kSpoilt) || !(bulk.total == bulk.total);
-        float max = bulk.max, most = -kInf;
-        each([&](uint32_t i) {
-            if (kRest) max = fmaxf(max, x[i]);
-            most = fmaxf(most, value[i]);
-        });
-        if (kRest) max = lanes_reduce<kLanes>(max, MaxFloat());
-        most = center_of(lanes_reduce<kLanes>(most, MaxFloat()));
-        const float center = center_of(max);
-        const bool lawless = max == -kInf;
-        // q, and with kRest the student's sum over named symbols, each once
-        float weight = 0.0f, mass = 0.0f;
-        each([&](uint32_t i) {
-            const float q = kRest ? expf(value[i]) : expf((value[i] - most) * a.turn);
-            weight += q;
-            if constexpr (kRest) {
-                bool first = true;
-                for (uint32_t j = 0; j < i; ++j) first &= sym[j] != sym[i];
-                if (first) mass += exp2_fast((x[i] - center) * factor);
-            }
-        });
-        double all = lanes_sum<kLanes>((double)weight);
-        const float norm = kRest || all == 0.0 ? 1.0f : 1.0f / (float)all;
-        const float beside = kRest ? bulk.total * exp2_fast((bulk.max - center) * factor) : 0.0f;  // the bulk's share of the sum
-        const float total = kRest ? beside + lanes_reduce<kLanes>(mass, Sum()) : bulk.total;
-        double sum = 0.0;
-        bool never = false;  // a symbol with q > 0 that the student rules out
-        each([&](uint32_t i) {
-            const float q = (kRest ? expf(value[i]) : expf((value[i] - most) * a.turn)) * norm;
-            if (q > 0.0f) {
-                never |= x[i] == -kInf;
-                const double mine = ((double)x[i] - center) * a.turn;
-                sum += q * ((kRest ? (double)value[i] : ((double)value[i] - most) * a.turn) - (x[i] == -kInf ? 0.0 : mine));
-            }
-            value[i] = q;
-        });
-        sum = lanes_sum<kLanes>(sum);
-        never = lanes_reduce<kLanes>((uint32_t)never, Or());
-        const bool weighted = all > 0.0;
-        const double log_total = log((double)total);
-        float share;  // of the bulk's powers, before up / temperature
-        if constexpr (kRest) {
-            const double left = bulk.total > 0.0f ? fmax(0.0, 1.0 - all) : 0.0;
-            sum += all * log_total;
-            if (left > 0.0) sum += left * (log(left) - (((double)bulk.max - center) * a.turn + log((double)bulk.total) - log_total));
-            share = bulk.total > 0.0f ? (beside / total - (float)left) / bulk.total : 0.0f;
-        } else {
-            if (weighted) sum += log_total - log(all);
-            share = weighted ? 1.0f / total : 0.0f;
-        }
-        loss = spoilt ? __builtin_nanf("") : lawless || never ? (weighted && (lawless || never) ? kInf : 0.0f) : (float)sum;
-        const float by = up * a.turn;
-        const bool zeros = up == 0.0f || (lawless && !spoilt);
-        if (a.grad) {
-            meet<64>();
-            for (uint32_t i = lane; i < top; i += kLanes) {
-                if (sym[i] < 0) continue;
-                float q = 0.0f;
-                for (uint32_t j = 0; j < top; ++j) q += sym[j] == sym[i] ? value[j] : 0.0f;
-                const float p = kRest || weighted ? exp2_fast((x[i] - center) * factor) / total : 0.0f;
-                x[i] = zeros ? 0.0f : spoilt ? __builtin_nanf("") : by * (p - q);
-            }
-        }
-        return {bulk.max, spoilt ? __builtin_nanf("") : by * share, zeros};
-    }
-};
 
 // The values whose bit is set become -inf.
 template <class T>
@@ -184,31 +86,174 @@ __device__ __forceinline__ void rule_out_bits(Raw<T> &x, uint32_t bits)
     }
 }
 
+// The entries of a row, in LDS, gone through by kLanes lanes of a wavefront.  What hangs on the teacher and on the named symbols' logits
+// alone is worked out while the row is on its way; once the bulk is known a few steps are left.
+template <int kLanes>
+struct Named {
+    static constexpr uint32_t kAny = 1, kSpoilt = 2, kNever = 4;
+    int32_t *sym;
+    float *value, *x, *mass_of;  // the entry's q; its symbol's power, then its gradient; q of all entries of its symbol
+    uint8_t *after;              // 1 + another entry in the same pack of the row, 0: none
+    uint32_t lane, top, flags;
+    float max, mass;   // of the named symbols: the largest logit, the sum of their powers, each once
+    double all, gain;  // sum of q, and of q (ln q - (x - max) / temperature)
+
+    __host__ __device__ static constexpr uint32_t bytes(uint32_t top) { return 16 * top + (top + 3) / 4 * 4; }
+    __device__ Named(void *room, uint32_t t)
+        : sym((int32_t *)room), value((float *)room + t), x((float *)room + 2 * t), mass_of((float *)room + 3 * t), after((uint8_t *)room + 16 * t),
+          lane(threadIdx.x % kLanes), top(t), flags(0)
+    {
+    }
+    template <class F>
+    __device__ void each(F f) const
+    {
+        for (uint32_t i = lane; i < top; i += kLanes)
+            if (sym[i] >= 0) f(i);
+    }
+    template <class T>
+    __device__ void load(const DistillArgs &a, uint32_t row)
+    {
+        const T *logits = (const T *)a.x + (uint64_t)row * a.stride;
+        flags = 0;
+        for (uint32_t i = lane; i < top; i += kLanes) {
+            const int32_t s = a.sym[(uint64_t)row * top + i];
+            const float v = a.value[(uint64_t)row * top + i];
+            const bool in = s >= 0 && (uint32_t)s < a.num_sym;
+            const float at = in ? widen(logits[s]) : 0.0f;
+            if (s >= 0) flags |= in && v < kInf && at < kInf ? kAny : kAny | kSpoilt;
+            sym[i] = in ? s : -1, value[i] = v, x[i] = at;
+        }
+    }
+    // All that does not hang on the bulk.  `marks`, or null: for each pack of kVec symbols 1 + an entry in it, from which `after`
+    // leads to the others; zeros before.
+    template <bool kRest, int kVec>
+    __device__ void prepare(const DistillArgs &a, uint8_t *marks)
+    {
+        const float factor = distill_factor(a);
+        float most = -kInf;
+        max = -kInf;
+        each([&](uint32_t i) {
+            max = fmaxf(max, x[i]);
+            most = fmaxf(most, value[i]);
+        });
+        max = lanes_reduce<kLanes>(max, MaxFloat());
+        most = center_of(lanes_reduce<kLanes>(most, MaxFloat()));
+        const float center = center_of(max);
+        double sum = 0.0, weight = 0.0;
+        each([&](uint32_t i) {
+            const float v = value[i], at = x[i], q = kRest ? expf(v) : expf((v - most) * a.turn);
+            weight += q;
+            if (q > 0.0f) {
+                if (at == -kInf)
+                    flags |= kNever;
+                else
+                    sum += q * ((kRest ? (double)v : ((double)v - most) * a.turn) - ((double)at - center) * a.turn);
+            }
+            value[i] = q;
+            x[i] = exp2_fast((at - center) * factor);
+        });
+        flags = lanes_reduce<kLanes>(flags, Or());
+        all = lanes_sum<kLanes>(weight), gain = lanes_sum<kLanes>(sum);
+        float norm = 1.0f;
+        if constexpr (!kRest)
+            if (all > 0.0) {
+                gain = gain / all - logf((float)all);
+                norm = (float)(1.0 / all);
+                all = 1.0;
+            }
+        mass = 0.0f;
+        if (!kRest && !a.grad) return;
+        meet<64>();
+        each([&](uint32_t i) {
+            const int32_t s = sym[i];
+            float q = 0.0f;
+            uint32_t next = 0;
+            bool first = true, head = true;
+#pragma unroll 4
+            for (uint32_t j = 0; j < top; ++j) {
+                const int32_t t = sym[j];
+                const bool same = t == s, beside = t >= 0 && (uint32_t)t / kVec == (uint32_t)s / kVec;
+                q += same ? value[j] : 0.0f;
+                first &= !same || j >= i;
+                head &= !beside || j <= i;
+                next = beside && j < i ? j + 1 : next;
+            }
+            mass_of[i] = q * norm;
+            after[i] = (uint8_t)next;
+            if (marks && head) marks[(uint32_t)s / kVec] = (uint8_t)(i + 1);
+            if (first) mass += x[i];
+        });
+        mass = lanes_reduce<kLanes>(mass, Sum());
+    }
+    // The student's sum, by the largest value that `center` is made of, and what of it is the bulk's
+    struct Whole {
+        float center, beside, each_power, total;
+        bool spoilt, lawless;
+    };
+    template <bool kRest>
+    __device__ Whole whole(const DistillArgs &a, Bulk bulk) const
+    {
+        const float factor = distill_factor(a), most = kRest ? fmaxf(max, bulk.max) : bulk.max;
+        Whole w;
+        w.center = center_of(most);
+        w.beside = bulk.max == -kInf ? 0.0f : bulk.total * exp2_fast((bulk.max - w.center) * factor);
+        w.each_power = max == -kInf ? 0.0f : exp2_fast((max - w.center) * factor);
+        w.total = kRest ? w.beside + mass * w.each_power : bulk.total;
+        w.spoilt = (flags & kSpoilt) || !(bulk.total == bulk.total);
+        w.lawless = most == -kInf;
+        return w;
+    }
+    // What moves the bulk, and the entries' gradients in the place of their powers
+    template <bool kRest>
+    __device__ Moves moves(const DistillArgs &a, Bulk bulk, float up) const
+    {
+        const Whole w = whole<kRest>(a, bulk);
+        const float left = kRest ? (float)fmax(0.0, 1.0 - all) : 0.0f;
+        const float share = kRest ? (bulk.total > 0.0f ? (w.beside / w.total - left) / bulk.total : 0.0f) : (float)all / w.total;
+        const bool zeros = up == 0.0f || (w.lawless && !w.spoilt) || !(flags & kAny);
+        const float by = w.spoilt ? __builtin_nanf("") : up * a.turn, p = (kRest ? 1.0f : (float)all) * w.each_power / w.total;
+        each([&](uint32_t i) { x[i] = zeros ? 0.0f : by * (x[i] * p - mass_of[i]); });
+        return {bulk.max, by * share, zeros};
+    }
+    // Logarithms in 32 bits: off by 2^-24 of themselves, at most 12 for 2^17 symbols
+    template <bool kRest>
+    __device__ float loss(const DistillArgs &a, Bulk bulk) const
+    {
+        const Whole w = whole<kRest>(a, bulk);
+        const double log_total = logf(w.total), left = kRest && bulk.total > 0.0f ? fmax(0.0, 1.0 - all) : 0.0;
+        double sum = gain + all * (log_total - ((double)center_of(max) - w.center) * a.turn);
+        if (left > 0.0) sum += left * ((double)logf((float)left) - (((double)bulk.max - w.center) * a.turn + logf(bulk.total) - log_total));
+        const bool weighted = all > 0.0;
+        if (!(flags & kAny)) return 0.0f;
+        if (w.spoilt) return __builtin_nanf("");
+        if (w.lawless || (flags & kNever)) return weighted ? kInf : 0.0f;
+        return weighted || kRest ? (float)sum : 0.0f;
+    }
+};
+
 template <class T, int kLanes, int kPer>
 struct DistillRow : LogitsRow<T, kLanes, kPer> {
     using Row = LogitsRow<T, kLanes, kPer>;
     using Row::kVec;
     static constexpr int kEntryLanes = kLanes < 64 ? kLanes : 64;
-    static constexpr size_t kMarks = (size_t)kLanes * kPer;  // bytes, one a pack
+    static constexpr uint32_t kMarks = kLanes * kPer;  // bytes, one a pack
 
-    // Named symbols of columns begin .. end-1 are ruled out: a byte a pack says which of its values are.
-    __device__ void leave_out(const Named<kEntryLanes> &named, bool mine, uint8_t *marks, uint32_t begin, uint32_t end, Raw<T> (&x)[kPer], int used) const
+    __device__ void clear(uint8_t *marks) const
     {
-        const uint32_t lane = this->lane;
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) marks[q * kLanes + lane] = 0;
-        meet<kLanes>();
-        if (mine)
-            named.each([&](uint32_t i) {
-                const uint32_t s = (uint32_t)named.sym[i];
-                if (s < begin || s >= end) return;
-                const uint32_t pack = (s - begin) / kVec, column = min(begin + pack * kVec, end - kVec);
-                atomicOr((uint32_t *)marks + pack / 4, 1u << (pack % 4 * 8 + (s - column)));
-            });
-        meet<kLanes>();
+        for (int q = 0; q < kPer; ++q) marks[q * kLanes + this->lane] = 0;
+    }
+    // Named symbols of columns begin .. end-1 are ruled out.
+    __device__ void leave_out(const Named<kEntryLanes> &named, const uint8_t *marks, uint32_t begin, uint32_t end, Raw<T> (&x)[kPer], int used) const
+    {
         Row::for_used(used, [&](int q) {
-            const uint32_t bits = marks[q * kLanes + lane];
-            if (bits) rule_out_bits(x[q], bits);
+            uint32_t entry = marks[q * kLanes + this->lane];
+            if (entry) {
+                const uint32_t column = this->column(q, begin, end);
+                uint32_t bits = 0;
+                for (; entry; entry = named.after[entry - 1]) bits |= 1u << ((uint32_t)named.sym[entry - 1] - column);
+                rule_out_bits(x[q], bits);
+            }
         });
     }
     // The bulk of all lanes' values, in all lanes.  `room` holds 2 * kWaves, its halves are used in turn.
@@ -231,11 +276,19 @@ struct DistillRow : LogitsRow<T, kLanes, kPer> {
         }
         return t;
     }
-    __device__ void put(const Raw<T> &x, T *to, int twice, float center, float factor, const Moves &m) const
+    // The gradient of a pack's values; of those that are named, from `entry` on, what the entries have.
+    __device__ void put(const Raw<T> &x, T *to, int twice, float center, float factor, const Moves &m, uint32_t entry, uint32_t column,
+                        const Named<kEntryLanes> *named) const
     {
         float d[kVec];
 #pragma unroll
         for (int k = 0; k < kVec; ++k) d[k] = m.zeros ? 0.0f : exp2_fast((x[k] - center) * factor) * m.each;
+        for (; entry; entry = named->after[entry - 1]) {
+            const uint32_t at = (uint32_t)named->sym[entry - 1] - column;
+            const float g = named->x[entry - 1];
+#pragma unroll
+            for (int k = 0; k < kVec; ++k) d[k] = at == (uint32_t)k ? g : d[k];
+        }
         if (twice == 0) {
             Raw<T>::of(d).store(to);
         } else {
@@ -251,53 +304,56 @@ template <class T, int kLanes, int kPer, bool kRest, bool kGrad>
 __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::kResident)) void k_distill(DistillArgs a)
 {
     using Row = DistillRow<T, kLanes, kPer>;
+    constexpr bool kMarked = kRest || kGrad;
     __shared__ Bulk room[2 * Row::kWaves];
     __shared__ Moves shared_moves;
     extern __shared__ uint32_t more_room[];  // the rows' marks, then their entries
     Row r;
     const uint64_t step = (uint64_t)gridDim.x * Row::kRows;
     const float factor = distill_factor(a);
-    uint8_t *marks = (uint8_t *)more_room + (kRest ? r.row_in_block * Row::kMarks : 0);
-    Named<Row::kEntryLanes> named((uint8_t *)more_room + (kRest ? Row::kRows * Row::kMarks : 0) + r.row_in_block * 12 * a.top, a.top);
+    uint8_t *marks = kMarked ? (uint8_t *)more_room + r.row_in_block * Row::kMarks : nullptr;
+    using Entries = Named<Row::kEntryLanes>;
+    Entries named((uint8_t *)more_room + (kMarked ? Row::kRows * Row::kMarks : 0) + r.row_in_block * Entries::bytes(a.top), a.top);
     const bool mine = Row::kWaves <= 1 || threadIdx.x < 64;  // of a row's wavefronts the first sees to the entries
     int half = 0;
     for (uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block; item < a.rows; item += step) {
         const uint32_t row = (uint32_t)item;
         const float up = kGrad ? a.up[row] : 0.0f;
+        if constexpr (kMarked) r.clear(marks);
         Raw<T> x[kPer];
         if (mine) named.template load<T>(a, row);
-        r.load((const T *)a.x + (uint64_t)row * a.stride, 0, a.num_sym, x);
+        // a row's only wavefront asks for it first; where there are more, the others' loads go on meanwhile, and the first has the
+        // registers to itself
+        if constexpr (Row::kWaves <= 1) r.load((const T *)a.x + (uint64_t)row * a.stride, 0, a.num_sym, x);
+        if constexpr (kMarked) meet<kLanes>();
+        if (mine) named.template prepare<kRest, Row::kVec>(a, marks);
+        if constexpr (Row::kWaves > 1) r.load((const T *)a.x + (uint64_t)row * a.stride, 0, a.num_sym, x);
+        if constexpr (kMarked) meet<kLanes>();
         r.rule_out(0, a.num_sym, x);
         const int used = r.used(0, a.num_sym);
-        meet<64>();
-        if constexpr (kRest) r.leave_out(named, mine, marks, 0, a.num_sym, x, used);
+        if constexpr (kRest) r.leave_out(named, marks, 0, a.num_sym, x, used);
         float of[kPer];
         const float own = r.largest(x, used, of);
         r.forget(x);
         const Bulk bulk = r.bulk(x, used, own, factor, room, half);
         r.forget(x);
         half ^= 1;
-        Moves moves = {};
-        if (mine) {
-            float loss;
-            moves = named.template settle<kRest>(a, bulk, up, loss);
-            if (r.lane == 0) {
-                a.loss[row] = loss;
-                if (Row::kWaves > 1) shared_moves = moves;
-            }
-        }
         if constexpr (kGrad) {
-            if constexpr (Row::kWaves > 1) {
-                __syncthreads();
-                moves = shared_moves;
-            }
+            Moves moves = {};
+            if (mine) moves = named.template moves<kRest>(a, bulk, up);
+            if (Row::kWaves > 1 && threadIdx.x == 0) shared_moves = moves;
+            meet<kLanes>();
+            if constexpr (Row::kWaves > 1) moves = shared_moves;
             const float center = center_of(moves.max);
             T *grad = (T *)a.grad + (uint64_t)row * a.grad_stride;
-            Row::for_used(used, [&](int q) { r.put(x[q], Row::address(grad, r.column(q, 0, a.num_sym), 0, a.num_sym), r.twice(q, 0, a.num_sym), center, factor, moves); });
-            // the bulk's stores are done before the entries take their places
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            meet<kLanes>();
-            if (mine) named.each([&](uint32_t i) { grad[named.sym[i]] = (T)named.x[i]; });
+            Row::for_used(used, [&](int q) {
+                const uint32_t column = r.column(q, 0, a.num_sym);
+                r.put(x[q], Row::address(grad, column, 0, a.num_sym), r.twice(q, 0, a.num_sym), center, factor, moves, marks[q * kLanes + r.lane], column, &named);
+            });
+        }
+        if (mine) {
+            const float loss = named.template loss<kRest>(a, bulk);
+            if (r.lane == 0) a.loss[row] = loss;
         }
         meet<kLanes>();
     }
@@ -314,7 +370,6 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
     const uint64_t items = (uint64_t)a.rows * a.splits, step = (uint64_t)gridDim.x * Row::kRows;
     const float factor = distill_factor(a);
     uint8_t *marks = (uint8_t *)more_room + r.row_in_block * Row::kMarks;
-    const bool mine = Row::kWaves <= 1 || threadIdx.x < 64;
     int half = 0;
     for (uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block; item < items; item += step) {
         const uint32_t row = (uint32_t)(item / a.splits), begin = (uint32_t)(item - (uint64_t)row * a.splits) * a.span;
@@ -323,11 +378,20 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         r.load((const T *)a.x + (uint64_t)row * a.stride, begin, end, x);
         r.rule_out(begin, end, x);
         const int used = r.used(begin, end);
-        if constexpr (kRest) {
-            // the entries' symbols are looked at where they lie
-            Named<Row::kEntryLanes> named(nullptr, a.top);
-            named.sym = (int32_t *)a.sym + (uint64_t)row * a.top;
-            r.leave_out(named, mine, marks, begin, end, x, used);
+        if constexpr (kRest) {  // a bit for each named symbol that lies in the run, a byte a pack
+            r.clear(marks);
+            meet<kLanes>();
+            for (uint32_t i = r.lane; i < a.top; i += kLanes) {
+                const uint32_t s = (uint32_t)a.sym[(uint64_t)row * a.top + i];  // a negative one lies behind all
+                if (s < begin || s >= end) continue;
+                const uint32_t pack = (s - begin) / Row::kVec, column = min(begin + pack * Row::kVec, end - Row::kVec);
+                atomicOr((uint32_t *)marks + pack / 4, 1u << (pack % 4 * 8 + (s - column)));
+            }
+            meet<kLanes>();
+            Row::for_used(used, [&](int q) {
+                const uint32_t bits = marks[q * kLanes + r.lane];
+                if (bits) rule_out_bits(x[q], bits);
+            });
         }
         float of[kPer];
         const float own = r.largest(x, used, of);
@@ -343,7 +407,7 @@ template <class T, bool kRest>
 __global__ __launch_bounds__(256) void k_distill_join(DistillArgs a)
 {
     extern __shared__ uint32_t more_room[];
-    Named<64> named((uint8_t *)more_room + (threadIdx.x >> 6) * 12 * a.top, a.top);
+    Named<64> named((uint8_t *)more_room + (threadIdx.x >> 6) * Named<64>::bytes(a.top), a.top);
     const uint32_t lane = threadIdx.x & 63;
     for (uint64_t row = blockIdx.x * 4ull + (threadIdx.x >> 6); row < a.rows; row += gridDim.x * 4ull) {
         named.template load<T>(a, (uint32_t)row);
@@ -353,9 +417,10 @@ __global__ __launch_bounds__(256) void k_distill_join(DistillArgs a)
             bulk = both(bulk, Bulk{p.x, p.y}, distill_factor(a));
         }
         for (int d = 1; d < 64; d *= 2) bulk = both(bulk, Bulk{__shfl_xor(bulk.max, d, 64), __shfl_xor(bulk.total, d, 64)}, distill_factor(a));
-        meet<64>();
-        float loss;
-        const Moves moves = named.template settle<kRest>(a, bulk, a.grad ? a.up[row] : 0.0f, loss);
+        named.template prepare<kRest, 1>(a, nullptr);
+        const float loss = named.template loss<kRest>(a, bulk);
+        Moves moves = {};
+        if (a.grad) moves = named.template moves<kRest>(a, bulk, a.up[row]);
         if (lane == 0) {
             a.loss[row] = loss;
             if (a.grad) a.record[row] = make_float4(moves.max, moves.each, moves.zeros ? 1.0f : 0.0f, 0.0f);
@@ -383,7 +448,7 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_dist
         T *grad = (T *)a.grad + (uint64_t)row * a.grad_stride;
 #pragma unroll
         for (int q = 0; q < kPer; ++q)
-            r.put(x[q], Row::address(grad, r.column(q, begin, end), begin, end), r.twice(q, begin, end), center_of(moves.max), factor, moves);
+            r.put(x[q], Row::address(grad, r.column(q, begin, end), begin, end), r.twice(q, begin, end), center_of(moves.max), factor, moves, 0, 0, nullptr);
     }
 }
 // and the entries' in their places.
@@ -402,7 +467,7 @@ template <class T, bool kRest>
 __global__ __launch_bounds__(256) void k_distill_short(DistillArgs a)
 {
     extern __shared__ uint32_t more_room[];
-    Named<64> named((uint8_t *)more_room + (threadIdx.x >> 6) * 12 * a.top, a.top);
+    Named<64> named((uint8_t *)more_room + (threadIdx.x >> 6) * Named<64>::bytes(a.top), a.top);
     const uint32_t lane = threadIdx.x & 63;
     const float factor = distill_factor(a);
     for (uint64_t row = blockIdx.x * 4ull + (threadIdx.x >> 6); row < a.rows; row += gridDim.x * 4ull) {
@@ -414,8 +479,10 @@ __global__ __launch_bounds__(256) void k_distill_short(DistillArgs a)
         if (kRest && is_named) x = -kInf;
         const float max = wave_reduce(x, MaxFloat());
         const Bulk bulk = {max, wave_reduce(exp2_fast((x - center_of(max)) * factor), Sum())};
-        float loss;
-        const Moves moves = named.template settle<kRest>(a, bulk, a.grad ? a.up[row] : 0.0f, loss);
+        named.template prepare<kRest, 1>(a, nullptr);
+        const float loss = named.template loss<kRest>(a, bulk);
+        Moves moves = {};
+        if (a.grad) moves = named.template moves<kRest>(a, bulk, a.up[row]);
         if (lane == 0) a.loss[row] = loss;
         if (a.grad) {
             T *grad = (T *)a.grad + row * a.grad_stride;
@@ -454,7 +521,7 @@ static void launch_distill_rows(DistillArgs a, hipStream_t stream)
 {
     logits_row<kGrad ? kTrainRows : kLaw>(a.num_sym * (uint32_t)sizeof(T), 0, true, [&](auto lanes, auto per) {
         using Row = DistillRow<T, decltype(lanes)::value, decltype(per)::value>;
-        const size_t lds = Row::kRows * ((kRest ? Row::kMarks : 0) + 12 * a.top);
+        const size_t lds = Row::kRows * ((kRest || kGrad ? Row::kMarks : 0) + Named<Row::kEntryLanes>::bytes(a.top));
         k_distill<T, decltype(lanes)::value, decltype(per)::value, kRest, kGrad><<<logits_blocks(a.rows, Row::kRows), Row::kThreads, lds, stream>>>(a);
     });
 }
@@ -463,7 +530,7 @@ template <class T, bool kRest>
 static void launch_distill(DistillArgs a, void *workspace, hipStream_t stream)
 {
     const uint32_t quarter = std::min(div_up(a.rows, 4), 1u << 20);
-    const size_t entries = 4 * 12 * (size_t)a.top;
+    const size_t entries = 4 * (size_t)Named<64>::bytes(a.top);
     if (a.num_sym < 16 / sizeof(T)) {
         k_distill_short<T, kRest><<<quarter, 256, entries, stream>>>(a);
         return;

@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 
 #        rows  n      top
-SIZES = [(1, 1, 1), (5, 2, 2), (300, 3, 5), (4, 7, 128), (9, 8, 3), (70, 64, 16), (33, 65, 7), (40, 256, 16), (20, 500, 128), (9, 1000, 64), (7, 2048, 1),
+SIZES = [(1, 1, 1), (5, 2, 2), (300, 3, 5), (4, 7, 128), (9, 8, 3), (70, 64, 16), (33, 65, 7), (35, 40, 128), (50, 200, 128), (40, 256, 16), (20, 500, 128), (9, 1000, 64), (7, 2048, 1),
          (5, 5003, 50), (3, 8192, 128), (4, 16385, 32), (2, 32769, 20), (3, 50001, 64), (1, 100003, 128), (2, 131072, 64)]
 
 
