@@ -124,8 +124,8 @@ struct Named {
             sym[i] = in ? s : -1, value[i] = v, x[i] = at;
         }
     }
-    // All that does not hang on the bulk.  `marks`, or null: for each pack of kVec symbols 1 + an entry in it, from which `after`
-    // leads to the others; zeros before.
+    // All that does not hang on the bulk.  `marks`, or null, zeros before: with kVec 1 for each symbol 1 + its entry, where it has
+    // one; else for each pack of kVec symbols 1 + an entry in it, from which `after` leads to the others.
     template <bool kRest, int kVec>
     __device__ void prepare(const DistillArgs &a, uint8_t *marks)
     {
@@ -163,6 +163,20 @@ struct Named {
             }
         mass = 0.0f;
         if (!kRest && !a.grad) return;
+        if (kVec == 1 && marks) {
+            each([&](uint32_t i) { marks[sym[i]] = (uint8_t)(i + 1); });
+            meet<64>();
+            bool twice = false;
+            each([&](uint32_t i) { twice |= marks[sym[i]] != (uint8_t)(i + 1); });
+            if (!lanes_reduce<kLanes>((uint32_t)twice, Or())) {
+                each([&](uint32_t i) {
+                    mass_of[i] = value[i] * norm;
+                    mass += x[i];
+                });
+                mass = lanes_reduce<kLanes>(mass, Sum());
+                return;
+            }
+        }
         meet<64>();
         each([&](uint32_t i) {
             const int32_t s = sym[i];
@@ -179,8 +193,10 @@ struct Named {
                 next = beside && j < i ? j + 1 : next;
             }
             mass_of[i] = q * norm;
-            after[i] = (uint8_t)next;
-            if (marks && head) marks[(uint32_t)s / kVec] = (uint8_t)(i + 1);
+            if (kVec > 1) {
+                after[i] = (uint8_t)next;
+                if (head) marks[(uint32_t)s / kVec] = (uint8_t)(i + 1);
+            }
             if (first) mass += x[i];
         });
         mass = lanes_reduce<kLanes>(mass, Sum());
@@ -236,34 +252,59 @@ struct DistillRow : LogitsRow<T, kLanes, kPer> {
     using Row = LogitsRow<T, kLanes, kPer>;
     using Row::kVec;
     static constexpr int kEntryLanes = kLanes < 64 ? kLanes : 64;
-    static constexpr uint32_t kMarks = kLanes * kPer;  // bytes, one a pack
+    // Where the entries are: short rows have a byte a symbol, long ones a byte a pack
+    static constexpr bool kTable = kLanes <= 64;
+    static constexpr uint32_t kMarks = kLanes * kPer * (kTable ? kVec : 1);
+    // Powers that the sum was made of are kept for the gradient where they are few
+    static constexpr bool kKept = Row::kWaves <= 1 && kPer <= 4;
 
     __device__ void clear(uint8_t *marks) const
     {
+        struct __attribute__((aligned(kTable ? kVec : 1))) None { uint8_t v[kTable ? kVec : 1]; };
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) marks[q * kLanes + this->lane] = 0;
+        for (int q = 0; q < kPer; ++q) ((None *)marks)[q * kLanes + this->lane] = None{};
     }
-    // Named symbols of columns begin .. end-1 are ruled out.
-    __device__ void leave_out(const Named<kEntryLanes> &named, const uint8_t *marks, uint32_t begin, uint32_t end, Raw<T> (&x)[kPer], int used) const
+    // f(place in the pack, entry) for the entries of pack q; those of its first values that another pack has are that one's.
+    template <class F>
+    __device__ void named_in(const Named<kEntryLanes> &named, const uint8_t *marks, int q, uint32_t end, F f) const
+    {
+        const uint32_t pack = q * kLanes + this->lane;
+        if constexpr (kTable) {
+            using Word = std::conditional_t<kVec == 8, uint64_t, uint32_t>;
+            const Word w = ((const Word *)marks)[pack];
+            if (w) {
+                const uint32_t twice = (uint32_t)this->twice(q, 0, end);
+#pragma unroll
+                for (int k = 0; k < kVec; ++k) {
+                    const uint32_t entry = (uint32_t)(w >> (8 * k)) & 255;
+                    if (entry) f(k + twice, entry - 1);
+                }
+            }
+        } else {
+            for (uint32_t entry = marks[pack]; entry; entry = named.after[entry - 1]) f((uint32_t)named.sym[entry - 1] - this->column(q, 0, end), entry - 1);
+        }
+    }
+    __device__ void leave_out(const Named<kEntryLanes> &named, const uint8_t *marks, uint32_t end, Raw<T> (&x)[kPer], int used) const
     {
         Row::for_used(used, [&](int q) {
-            uint32_t entry = marks[q * kLanes + this->lane];
-            if (entry) {
-                const uint32_t column = this->column(q, begin, end);
-                uint32_t bits = 0;
-                for (; entry; entry = named.after[entry - 1]) bits |= 1u << ((uint32_t)named.sym[entry - 1] - column);
-                rule_out_bits(x[q], bits);
-            }
+            uint32_t bits = 0;
+            named_in(named, marks, q, end, [&](uint32_t k, uint32_t) { bits |= 1u << k; });
+            if (bits) rule_out_bits(x[q], bits);
         });
     }
     // The bulk of all lanes' values, in all lanes.  `room` holds 2 * kWaves, its halves are used in turn.
-    __device__ Bulk bulk(const Raw<T> (&x)[kPer], int used, float own, float factor, Bulk *room, int half) const
+    template <bool kKeep>
+    __device__ Bulk bulk(const Raw<T> (&x)[kPer], int used, float own, float factor, Bulk *room, int half, float (&kept)[kKeep ? kPer : 1][kVec]) const
     {
         const float max = lanes_reduce<Row::kWithin>(own, MaxFloat()), center = center_of(max);
         float total[2] = {0.0f, 0.0f};
         Row::for_used(used, [&](int q) {
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) total[k & 1] += exp2_fast((x[q][k] - center) * factor);
+            for (int k = 0; k < kVec; ++k) {
+                const float e = exp2_fast((x[q][k] - center) * factor);
+                total[k & 1] += e;
+                if (kKeep) kept[kKeep ? q : 0][k] = e;
+            }
         });
         Bulk t = {max, lanes_reduce<Row::kWithin>(total[0] + total[1], Sum())};
         if constexpr (Row::kWaves > 1) {
@@ -276,19 +317,13 @@ struct DistillRow : LogitsRow<T, kLanes, kPer> {
         }
         return t;
     }
-    // The gradient of a pack's values; of those that are named, from `entry` on, what the entries have.
-    __device__ void put(const Raw<T> &x, T *to, int twice, float center, float factor, const Moves &m, uint32_t entry, uint32_t column,
-                        const Named<kEntryLanes> *named) const
+    // The gradient of a pack's values, made of their powers; patch(d) puts the entries' in their places
+    template <class F>
+    __device__ void put(float (&d)[kVec], T *to, int twice, const Moves &m, F patch) const
     {
-        float d[kVec];
 #pragma unroll
-        for (int k = 0; k < kVec; ++k) d[k] = m.zeros ? 0.0f : exp2_fast((x[k] - center) * factor) * m.each;
-        for (; entry; entry = named->after[entry - 1]) {
-            const uint32_t at = (uint32_t)named->sym[entry - 1] - column;
-            const float g = named->x[entry - 1];
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) d[k] = at == (uint32_t)k ? g : d[k];
-        }
+        for (int k = 0; k < kVec; ++k) d[k] = m.zeros ? 0.0f : d[k] * m.each;
+        patch(d);
         if (twice == 0) {
             Raw<T>::of(d).store(to);
         } else {
@@ -296,6 +331,11 @@ struct DistillRow : LogitsRow<T, kLanes, kPer> {
             for (int k = 0; k < kVec; ++k)
                 if (k >= twice) to[k] = (T)d[k];
         }
+    }
+    __device__ void powers(const Raw<T> &x, float center, float factor, float (&d)[kVec]) const
+    {
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) d[k] = exp2_fast((x[k] - center) * factor);
     }
 };
 
@@ -326,16 +366,18 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         // registers to itself
         if constexpr (Row::kWaves <= 1) r.load((const T *)a.x + (uint64_t)row * a.stride, 0, a.num_sym, x);
         if constexpr (kMarked) meet<kLanes>();
-        if (mine) named.template prepare<kRest, Row::kVec>(a, marks);
+        if (mine) named.template prepare<kRest, Row::kTable ? 1 : Row::kVec>(a, marks);
         if constexpr (Row::kWaves > 1) r.load((const T *)a.x + (uint64_t)row * a.stride, 0, a.num_sym, x);
         if constexpr (kMarked) meet<kLanes>();
         r.rule_out(0, a.num_sym, x);
         const int used = r.used(0, a.num_sym);
-        if constexpr (kRest) r.leave_out(named, marks, 0, a.num_sym, x, used);
+        if constexpr (kRest) r.leave_out(named, marks, a.num_sym, x, used);
         float of[kPer];
         const float own = r.largest(x, used, of);
         r.forget(x);
-        const Bulk bulk = r.bulk(x, used, own, factor, room, half);
+        constexpr bool kKept = kGrad && Row::kKept;
+        float kept[kKept ? kPer : 1][Row::kVec];
+        const Bulk bulk = r.template bulk<kKept>(x, used, own, factor, room, half, kept);
         r.forget(x);
         half ^= 1;
         if constexpr (kGrad) {
@@ -348,7 +390,20 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
             T *grad = (T *)a.grad + (uint64_t)row * a.grad_stride;
             Row::for_used(used, [&](int q) {
                 const uint32_t column = r.column(q, 0, a.num_sym);
-                r.put(x[q], Row::address(grad, column, 0, a.num_sym), r.twice(q, 0, a.num_sym), center, factor, moves, marks[q * kLanes + r.lane], column, &named);
+                float d[Row::kVec];
+                if constexpr (kKept) {
+#pragma unroll
+                    for (int k = 0; k < Row::kVec; ++k) d[k] = kept[q][k];
+                } else {
+                    r.powers(x[q], center, factor, d);
+                }
+                r.put(d, Row::address(grad, column, 0, a.num_sym), r.twice(q, 0, a.num_sym), moves, [&](float(&d)[Row::kVec]) {
+                    r.named_in(named, marks, q, a.num_sym, [&](uint32_t at, uint32_t entry) {
+                        const float g = named.x[entry];
+#pragma unroll
+                        for (int k = 0; k < Row::kVec; ++k) d[k] = at == (uint32_t)k ? g : d[k];
+                    });
+                });
             });
         }
         if (mine) {
@@ -369,7 +424,7 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
     Row r;
     const uint64_t items = (uint64_t)a.rows * a.splits, step = (uint64_t)gridDim.x * Row::kRows;
     const float factor = distill_factor(a);
-    uint8_t *marks = (uint8_t *)more_room + r.row_in_block * Row::kMarks;
+    uint8_t *marks = (uint8_t *)more_room + r.row_in_block * (kLanes * kPer);
     int half = 0;
     for (uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block; item < items; item += step) {
         const uint32_t row = (uint32_t)(item / a.splits), begin = (uint32_t)(item - (uint64_t)row * a.splits) * a.span;
@@ -379,7 +434,7 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         r.rule_out(begin, end, x);
         const int used = r.used(begin, end);
         if constexpr (kRest) {  // a bit for each named symbol that lies in the run, a byte a pack
-            r.clear(marks);
+            for (uint32_t i = r.lane; i < (uint32_t)(kLanes * kPer / 4); i += kLanes) ((uint32_t *)marks)[i] = 0;
             meet<kLanes>();
             for (uint32_t i = r.lane; i < a.top; i += kLanes) {
                 const uint32_t s = (uint32_t)a.sym[(uint64_t)row * a.top + i];  // a negative one lies behind all
@@ -396,7 +451,8 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         float of[kPer];
         const float own = r.largest(x, used, of);
         r.forget(x);
-        const Bulk bulk = r.bulk(x, used, own, factor, room, half);
+        float none[1][Row::kVec];
+        const Bulk bulk = r.template bulk<false>(x, used, own, factor, room, half, none);
         half ^= 1;
         if (r.lane == 0) a.part[item] = make_float2(bulk.max, bulk.total);
         meet<kLanes>();
@@ -447,8 +503,11 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads)) void k_dist
         r.load((const T *)a.x + (uint64_t)row * a.stride, begin, end, x);
         T *grad = (T *)a.grad + (uint64_t)row * a.grad_stride;
 #pragma unroll
-        for (int q = 0; q < kPer; ++q)
-            r.put(x[q], Row::address(grad, r.column(q, begin, end), begin, end), r.twice(q, begin, end), center_of(moves.max), factor, moves, 0, 0, nullptr);
+        for (int q = 0; q < kPer; ++q) {
+            float d[Row::kVec];
+            r.powers(x[q], center_of(moves.max), factor, d);
+            r.put(d, Row::address(grad, r.column(q, begin, end), begin, end), r.twice(q, begin, end), moves, [](auto &) {});
+        }
     }
 }
 // and the entries' in their places.
@@ -547,7 +606,7 @@ static void launch_distill(DistillArgs a, void *workspace, hipStream_t stream)
     logits_row<kLaw>(a.span * (uint32_t)sizeof(T), 0, false, [&](auto lanes, auto per) {
         using Row = DistillRow<T, decltype(lanes)::value, decltype(per)::value>;
         k_distill_runs<T, decltype(lanes)::value, decltype(per)::value, kRest>
-            <<<logits_blocks((uint64_t)a.rows * a.splits, Row::kRows), Row::kThreads, kRest ? Row::kRows * Row::kMarks : 0, stream>>>(a);
+            <<<logits_blocks((uint64_t)a.rows * a.splits, Row::kRows), Row::kThreads, kRest ? Row::kThreads * decltype(per)::value : 0, stream>>>(a);
     });
     k_distill_join<T, kRest><<<quarter, 256, entries, stream>>>(a);
     if (!a.grad) return;
