@@ -107,26 +107,37 @@ __global__ __launch_bounds__(kTileThreads) void k_block8_tiles(uint32_t rows, ui
     }
 }
 
-// Values back, sixteen a thread.
+// Values back, eight a thread and row, so that lanes' stores of 16-bit values follow one another; two rows at a time.
 template <class T>
 __global__ __launch_bounds__(256) void k_block8_values(uint32_t rows, uint32_t width, Block8 in, T *out, uint64_t stride)
 {
-    const uint32_t packs = div_up(width, 16);
-    const uint64_t items = (uint64_t)rows * packs;
+    constexpr int kRows = 2;
+    const uint32_t packs = div_up(width, 8);
+    const uint64_t items = (uint64_t)div_up(rows, kRows) * packs;
     for (uint64_t item = blockIdx.x * 256ull + threadIdx.x; item < items; item += gridDim.x * 256ull) {
-        const uint32_t row = (uint32_t)(item / packs), column = (uint32_t)(item % packs) * 16;
-        const int valid = (int)min(width - column, 16u);
-        const uint32_t byte = in.scale[(uint64_t)(row >> in.shared_bits) * in.scale_stride + column / kBlock8];
-        const u32x4_t codes = __builtin_bit_cast(u32x4_t, load_pack<16>(in.code + (uint64_t)row * in.stride + column, valid));
-        Pack<T, 16> t;
+        const uint32_t row = (uint32_t)(items >> 32 ? item / packs : (uint32_t)item / packs), column = (uint32_t)(item - (uint64_t)row * packs) * 8;
+        const int valid = (int)min(width - column, 8u);
+        Pack<uint8_t, 8> codes[kRows];
+        uint32_t byte[kRows];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float v[4];
-            values_of(codes[i], in.type, byte, v);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) t.v[4 * i + k] = (T)v[k];
+        for (int i = 0; i < kRows; ++i) {
+            const uint32_t r = min(row * kRows + i, rows - 1);
+            byte[i] = in.scale[(uint64_t)(r >> in.shared_bits) * in.scale_stride + column / kBlock8];
+            codes[i] = load_pack<8>(in.code + (uint64_t)r * in.stride + column, valid);
         }
-        store_pack<16>(out + (uint64_t)row * stride + column, valid, t);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const uint64_t both = __builtin_bit_cast(uint64_t, codes[i]);
+            Pack<T, 8> t;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                float v[4];
+                values_of((uint32_t)(both >> (32 * n)), in.type, byte[i], v);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) t.v[4 * n + k] = (T)v[k];
+            }
+            if (row * kRows + i < rows) store_pack<8>(out + (uint64_t)(row * kRows + i) * stride + column, valid, t);
+        }
     }
 }
 
@@ -160,7 +171,7 @@ int pilc_block8_values(uint32_t rows, uint32_t width, const pilc_block8 *in, voi
     if (!in->code || !in->scale || !values_dev || !aligned_to(values_dev, value_bytes(dtype))) return PILC_E_ARG;
     return by_type(dtype, [&](auto *type) {
         using T = std::remove_pointer_t<decltype(type)>;
-        const uint64_t blocks = ((uint64_t)rows * div_up(width, 16) + 255) / 256;
+        const uint64_t blocks = ((uint64_t)div_up(rows, 2) * div_up(width, 8) + 255) / 256;
         k_block8_values<T><<<(uint32_t)std::min<uint64_t>(blocks, 1u << 20), 256, 0, (hipStream_t)hip_stream>>>(rows, width, block8_of(*in), (T *)values_dev, stride);
     });
 }

@@ -1,6 +1,6 @@
 """Learns the laws of a stream of vector indices and codes the stream under them.
 
-    python -m paper_2206_05279_amd.fit_laws [--images N] [--steps K]
+    python -m paper_2206_05279_amd.fit_laws [--images N] [--steps K] [--student WIDTH]
 
 An image of 32 x 32 pixels is 16 x 16 indices out of 256 (arXiv 2206.05279, Sec. 3.1).  One static law
 for all of them costs what their histogram does.  Here the law of an index hangs on what both sides know
@@ -9,6 +9,11 @@ answers with as logits.  A training step takes a batch of indices through an emb
 linear layer, lets `pilc_logprobs_train` say what the indices cost and how the logits should move, and goes
 back through `pilc_norm_backward` to `pilc_adamw_step`, whose states are held in 8 bits.  At the end the laws
 become the integer masses of the table-driven coder, which codes the stream and gives it back.
+
+With `--student` a smaller network then learns the laws from the first one's sixteen likeliest symbols of each alone, without
+looking at the stream.  Its head works in 8 bits: root-mean-square norm of the sum of both embeddings with its answer in 8 bits,
+the product with weights in 8 bits, `pilc_distill` for what its laws lose against the teacher's and how the logits should move, and the
+products of the way back on matrices that are put into 8 bits both ways round.  The stream is coded under its laws too.
 
 The indices are synthetic, drawn from laws of low rank.
 """
@@ -114,6 +119,84 @@ class LawNetwork:
         return torch.softmax(x.float(), 1).cpu().numpy()
 
 
+class Held:
+    """A matrix in 8 bits with room of its own: rows x width, under scales for blocks of 128 in one row or in 128."""
+
+    def __init__(self, rows: int, width: int, device, block_rows: int = 1, dtype=torch.float8_e4m3fn):
+        codes = torch.empty(rows, width, dtype=dtype, device=device)
+        scales = torch.empty(-(-rows // block_rows), -(-width // 128), dtype=torch.uint8, device=device)
+        self.block = pb.make_block8(codes, scales, block_rows)
+
+
+class StudentNetwork:
+    """Logits of a law in 8 bits: the sum of the embeddings of its cell and class, root-mean-square norm, linear layer.  Learns from
+    a teacher's likeliest symbols, all laws at a step."""
+
+    def __init__(self, width: int = 32, device: str = "cuda:0", seed: int = 1):
+        g = torch.Generator().manual_seed(seed)
+        new = lambda *shape, scale: (torch.randn(*shape, generator=g) * scale).to(device)  # noqa: E731
+        self.width, self.device = width, device
+        self.params = {"cell": new(CELLS, width, scale=0.5), "class": new(CLASSES, width, scale=0.5), "norm_weight": torch.ones(width, device=device),
+                       "head": new(NUM_SYM, width, scale=width ** -0.5)}
+        self.grads = {k: torch.empty_like(v) for k, v in self.params.items()}
+        state = lambda: [torch.zeros_like(v) for v in self.params.values()]  # noqa: E731
+        self.list = pb.make_adamw_tensors(list(self.params.values()), list(self.grads.values()), state(), state())
+        self.steps, self.laws = 0, torch.arange(LAWS, device=device)
+        made = lambda *shape, t=torch.bfloat16: torch.empty(*shape, dtype=t, device=device)  # noqa: E731
+        self.sum, self.y, self.dy = made(LAWS, width), made(LAWS, width), made(LAWS, width)
+        self.rstd, self.logits, self.loss = made(LAWS, t=torch.float32), made(LAWS, NUM_SYM), made(LAWS, t=torch.float32)
+        # states and weights forward; what comes back and the weights by inputs; both turned round for the weights' gradient
+        self.y8, self.head8 = Held(LAWS, width, device), Held(NUM_SYM, width, device, 128)
+        self.back8, self.turned_head8 = Held(LAWS, NUM_SYM, device, dtype=torch.float8_e5m2), Held(width, NUM_SYM, device, 128)
+        self.turned_back8, self.turned_y8 = Held(NUM_SYM, LAWS, device, dtype=torch.float8_e5m2), Held(width, LAWS, device)
+        sizes = [pb.pilc_block8_product_workspace_size(*s) for s in ((LAWS, NUM_SYM, width), (LAWS, width, NUM_SYM), (NUM_SYM, width, LAWS))]
+        self.workspace = made(max(sizes + [pb.pilc_rms_workspace_size(LAWS, width), pb.pilc_distill_workspace_size(LAWS, NUM_SYM, 128)]), t=torch.uint8)
+
+    def forward(self) -> torch.Tensor:
+        """Logits (bfloat16) of all laws."""
+        p = self.params
+        pb.pilc_rms_forward(p["cell"][self.laws % CELLS].bfloat16(), p["norm_weight"], y=self.y, y8=self.y8.block,
+                            add=p["class"][self.laws // CELLS].bfloat16(), sum=self.sum, rstd=self.rstd)
+        pb.pilc_block8_quantize(p["head"], self.head8.block, self.turned_head8.block)
+        pb.pilc_block8_product(self.y8.block, self.head8.block, self.logits, workspace=self.workspace)
+        return self.logits
+
+    def backward(self, dlogits: torch.Tensor) -> None:
+        """The parameters' gradients from the logits'."""
+        g = self.grads
+        pb.pilc_block8_quantize(dlogits, self.back8.block, self.turned_back8.block)
+        pb.pilc_block8_quantize(self.y, None, self.turned_y8.block)
+        pb.pilc_block8_product(self.back8.block, self.turned_head8.block, self.dy, workspace=self.workspace)
+        pb.pilc_block8_product(self.turned_back8.block, self.turned_y8.block, g["head"], workspace=self.workspace)
+        pb.pilc_rms_backward(self.dy, self.sum, self.params["norm_weight"], self.rstd, dx=self.dy, dweight=g["norm_weight"], workspace=self.workspace)
+        dh = self.dy.float()
+        g["cell"].zero_().index_add_(0, self.laws % CELLS, dh)
+        g["class"].zero_().index_add_(0, self.laws // CELLS, dh)
+
+    def step(self, sym: torch.Tensor, logp: torch.Tensor, lr: float) -> torch.Tensor:
+        """One step against a teacher's symbols and ln p of each [laws, named]; returns what each law loses before it."""
+        up = torch.full((LAWS,), 1.0 / LAWS, device=self.device)
+        logits = self.forward()
+        pb.pilc_distill(logits, sym, logp, self.loss, up=up, grad=logits, rest=True, workspace=self.workspace)      # the gradient takes the logits' place
+        self.backward(logits)
+        self.steps += 1
+        pb.pilc_adamw_step(self.list, lr=lr, beta1=0.9, beta2=0.99, eps=1e-8, step=self.steps)
+        return self.loss
+
+
+def distil(table: torch.Tensor, width: int = 32, steps: int = 300, lr: float = 2e-2, named: int = 16, seed: int = 1, say=print) -> StudentNetwork:
+    """A student of the laws that a teacher's logits [192, 256] stand for."""
+    sym, logp = torch.empty(LAWS, named, dtype=torch.int32, device=table.device), torch.empty(LAWS, named, device=table.device)
+    workspace = torch.empty(pb.pilc_logprobs_workspace_size(LAWS, NUM_SYM, named), dtype=torch.uint8, device=table.device)
+    pb.pilc_logprobs(table, None, top_sym=sym, top_logp=logp, workspace=workspace)
+    net = StudentNetwork(width, device=str(table.device), seed=seed)
+    for k in range(steps):
+        loss = net.step(sym, logp, lr * min(1.0, 4.0 * (1 - k / steps)))
+        if say and (k % 50 == 0 or k == steps - 1):
+            say("student, step %3d: loses %.4f bits an index" % (k, float(loss.double().mean()) / math.log(2)))
+    return net
+
+
 def _bits(nats: torch.Tensor) -> float:
     return float(-nats.double().mean()) / math.log(2)
 
@@ -132,8 +215,8 @@ def code(symbols: torch.Tensor, laws: torch.Tensor, masses: np.ndarray):
     return nbytes, torch.equal(back, symbols)
 
 
-def fit(images: int = 20000, steps: int = 300, batch: int = 16384, lr: float = 5e-3, seed: int = 0, say=print) -> dict:
-    """Learns, codes and compares; returns the figures, bits an index."""
+def fit(images: int = 20000, steps: int = 300, batch: int = 16384, lr: float = 5e-3, seed: int = 0, say=print, student: int = 0) -> dict:
+    """Learns, codes and compares; returns the figures, bits an index.  student: the width of a student, 0 for none."""
     symbols, laws = make_stream(images, seed)
     flat_s, flat_l = symbols.reshape(-1), laws.reshape(-1).long()
     net = LawNetwork(seed=seed)
@@ -161,6 +244,12 @@ def fit(images: int = 20000, steps: int = 300, batch: int = 16384, lr: float = 5
         say("learned laws: %.4f bits an index (they expect %.4f), coded %.4f; one static law, coded %.4f; lossless: %s" % (
             learned, expected, out["coded"], out["static"], out["lossless"]))
         say("law 0 answers with %s at %s bits" % (best[0].tolist(), ["%.2f" % b for b in (-best_logp[0] / math.log(2)).tolist()]))
+    if student:
+        small = distil(table, student, steps, say=say)
+        student_bytes, student_back = code(symbols, laws, masses_of(torch.softmax(small.forward().float(), 1).cpu().numpy()))
+        out.update(student=8.0 * student_bytes / symbols.numel(), lossless=out["lossless"] and student_back)
+        if say:
+            say("student's laws, coded %.4f" % out["student"])
     return out
 
 
@@ -169,5 +258,6 @@ if __name__ == "__main__":
     ap.add_argument("--images", type=int, default=20000)
     ap.add_argument("--steps", type=int, default=300)
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--student", type=int, default=0, metavar="WIDTH", help="distil the laws into a student of this width (0: none)")
     a = ap.parse_args()
-    fit(a.images, a.steps, seed=a.seed)
+    fit(a.images, a.steps, seed=a.seed, student=a.student)
