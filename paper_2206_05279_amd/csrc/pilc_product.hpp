@@ -262,23 +262,24 @@ __global__ __launch_bounds__(256, kTile == 256 ? 1 : 2) void k_product_groups(Pr
                     from_b[i] = code_row(p.b, min(col0 + row, p.cols - 1)) + (lane & 7) * 16;
                 }
                 Raw<uint8_t> held_a[kLoads], held_b[kLoads];
-                const auto fetch = [&](uint32_t block) {
-#pragma unroll
-                    for (int i = 0; i < kLoads; ++i) {
-                        held_a[i] = Raw<uint8_t>::load(from_a[i] + (uint64_t)block * kBlock8);
-                        held_b[i] = Raw<uint8_t>::load(from_b[i] + (uint64_t)block * kBlock8);
-                    }
+                const auto fetch = [&](uint32_t block, int n) {  // chunk n / 2 of a or b
+                    if (n % 2 == 0)
+                        held_a[n / 2] = Raw<uint8_t>::load(from_a[n / 2] + (uint64_t)block * kBlock8);
+                    else
+                        held_b[n / 2] = Raw<uint8_t>::load(from_b[n / 2] + (uint64_t)block * kBlock8);
                 };
-                const auto put = [&](uint32_t buffer) {
+                const auto put = [&](uint32_t buffer, int n) { *(u32x4_t *)(codes + buffer + (n % 2 ? kSide : 0) + to[n / 2]) = n % 2 ? held_b[n / 2].bits : held_a[n / 2].bits; };
+                const uint32_t end = whole - 1;
 #pragma unroll
-                    for (int i = 0; i < kLoads; ++i) {
-                        *(u32x4_t *)(codes + buffer + to[i]) = held_a[i].bits;
-                        *(u32x4_t *)(codes + buffer + kSide + to[i]) = held_b[i].bits;
-                    }
-                };
-                fetch(first);
-                put(0);
+                for (int n = 0; n < 2 * kLoads; ++n) fetch(first, n);
+#pragma unroll
+                for (int n = 0; n < 2 * kLoads; ++n) put(0, n);
+#pragma unroll
+                for (int n = 0; n < 2 * kLoads; ++n) fetch(min(first + 1, end), n);
                 __syncthreads();
+#pragma unroll
+                for (int j = 0; j < kT; ++j) b[j] = frag(kSide, wave_col + j * 16);
+                a[0] = frag(0, wave_row);
                 uint32_t here = 0;
 #pragma unroll 1
                 for (uint32_t block = first; block < whole; ++block) {
@@ -289,25 +290,40 @@ __global__ __launch_bounds__(256, kTile == 256 ? 1 : 2) void k_product_groups(Pr
                             sb[i] = four_scales(scale_row(p.b, min(col0 + wave_col + i * 16 + r, p.cols - 1)), block / 4, p.blocks);
                         }
                     }
-                    fetch(min(block + 1, whole - 1));
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int j = 0; j < kT; ++j) b[j] = frag(here + kSide, wave_col + j * 16);
-                    a[0] = frag(here, wave_row);
+                    const uint32_t after = min(block + 2, end);
 #pragma unroll
                     for (int i = 0; i < kT; ++i) {
-                        if (i + 1 < kT) a[(i + 1) & 1] = frag(here, wave_row + (i + 1) * 16);
+                        // what was fetched a step ago goes into the next step's place, beside the first rows' products
+                        constexpr int kMost = 2 * kLoads, kOver = kT - 1;
+                        if (i + 1 < kT) {
+                            a[(i + 1) & 1] = frag(here, wave_row + (i + 1) * 16);
+                        } else {
+                            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                            __builtin_amdgcn_s_barrier();
+                            a[(i + 1) & 1] = frag(here ^ kBuffer, wave_row);
+                        }
                         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int j = 0; j < kT; ++j) sum[i][j] = multiply(b[j], a[i & 1], sum[i][j], sb[j], sa[i]);
+                        for (int j = 0; j < kT; ++j) {
+                            sum[i][j] = multiply(b[j], a[i & 1], sum[i][j], sb[j], sa[i]);
+                            if (i + 1 == kT) {
+                                b[j] = frag((here ^ kBuffer) + kSide, wave_col + j * 16);
+                                __builtin_amdgcn_sched_barrier(0);
+                            } else {
+                                const int n = (i * kMost + kOver - 1) / kOver + j, until = min(kMost, ((i + 1) * kMost + kOver - 1) / kOver);
+                                if (n < until) {
+                                    put(here ^ kBuffer, n);
+                                    fetch(after, n);
+                                    __builtin_amdgcn_sched_barrier(0);
+                                }
+                            }
+                        }
                         sa[i] >>= 8;
                         __builtin_amdgcn_sched_barrier(0);
                     }
 #pragma unroll
                     for (int j = 0; j < kT; ++j) sb[j] >>= 8;
                     here ^= kBuffer;
-                    put(here);
-                    __syncthreads();
                 }
             }
         }
@@ -359,7 +375,7 @@ __global__ __launch_bounds__(256, kTile == 256 ? 1 : 2) void k_product_singles(P
         const uint32_t row0 = item.row * kTile, col0 = item.col * kTile;
         const uint32_t begin = item.split * p.blocks_each * 2, end = min(div_up(p.depth, kStep), begin + p.blocks_each * 2);  // steps
         f32x4_t sum[kT][kT] = {};
-        bf16x8_t b[2][kT], a[2];
+        bf16x8_t b[2][kT], a[4];
         // four threads a row
         const uint32_t own_row = threadIdx.x / 4, own_chunk = threadIdx.x % 4;
         const uint8_t *from[2][kLoads], *from_scale[2][kLoads];
@@ -377,46 +393,67 @@ __global__ __launch_bounds__(256, kTile == 256 ? 1 : 2) void k_product_singles(P
             held[side][i] = Raw<uint8_t>::load(from[side][i] + (uint64_t)step * kStep).bits;
             held_scale[side][i] = from_scale[side][i][step / 2];
         };
-        const auto put = [&](uint32_t buffer, int side, int i) {
+        const auto put = [&](uint32_t buffer, int side, int i, int half) {
             const uint32_t row = i * 64 + own_row, swap = row >> 1 & 7;
             const float scale = scale_value(held_scale[side][i]);
-            uint8_t *to = values + buffer + side * kSide + row * 128;
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-                *(bf16x8_t *)(to + (((2 * own_chunk + half) ^ swap) * 16)) = side == 0 ? widen8<kTypeA>(held[side][i], half, scale) : widen8<kTypeB>(held[side][i], half, scale);
+            *(bf16x8_t *)(values + buffer + side * kSide + row * 128 + (((2 * own_chunk + half) ^ swap) * 16)) =
+                side == 0 ? widen8<kTypeA>(held[side][i], half, scale) : widen8<kTypeB>(held[side][i], half, scale);
         };
         uint32_t here = 0;
         if (begin < whole) {
+            constexpr int kRows = 2 * kT, kHalves = 4 * kLoads;  // rows of products; half chunks
 #pragma unroll
-            for (int i = 0; i < 2 * kLoads; ++i) fetch(begin, i & 1, i / 2);
+            for (int n = 0; n < 2 * kLoads; ++n) fetch(begin, n & 1, n / 2);
 #pragma unroll
-            for (int i = 0; i < 2 * kLoads; ++i) put(0, i & 1, i / 2);
+            for (int n = 0; n < kHalves; ++n) put(0, n / 2 & 1, n / 4, n & 1);
 #pragma unroll
-            for (int i = 0; i < 2 * kLoads; ++i) fetch(min(begin + 1, whole - 1), i & 1, i / 2);
+            for (int n = 0; n < 2 * kLoads; ++n) fetch(min(begin + 1, whole - 1), n & 1, n / 2);
             __syncthreads();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int j = 0; j < kT; ++j) b[h][j] = frag(kSide, wave_col + j * 16, h);
+                a[h] = frag(0, wave_row, h);
+            }
 #pragma unroll 1
             for (uint32_t step = begin; step < whole; ++step) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < kT; ++j) b[h][j] = frag(here + kSide, wave_col + j * 16, h);
-                a[0] = frag(here, wave_row, 0);
                 const uint32_t after = min(step + 2, whole - 1);
 #pragma unroll
-                for (int i = 0; i < 2 * kT; ++i) {  // half i % 2 of tile row i / 2
-                    if (i + 1 < 2 * kT) a[(i + 1) & 1] = frag(here, wave_row + (i + 1) / 2 * 16, (i + 1) % 2);
+                for (int i = 0; i < kRows; ++i) {  // half i % 2 of tile row i / 2
+                    if (i + 2 < kRows) {
+                        a[(i + 2) & 3] = frag(here, wave_row + (i + 2) / 2 * 16, i % 2);
+                    } else {
+                        if (i + 2 == kRows) {  // all are done with this step's place, and the next step's values are there
+                            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                            __builtin_amdgcn_s_barrier();
+                        }
+                        a[(i + 2) & 3] = frag(here ^ kBuffer, wave_row, i % 2);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int j = 0; j < kT; ++j) sum[i / 2][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[i % 2][j], a[i & 1], sum[i / 2][j], 0, 0, 0);
-                    if (i % 2 == 1) {  // as many as there are chunks
-                        const int n = i / 2;
-                        put(here ^ kBuffer, n & 1, n / 2);
-                        fetch(after, n & 1, n / 2);
+                    for (int j = 0; j < kT; ++j) {
+                        sum[i / 2][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[i % 2][j], a[i & 3], sum[i / 2][j], 0, 0, 0);
+                        if (i + 2 >= kRows) {
+                            b[i % 2][j] = frag((here ^ kBuffer) + kSide, wave_col + j * 16, i % 2);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                    if (i + 2 < kRows) {
+#pragma unroll
+                        for (int n = (i * kHalves + kRows - 3) / (kRows - 2); n < min(kHalves, ((i + 1) * kHalves + kRows - 3) / (kRows - 2)); ++n) {
+                            put(here ^ kBuffer, n / 2 & 1, n / 4, n & 1);
+                            if (n & 1) fetch(after, n / 2 & 1, n / 4);
+                        }
+                        // widening goes between the products
+#pragma unroll
+                        for (int j = 0; j < kT; ++j) {
+                            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                            __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+                        }
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 here ^= kBuffer;
-                __syncthreads();
             }
         }
         if (whole < end) {
@@ -427,7 +464,8 @@ __global__ __launch_bounds__(256, kTile == 256 ? 1 : 2) void k_product_singles(P
                 const uint32_t row = side ? min(col0 + n * 64 + own_row, p.cols - 1) : min(row0 + n * 64 + own_row, p.rows - 1);
                 held[side][n] = product_chunk(code_row(side ? p.b : p.a, row), whole * kStep + own_chunk * 16, p.depth);
                 held_scale[side][n] = from_scale[side][n][whole / 2];
-                put(0, side, n);
+                put(0, side, n, 0);
+                put(0, side, n, 1);
             }
             __syncthreads();
 #pragma unroll
