@@ -600,33 +600,42 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs p)
     }
 }
 
-// How a product is gone about: rows up to 64 by k_product_few, others by tiles of 256 or 128; the depth in splits where the tiles do
-// not fill the GPU.
-constexpr uint32_t kFewRows = 64;
+// How a product is gone about.  Up to 48 rows by k_product_few (8192 x 8192 bf16, us: 33 rows 25 and by tiles 24, 64 rows 35 and 24),
+// in splits of the depth where the columns do not fill the GPU.  Others by the tiles and splits that the least time is expected of,
+// from what these measured on 256 compute units (bf16, codes from memory to LDS; with codes through registers and in 32 bits all of
+// them take about twice as long): a step of 128 of the depth 1.6 us with tiles of 256, of which a compute unit has one, with tiles of
+// 128 0.6 us where it has one of them and 0.95 where it has two, and the join 3 us and what the parts take to write and read at 4 TB/s.  us by
+// this rule, and by the other size of tile without splits: 8192 x 8192 x 8192 400 464, 4096 x 4096 x 4096 62 64, 1024 x 4096 x 4096 25 57,
+// 2048 x 2048 x 2048 14 38, 512 x 8192 x 8192 43 93; and without splits 128 x 8192 x 8192 24 40, 512 x 2048 x 16384 30 69.
+constexpr uint32_t kFewRows = 48, kMostSplits = 64;
 struct ProductPlan {
     uint32_t tile, width, splits, blocks_each;  // tile 0: few rows, `width` columns a workgroup
 };
 static ProductPlan product_plan(uint32_t rows, uint32_t cols, uint32_t depth)
 {
     const uint32_t blocks = div_up(depth, kBlock8), units = compute_units();
-    const auto in_splits = [&](uint32_t tile, uint32_t width, uint64_t groups, uint32_t least) {
-        const uint32_t wanted = (uint32_t)std::max<uint64_t>(1, units / std::max<uint64_t>(groups, 1)), splits = std::max(1u, std::min(wanted, blocks / least));
-        const uint32_t each = std::max(4u, div_up(div_up(blocks, splits), 4) * 4);
+    const auto in_splits = [&](uint32_t tile, uint32_t width, uint32_t splits) {
+        const uint32_t each = std::max(4u, div_up(div_up(blocks, splits), 4) * 4);  // scales are read by fours
         return ProductPlan{tile, width, std::max(1u, div_up(blocks, each)), each};
     };
     if (rows <= kFewRows) {
         const uint32_t width = div_up(cols, 32) >= units ? 32 : 16;
-        return in_splits(0, width, div_up(cols, width), 32);
+        return in_splits(0, width, std::max(1u, std::min(units / std::max(1u, div_up(cols, width)), blocks / 32)));
     }
-    // what share of the GPU works on what is wanted
-    const auto worth = [&](const ProductPlan &p) {
-        const double groups = (double)div_up(rows, p.tile) * div_up(cols, p.tile) * p.splits, room = p.tile == 256 ? units : 2.0 * units;
-        const double full = groups / (room * std::ceil(groups / room));
-        return full * rows / ((double)div_up(rows, p.tile) * p.tile) * cols / ((double)div_up(cols, p.tile) * p.tile);
+    const auto expected = [&](const ProductPlan &p) {
+        const double groups = (double)div_up(rows, p.tile) * div_up(cols, p.tile) * p.splits, steps = std::min(p.blocks_each, blocks);
+        const double join = p.splits > 1 ? 3.0 + p.splits * 8e-6 / 4 * rows * cols : 0.0;
+        if (p.tile == 256) return std::ceil(groups / units) * steps * 2.0 + join;
+        const double full = std::floor(groups / (2.0 * units)), left = groups - full * 2.0 * units;
+        return (full * 1.2 + (left == 0 ? 0.0 : left <= units ? 0.72 : 1.2)) * steps + join;
     };
-    const ProductPlan large = in_splits(256, 256, (uint64_t)div_up(rows, 256) * div_up(cols, 256), 8);
-    const ProductPlan small = in_splits(128, 128, ((uint64_t)div_up(rows, 128) * div_up(cols, 128) + 1) / 2, 8);
-    return worth(large) >= 0.6 * worth(small) ? large : small;
+    ProductPlan best = in_splits(128, 128, 1);
+    for (uint32_t tile : {128u, 256u})
+        for (uint32_t splits = 1; splits <= std::min(kMostSplits, std::max(1u, blocks / 4)); ++splits) {
+            const ProductPlan p = in_splits(tile, tile, splits);
+            if (expected(p) < expected(best)) best = p;
+        }
+    return best;
 }
 // Whether codes and scales of a matrix can go to LDS without registers.
 static bool product_direct(const pilc_block8 &m, uint32_t blocks)
