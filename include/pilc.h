@@ -515,7 +515,7 @@ int pilc_block8_product_workspace_size(uint32_t rows, uint32_t cols, uint32_t de
  * c_stride.  So a layer is states times weights [outputs, inputs]; its way back takes the weights
  * transposed, and the weights' gradient both sides transposed (pilc_block8_quantize's out_t).
  * Products are exact and sums go by 32 bits, in an order that the shape and the GPU's number of compute
- * units fix, with one exception: where c is of 16 bits and rows are more than 48, products are added up in groups
+ * units fix, with one exception: where c is of 16 bits and rows are more than 32, products are added up in groups
  * of eight with 13 bits below the largest one's power of two (up to 2^-13 of the sum of the products'
  * sizes; a c of 16 bits is rounded by 2^-9 or 2^-12 of itself).  Products under 2^-126 may be lost.
  * depth 0: c is 0.  Each of rows, cols, depth: up to 2^31 - 1.

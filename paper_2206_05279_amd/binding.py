@@ -830,7 +830,10 @@ def pilc_rms_forward(x, weight, y=None, y8: Optional[Block8] = None, add=None, s
     dev = _device_of(x, "x")
     own, kind = _norm_types(x, weight)
     rows, width = _matrix(x, "x")
-    (xp, xs), (ap, a_s), (sp, ss), (yp, ys) = (_strided(t, own, rows, width, dev, n) for t, n in ((x, "x"), (add, "add"), (sum, "sum"), (y, "y")))
+    xp, xs = _rows(x, own, rows, width, dev, "x")
+    ap, a_s = _strided(add, own, rows, width, dev, "add")
+    sp, ss = _strided(sum, own, rows, width, dev, "sum")
+    yp, ys = _strided(y, own, rows, width, dev, "y")
     shape = pilc_rms_shape(rows, width, xs, a_s, ss, ys, _VALUES[own], _VALUES[kind], eps)
     rc = lib().pilc_rms_forward(C.byref(shape), xp, ap, _vector(weight, kind, width, dev, "weight"), sp, yp, _block8(y8, rows, width, dev, "y8"),
                                 _vector(rstd, torch.float32, rows, dev, "rstd"), _raw_stream(stream, dev))
@@ -857,7 +860,10 @@ def pilc_rms_backward(dy, h, weight, rstd, dx=None, dweight=None, dsum=None, *, 
     dev = _device_of(h, "h")
     own, kind = _norm_types(h, weight, dweight)
     rows, width = _matrix(h, "h")
-    (hp, hs), (gp, gs), (sp, ss), (xp, xs) = (_strided(t, own, rows, width, dev, n) for t, n in ((h, "h"), (dy, "dy"), (dsum, "dsum"), (dx, "dx")))
+    hp, hs = _rows(h, own, rows, width, dev, "h")
+    gp, gs = _rows(dy, own, rows, width, dev, "dy")
+    sp, ss = _strided(dsum, own, rows, width, dev, "dsum")
+    xp, xs = _strided(dx, own, rows, width, dev, "dx")
     shape = pilc_rms_shape(rows, width, hs, ss, xs, gs, _VALUES[own], _VALUES[kind], 0.0)
     rc = lib().pilc_rms_backward(C.byref(shape), gp, hp, _vector(weight, kind, width, dev, "weight"), _vector(rstd, torch.float32, rows, dev, "rstd"),
                                  sp, xp, _vector(dweight, kind, width, dev, "dweight"), *_workspace(workspace, dev), _raw_stream(stream, dev))

@@ -539,7 +539,8 @@ __global__ __launch_bounds__(512) void k_product_few(ProductArgs p)
                 h.a[i][0] = Raw<uint8_t>::load(a[i] + at).bits, h.a[i][1] = Raw<uint8_t>::load(a[i] + at + 64).bits;
             }
         };
-        // the next block is on its way while one is worked on
+        // The next block is on its way while one is worked on.  (Workgroups that begin at different blocks, so that rows a power of
+        // two apart do not all ask the same of memory's channels: 1 x 8192 x 8192 18.7 -> 17.6 us, but 1 x 131072 x 4096 92 -> 112.)
         Held h[2];
         uint32_t block = first + wave;
         if (block < whole) fetch(h[0], block);
@@ -600,25 +601,26 @@ __global__ __launch_bounds__(256) void k_product_join(ProductArgs p)
     }
 }
 
-// How a product is gone about.  Up to 48 rows by k_product_few (8192 x 8192 bf16, us: 33 rows 25 and by tiles 24, 64 rows 35 and 24),
-// in splits of the depth where the columns do not fill the GPU.  Others by the tiles and splits that the least time is expected of,
+// How a product is gone about.  Up to 32 rows by k_product_few, in splits of the depth where the columns do not fill the GPU, if b's
+// rows begin at multiples of four bytes (8192 x 8192 bf16, us, rows four bytes apart from a power of two and one byte: 1 row
+// 13 and 35, 16 rows 17 and 51, 48 rows 29 and 85; by tiles 49 rows 19 and 24, in 32 bits 30 and 29).  Others by the tiles and splits that the least time is expected of,
 // from what these measured on 256 compute units (bf16, codes from memory to LDS; with codes through registers and in 32 bits all of
 // them take about twice as long): a step of 128 of the depth 1.6 us with tiles of 256, of which a compute unit has one, with tiles of
 // 128 0.6 us where it has one of them and 0.95 where it has two, and the join 3 us and what the parts take to write and read at 4 TB/s.  us by
 // this rule, and by the other size of tile without splits: 8192 x 8192 x 8192 400 464, 4096 x 4096 x 4096 62 64, 1024 x 4096 x 4096 25 57,
 // 2048 x 2048 x 2048 14 38, 512 x 8192 x 8192 43 93; and without splits 128 x 8192 x 8192 24 40, 512 x 2048 x 16384 30 69.
-constexpr uint32_t kFewRows = 48, kMostSplits = 64;
+constexpr uint32_t kFewRows = 32, kMostSplits = 64;
 struct ProductPlan {
     uint32_t tile, width, splits, blocks_each;  // tile 0: few rows, `width` columns a workgroup
 };
-static ProductPlan product_plan(uint32_t rows, uint32_t cols, uint32_t depth)
+static ProductPlan product_plan(uint32_t rows, uint32_t cols, uint32_t depth, bool few)
 {
     const uint32_t blocks = div_up(depth, kBlock8), units = compute_units();
     const auto in_splits = [&](uint32_t tile, uint32_t width, uint32_t splits) {
         const uint32_t each = std::max(4u, div_up(div_up(blocks, splits), 4) * 4);  // scales are read by fours
         return ProductPlan{tile, width, std::max(1u, div_up(blocks, each)), each};
     };
-    if (rows <= kFewRows) {
+    if (few) {
         const uint32_t width = div_up(cols, 32) >= units ? 32 : 16;
         return in_splits(0, width, std::max(1u, std::min(units / std::max(1u, div_up(cols, width)), blocks / 32)));
     }
@@ -664,8 +666,13 @@ using namespace pilc;
 int pilc_block8_product_workspace_size(uint32_t rows, uint32_t cols, uint32_t depth, size_t *workspace_bytes_host)
 {
     if (rows > kMostRows || cols > kMostRows || depth > kMostRows || !workspace_bytes_host) return PILC_E_ARG;
-    const ProductPlan plan = product_plan(rows, cols, depth);
-    *workspace_bytes_host = std::max<size_t>(256, plan.splits > 1 ? sizeof(float) * plan.splits * (size_t)rows * cols : 0);
+    size_t most = 256;
+    for (bool few : {false, true})  // wherever the codes will lie
+        if (!few || rows <= kFewRows) {
+            const ProductPlan plan = product_plan(rows, cols, depth, few);
+            if (plan.splits > 1) most = std::max(most, sizeof(float) * plan.splits * (size_t)rows * cols);
+        }
+    *workspace_bytes_host = most;
     return PILC_OK;
 }
 
@@ -681,7 +688,7 @@ int pilc_block8_product(uint32_t rows, uint32_t cols, uint32_t depth, const pilc
         !aligned_to(workspace_dev, 256))
         return PILC_E_ARG;
     if (workspace_bytes < needed) return PILC_E_WORKSPACE;
-    const ProductPlan plan = product_plan(rows, cols, depth);
+    const ProductPlan plan = product_plan(rows, cols, depth, rows <= kFewRows && aligned_to(b->code, 4) && b->stride % 4 == 0);
     ProductArgs p = {};
     p.a = block8_of(*a), p.b = block8_of(*b), p.c = c_dev, p.part = (float *)workspace_dev, p.c_stride = c_stride;
     p.rows = rows, p.cols = cols, p.depth = depth, p.c_type = c_type, p.blocks = div_up(depth, kBlock8);
@@ -699,11 +706,9 @@ int pilc_block8_product(uint32_t rows, uint32_t cols, uint32_t depth, const pilc
             };
             switch (div_up(rows, 16)) {
             case 1: few(std::integral_constant<int, 1>()); break;
-            case 2: few(std::integral_constant<int, 2>()); break;
-            case 3: few(std::integral_constant<int, 3>()); break;
-            default: few(std::integral_constant<int, 4>()); break;
+            default: few(std::integral_constant<int, 2>()); break;
             }
-        } else if (c_type == PILC_F32) {
+        } else if (c_type == PILC_F32 || rows <= kFewRows) {
             plan.tile == 256 ? k_product_singles<kA, kB, 256><<<grid, 256, 0, stream>>>(p) : k_product_singles<kA, kB, 128><<<grid, 256, 0, stream>>>(p);
         } else if (direct) {
             plan.tile == 256 ? k_product_groups<kA, kB, 256, true><<<grid, 256, 0, stream>>>(p) : k_product_groups<kA, kB, 128, true><<<grid, 256, 0, stream>>>(p);
