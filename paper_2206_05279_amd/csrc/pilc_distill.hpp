@@ -86,22 +86,27 @@ __device__ __forceinline__ void rule_out_bits(Raw<T> &x, uint32_t bits)
     }
 }
 
+// What is known of a row's entries together.
+struct Known {
+    uint32_t flags;
+    float max, mass;   // of the named symbols: the largest logit, the sum of their powers, each once
+    double all, gain;  // sum of q, and of q (ln q - (x - max) / temperature)
+};
+
 // The entries of a row, in LDS, gone through by kLanes lanes of a wavefront.  What hangs on the teacher and on the named symbols' logits
 // alone is worked out while the row is on its way; once the bulk is known a few steps are left.
 template <int kLanes>
-struct Named {
+struct Named : Known {
     static constexpr uint32_t kAny = 1, kSpoilt = 2, kNever = 4;
     int32_t *sym;
     float *value, *x, *mass_of;  // the entry's q; its symbol's power, then its gradient; q of all entries of its symbol
     uint8_t *after;              // 1 + another entry in the same pack of the row, 0: none
-    uint32_t lane, top, flags;
-    float max, mass;   // of the named symbols: the largest logit, the sum of their powers, each once
-    double all, gain;  // sum of q, and of q (ln q - (x - max) / temperature)
+    uint32_t lane, top;
 
     __host__ __device__ static constexpr uint32_t bytes(uint32_t top) { return 16 * top + (top + 3) / 4 * 4; }
-    __device__ Named(void *room, uint32_t t)
-        : sym((int32_t *)room), value((float *)room + t), x((float *)room + 2 * t), mass_of((float *)room + 3 * t), after((uint8_t *)room + 16 * t),
-          lane(threadIdx.x % kLanes), top(t), flags(0)
+    __device__ Named(void *room, uint32_t t, const Known &known = {})
+        : Known(known), sym((int32_t *)room), value((float *)room + t), x((float *)room + 2 * t), mass_of((float *)room + 3 * t), after((uint8_t *)room + 16 * t),
+          lane(threadIdx.x % kLanes), top(t)
     {
     }
     template <class F>
@@ -353,7 +358,9 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
     const float factor = distill_factor(a);
     uint8_t *marks = kMarked ? (uint8_t *)more_room + r.row_in_block * Row::kMarks : nullptr;
     using Entries = Named<Row::kEntryLanes>;
-    Entries named((uint8_t *)more_room + (kMarked ? Row::kRows * Row::kMarks : 0) + r.row_in_block * Entries::bytes(a.top), a.top);
+    uint8_t *entries = (uint8_t *)more_room + (kMarked ? Row::kRows * Row::kMarks : 0) + r.row_in_block * Entries::bytes(a.top);
+    __shared__ Known shared_known;  // where a row has several wavefronts, which would keep it in registers for the first one
+    constexpr bool kApart = Row::kWaves > 1;
     const bool mine = Row::kWaves <= 1 || threadIdx.x < 64;  // of a row's wavefronts the first sees to the entries
     int half = 0;
     for (uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block; item < a.rows; item += step) {
@@ -361,12 +368,14 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         const float up = kGrad ? a.up[row] : 0.0f;
         if constexpr (kMarked) r.clear(marks);
         Raw<T> x[kPer];
+        Entries named(entries, a.top);
         if (mine) named.template load<T>(a, row);
         // a row's only wavefront asks for it first; where there are more, the others' loads go on meanwhile, and the first has the
         // registers to itself
         if constexpr (Row::kWaves <= 1) r.load((const T *)a.x + (uint64_t)row * a.stride, 0, a.num_sym, x);
         if constexpr (kMarked) meet<kLanes>();
         if (mine) named.template prepare<kRest, Row::kTable ? 1 : Row::kVec>(a, marks);
+        if (kApart && threadIdx.x == 0) shared_known = named;
         if constexpr (Row::kWaves > 1) r.load((const T *)a.x + (uint64_t)row * a.stride, 0, a.num_sym, x);
         if constexpr (kMarked) meet<kLanes>();
         r.rule_out(0, a.num_sym, x);
@@ -382,8 +391,8 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         half ^= 1;
         if constexpr (kGrad) {
             Moves moves = {};
-            if (mine) moves = named.template moves<kRest>(a, bulk, up);
-            if (Row::kWaves > 1 && threadIdx.x == 0) shared_moves = moves;
+            if (mine) moves = Entries(entries, a.top, kApart ? shared_known : (const Known &)named).template moves<kRest>(a, bulk, up);
+            if (kApart && threadIdx.x == 0) shared_moves = moves;
             meet<kLanes>();
             if constexpr (Row::kWaves > 1) moves = shared_moves;
             const float center = center_of(moves.max);
@@ -407,7 +416,7 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
             });
         }
         if (mine) {
-            const float loss = named.template loss<kRest>(a, bulk);
+            const float loss = Entries(entries, a.top, kApart ? shared_known : (const Known &)named).template loss<kRest>(a, bulk);
             if (r.lane == 0) a.loss[row] = loss;
         }
         meet<kLanes>();
