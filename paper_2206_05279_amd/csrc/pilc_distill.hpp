@@ -130,9 +130,9 @@ struct Named : Known {
         }
     }
     // All that does not hang on the bulk.  `marks`, or null, zeros before: with kVec 1 for each symbol 1 + its entry, where it has
-    // one; else for each pack of kVec symbols 1 + an entry in it, from which `after` leads to the others.
-    template <bool kRest, int kVec>
-    __device__ void prepare(const DistillArgs &a, uint8_t *marks)
+    // one; else for each pack of kVec symbols, at place(its number), 1 + an entry in it, from which `after` leads to the others.
+    template <bool kRest, int kVec, class Place>
+    __device__ void prepare(const DistillArgs &a, uint8_t *marks, Place place)
     {
         const float factor = distill_factor(a);
         float most = -kInf;
@@ -168,42 +168,59 @@ struct Named : Known {
             }
         mass = 0.0f;
         if (!kRest && !a.grad) return;
-        if (kVec == 1 && marks) {
-            each([&](uint32_t i) { marks[sym[i]] = (uint8_t)(i + 1); });
-            meet<64>();
-            bool twice = false;
-            each([&](uint32_t i) { twice |= marks[sym[i]] != (uint8_t)(i + 1); });
-            if (!lanes_reduce<kLanes>((uint32_t)twice, Or())) {
-                each([&](uint32_t i) {
-                    mass_of[i] = value[i] * norm;
-                    mass += x[i];
-                });
-                mass = lanes_reduce<kLanes>(mass, Sum());
-                return;
-            }
-        }
-        meet<64>();
-        each([&](uint32_t i) {
-            const int32_t s = sym[i];
+        // q of all entries of an entry's symbol, in their order, and whether it is the first of them
+        const auto together = [&](uint32_t i, bool &first) {
             float q = 0.0f;
-            uint32_t next = 0;
-            bool first = true, head = true;
 #pragma unroll 4
             for (uint32_t j = 0; j < top; ++j) {
-                const int32_t t = sym[j];
-                const bool same = t == s, beside = t >= 0 && (uint32_t)t / kVec == (uint32_t)s / kVec;
+                const bool same = sym[j] == sym[i];
                 q += same ? value[j] : 0.0f;
                 first &= !same || j >= i;
-                head &= !beside || j <= i;
-                next = beside && j < i ? j + 1 : next;
             }
-            mass_of[i] = q * norm;
-            if (kVec > 1) {
-                after[i] = (uint8_t)next;
-                if (head) marks[(uint32_t)s / kVec] = (uint8_t)(i + 1);
+            return q;
+        };
+        if constexpr (kVec == 1) {
+            bool alone = marks != nullptr;
+            if (marks) {
+                each([&](uint32_t i) { marks[sym[i]] = (uint8_t)(i + 1); });
+                meet<64>();
+                bool twice = false;
+                each([&](uint32_t i) { twice |= marks[sym[i]] != (uint8_t)(i + 1); });
+                alone = !lanes_reduce<kLanes>((uint32_t)twice, Or());
             }
-            if (first) mass += x[i];
-        });
+            meet<64>();
+            each([&](uint32_t i) {
+                bool first = true;
+                mass_of[i] = (alone ? value[i] : together(i, first)) * norm;
+                if (first) mass += x[i];
+            });
+        } else {
+            // One of a pack's entries at a time becomes the first of those that are in it: as many rounds as the fullest pack has
+            // entries.  (All pairs looked at instead: 8192 x 65536 with 64 entries 552 us, 4096 x 131072 with 128 839.)
+            static_assert(kLanes == 64);
+            for (uint32_t from = 0; from < top; from += kLanes) {
+                const uint32_t i = from + lane;
+                bool waits = i < top && sym[i] >= 0;
+                const uint32_t at = waits ? place((uint32_t)sym[i] / kVec) : 0;
+                while (__ballot(waits)) {
+                    const uint32_t before = waits ? marks[at] : 0;
+                    meet<64>();
+                    if (waits) marks[at] = (uint8_t)(i + 1);
+                    meet<64>();
+                    if (waits && marks[at] == (uint8_t)(i + 1)) {
+                        after[i] = (uint8_t)before;
+                        waits = false;
+                    }
+                    meet<64>();
+                }
+            }
+            each([&](uint32_t i) {
+                bool alone = true, first = true;
+                for (uint32_t entry = marks[place((uint32_t)sym[i] / kVec)]; entry; entry = after[entry - 1]) alone &= entry - 1 == i || sym[entry - 1] != sym[i];
+                mass_of[i] = (alone ? value[i] : together(i, first)) * norm;
+                if (first) mass += x[i];
+            });
+        }
         mass = lanes_reduce<kLanes>(mass, Sum());
     }
     // The student's sum, by the largest value that `center` is made of, and what of it is the bulk's
@@ -263,20 +280,45 @@ struct DistillRow : LogitsRow<T, kLanes, kPer> {
     // Powers that the sum was made of are kept for the gradient where they are few
     static constexpr bool kKept = Row::kWaves <= 1 && kPer <= 4;
 
+    // Nothing worked out from the lane's number before is kept for after: it would take registers that the row needs.
+    __device__ void anew() { asm volatile("" : "+v"(this->lane)); }
+    // Bytes a pack: a lane's lie side by side, so that it reads them all at once
+    __device__ static uint32_t place_of(uint32_t pack) { return pack % kLanes * kPer + pack / kLanes; }
+    static constexpr int kWords = kTable ? 1 : (kPer + 3) / 4;
+    struct __attribute__((aligned(kTable || kPer < 4 ? 1 : kPer < 16 ? kPer : 16))) Bytes { uint32_t w[kWords]; };
+
     __device__ void clear(uint8_t *marks) const
     {
-        struct __attribute__((aligned(kTable ? kVec : 1))) None { uint8_t v[kTable ? kVec : 1]; };
+        if constexpr (kTable) {
+            using Word = std::conditional_t<kVec == 8, uint64_t, uint32_t>;
 #pragma unroll
-        for (int q = 0; q < kPer; ++q) ((None *)marks)[q * kLanes + this->lane] = None{};
+            for (int q = 0; q < kPer; ++q) ((Word *)marks)[q * kLanes + this->lane] = 0;
+        } else if constexpr (kPer >= 4) {
+            ((Bytes *)marks)[this->lane] = Bytes{};
+        } else {
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) marks[this->lane * kPer + q] = 0;
+        }
+    }
+    __device__ Bytes marks_of(const uint8_t *marks) const
+    {
+        Bytes m = {};
+        if constexpr (kTable) {
+        } else if constexpr (kPer >= 4) {
+            m = ((const Bytes *)marks)[this->lane];
+        } else {
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) m.w[0] |= (uint32_t)marks[this->lane * kPer + q] << (8 * q);
+        }
+        return m;
     }
     // f(place in the pack, entry) for the entries of pack q; those of its first values that another pack has are that one's.
     template <class F>
-    __device__ void named_in(const Named<kEntryLanes> &named, const uint8_t *marks, int q, uint32_t end, F f) const
+    __device__ void named_in(const Named<kEntryLanes> &named, const uint8_t *marks, const Bytes &bytes, int q, uint32_t end, F f) const
     {
-        const uint32_t pack = q * kLanes + this->lane;
         if constexpr (kTable) {
             using Word = std::conditional_t<kVec == 8, uint64_t, uint32_t>;
-            const Word w = ((const Word *)marks)[pack];
+            const Word w = ((const Word *)marks)[q * kLanes + this->lane];
             if (w) {
                 const uint32_t twice = (uint32_t)this->twice(q, 0, end);
 #pragma unroll
@@ -286,14 +328,16 @@ struct DistillRow : LogitsRow<T, kLanes, kPer> {
                 }
             }
         } else {
-            for (uint32_t entry = marks[pack]; entry; entry = named.after[entry - 1]) f((uint32_t)named.sym[entry - 1] - this->column(q, 0, end), entry - 1);
+            for (uint32_t entry = bytes.w[q / 4] >> (q % 4 * 8) & 255; entry; entry = named.after[entry - 1])
+                f((uint32_t)named.sym[entry - 1] - this->column(q, 0, end), entry - 1);
         }
     }
     __device__ void leave_out(const Named<kEntryLanes> &named, const uint8_t *marks, uint32_t end, Raw<T> (&x)[kPer], int used) const
     {
+        const Bytes bytes = marks_of(marks);
         Row::for_used(used, [&](int q) {
             uint32_t bits = 0;
-            named_in(named, marks, q, end, [&](uint32_t k, uint32_t) { bits |= 1u << k; });
+            named_in(named, marks, bytes, q, end, [&](uint32_t k, uint32_t) { bits |= 1u << k; });
             if (bits) rule_out_bits(x[q], bits);
         });
     }
@@ -374,12 +418,14 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         // registers to itself
         if constexpr (Row::kWaves <= 1) r.load((const T *)a.x + (uint64_t)row * a.stride, 0, a.num_sym, x);
         if constexpr (kMarked) meet<kLanes>();
-        if (mine) named.template prepare<kRest, Row::kTable ? 1 : Row::kVec>(a, marks);
+        if (mine) named.template prepare<kRest, Row::kTable ? 1 : Row::kVec>(a, marks, Row::place_of);
         if (kApart && threadIdx.x == 0) shared_known = named;
+        r.anew();
         if constexpr (Row::kWaves > 1) r.load((const T *)a.x + (uint64_t)row * a.stride, 0, a.num_sym, x);
         if constexpr (kMarked) meet<kLanes>();
         r.rule_out(0, a.num_sym, x);
         const int used = r.used(0, a.num_sym);
+        r.anew();
         if constexpr (kRest) r.leave_out(named, marks, a.num_sym, x, used);
         float of[kPer];
         const float own = r.largest(x, used, of);
@@ -397,6 +443,8 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
             if constexpr (Row::kWaves > 1) moves = shared_moves;
             const float center = center_of(moves.max);
             T *grad = (T *)a.grad + (uint64_t)row * a.grad_stride;
+            r.anew();
+            const auto bytes = r.marks_of(marks);
             Row::for_used(used, [&](int q) {
                 const uint32_t column = r.column(q, 0, a.num_sym);
                 float d[Row::kVec];
@@ -407,7 +455,7 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
                     r.powers(x[q], center, factor, d);
                 }
                 r.put(d, Row::address(grad, column, 0, a.num_sym), r.twice(q, 0, a.num_sym), moves, [&](float(&d)[Row::kVec]) {
-                    r.named_in(named, marks, q, a.num_sym, [&](uint32_t at, uint32_t entry) {
+                    r.named_in(named, marks, bytes, q, a.num_sym, [&](uint32_t at, uint32_t entry) {
                         const float g = named.x[entry];
 #pragma unroll
                         for (int k = 0; k < Row::kVec; ++k) d[k] = at == (uint32_t)k ? g : d[k];
@@ -482,7 +530,7 @@ __global__ __launch_bounds__(256) void k_distill_join(DistillArgs a)
             bulk = both(bulk, Bulk{p.x, p.y}, distill_factor(a));
         }
         for (int d = 1; d < 64; d *= 2) bulk = both(bulk, Bulk{__shfl_xor(bulk.max, d, 64), __shfl_xor(bulk.total, d, 64)}, distill_factor(a));
-        named.template prepare<kRest, 1>(a, nullptr);
+        named.template prepare<kRest, 1>(a, nullptr, [](uint32_t pack) { return pack; });
         const float loss = named.template loss<kRest>(a, bulk);
         Moves moves = {};
         if (a.grad) moves = named.template moves<kRest>(a, bulk, a.up[row]);
@@ -547,7 +595,7 @@ __global__ __launch_bounds__(256) void k_distill_short(DistillArgs a)
         if (kRest && is_named) x = -kInf;
         const float max = wave_reduce(x, MaxFloat());
         const Bulk bulk = {max, wave_reduce(exp2_fast((x - center_of(max)) * factor), Sum())};
-        named.template prepare<kRest, 1>(a, nullptr);
+        named.template prepare<kRest, 1>(a, nullptr, [](uint32_t pack) { return pack; });
         const float loss = named.template loss<kRest>(a, bulk);
         Moves moves = {};
         if (a.grad) moves = named.template moves<kRest>(a, bulk, a.up[row]);

@@ -128,6 +128,23 @@ def test_rows_that_are_spoilt(n, rest):
 
 
 @pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("n,top", [(5, 128), (300, 128), (9000, 128), (40000, 128), (140000, 128), (40000, 65)])
+def test_symbols_side_by_side_and_named_again_and_again(n, top, rest):
+    """Entries that share 16 bytes of a row, all of the same symbol, and at the row's very end."""
+    x, sym, value = inputs(6, n, top, rest)
+    rng = np.random.default_rng(top)
+    sym[0] = rng.permutation(np.arange(top) % n)
+    sym[1] = n - 1
+    sym[3] = n - 1 - rng.permutation(np.arange(top) % min(n, 40))
+    sym[4] = rng.integers(0, min(n, 3), top)
+    sym[5, ::2], sym[5, 1::2] = 0, n - 1
+    value[:] = -np.log(2.0 * top) - rng.random(value.shape) if rest else value
+    value[np.isinf(value)] = -20.0
+    run(x, sym, value, torch.float32, 1.0, rest, True)
+    run(x, sym, value, torch.bfloat16, 2.0, rest, True, in_place=True)
+
+
+@pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("n", [5, 300, 40000, 140000])
 def test_far_logits_and_one_sided_laws(n, rest):
     """Offsets that 32 bits hardly hold, a student that is certain of what is named, or of what is not: a rest of next to nothing."""
