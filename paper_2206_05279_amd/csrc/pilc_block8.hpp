@@ -107,6 +107,37 @@ __global__ __launch_bounds__(kTileThreads) void k_block8_tiles(uint32_t rows, ui
     }
 }
 
+// Rows by themselves, where no transposed matrix is wanted and no scales are shared: sixteen lanes a block, four rows at a time.
+template <class T>
+__global__ __launch_bounds__(256) void k_block8_rows(uint32_t rows, uint32_t width, const T *x, uint64_t x_stride, Block8 out)
+{
+    constexpr int kRows = 4;
+    const uint32_t packs = div_up(width, kBlock8) * 16;
+    const uint64_t items = (uint64_t)div_up(rows, kRows) * packs;  // whole blocks: lanes of a block go on together
+    for (uint64_t item = blockIdx.x * 256ull + threadIdx.x; item < items; item += gridDim.x * 256ull) {
+        const uint32_t group = (uint32_t)(items >> 32 ? item / packs : (uint32_t)item / packs), column = (uint32_t)(item - (uint64_t)group * packs) * 8;
+        const int valid = (int)min(width - min(column, width), 8u);
+        Pack<T, 8> p[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) p[i] = load_pack<8>(x + (uint64_t)min(group * kRows + i, rows - 1) * x_stride + (valid > 0 ? column : 0), valid);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            float v[8];
+            uint32_t m = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = widen(p[i].v[k]), m = max(m, size_bits(v[k]));
+            const uint32_t byte = scale_byte(lanes_reduce<16>(m, Max()), out.type), row = group * kRows + i;
+            const float f = scale_inverse(byte);
+            const uint32_t lo = codes_of(v[0] * f, v[1] * f, v[2] * f, v[3] * f, out.type, byte);
+            const uint32_t hi = codes_of(v[4] * f, v[5] * f, v[6] * f, v[7] * f, out.type, byte);
+            if (row < rows && valid > 0) {
+                store_pack<8>(out.code + (uint64_t)row * out.stride + column, valid, __builtin_bit_cast(Pack<uint8_t, 8>, (uint64_t)hi << 32 | lo));
+                if (column % kBlock8 == 0) out.scale[(uint64_t)row * out.scale_stride + column / kBlock8] = (uint8_t)byte;
+            }
+        }
+    }
+}
+
 // Values back, eight a thread and row, so that lanes' stores of 16-bit values follow one another; two rows at a time.
 template <class T>
 __global__ __launch_bounds__(256) void k_block8_values(uint32_t rows, uint32_t width, Block8 in, T *out, uint64_t stride)
@@ -158,6 +189,11 @@ int pilc_block8_quantize(uint32_t rows, uint32_t width, const void *x_dev, uint6
     const Block8 none = {}, o = out ? block8_of(*out) : none, t = out_t ? block8_of(*out_t) : none;
     return by_type(dtype, [&](auto *type) {
         using T = std::remove_pointer_t<decltype(type)>;
+        if (!out_t && !o.shared_bits) {
+            const uint64_t blocks = ((uint64_t)div_up(rows, 4) * div_up(width, kBlock8) * 16 + 255) / 256;
+            k_block8_rows<T><<<(uint32_t)std::min<uint64_t>(blocks, 1u << 20), 256, 0, (hipStream_t)hip_stream>>>(rows, width, (const T *)x_dev, x_stride, o);
+            return;
+        }
         const uint64_t tiles = (uint64_t)div_up(rows, kBlock8) * div_up(width, kBlock8);
         k_block8_tiles<T><<<(uint32_t)std::min<uint64_t>(tiles, 1u << 20), kTileThreads, 0, (hipStream_t)hip_stream>>>(rows, width, (const T *)x_dev, x_stride, o, t);
     });

@@ -48,25 +48,6 @@ struct Moves {
 struct Or {
     __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a | b; }
 };
-// As lanes_reduce, in 64 bits.
-template <int kDpp>
-__device__ __forceinline__ double from_partner64(double v)
-{
-    const uint64_t b = __builtin_bit_cast(uint64_t, v);
-    return __builtin_bit_cast(double, (uint64_t)from_partner<kDpp>((uint32_t)(b >> 32)) << 32 | from_partner<kDpp>((uint32_t)b));
-}
-template <int kLanes>
-__device__ __forceinline__ double lanes_sum(double v)
-{
-    if constexpr (kLanes >= 2) v += from_partner64<0xB1>(v);
-    if constexpr (kLanes >= 4) v += from_partner64<0x4E>(v);
-    if constexpr (kLanes >= 8) v += from_partner64<0x141>(v);
-    if constexpr (kLanes >= 16) v += from_partner64<0x140>(v);
-    if constexpr (kLanes >= 32) v += __shfl_xor(v, 16, 64);
-    if constexpr (kLanes >= 64) v += __shfl_xor(v, 32, 64);
-    return v;
-}
-
 // The values whose bit is set become -inf.
 template <class T>
 __device__ __forceinline__ void rule_out_bits(Raw<T> &x, uint32_t bits)
@@ -84,6 +65,23 @@ __device__ __forceinline__ void rule_out_bits(Raw<T> &x, uint32_t bits)
             x.bits[i] = w;
         }
     }
+}
+
+// ln x in 64 bits of a positive number of 32: x = 2^e m with m around 1, s = (m - 1) / (m + 1), ln m = 2 s (1 + s^2 / 3 + s^4 / 5 ..),
+// |s| < 0.172: what is left out is under 1e-11 of it.  The reciprocal is the hardware's with one step by Newton.
+__device__ __forceinline__ double log64(float x)
+{
+    int e = __builtin_amdgcn_frexp_expf(x);
+    float half = __builtin_amdgcn_frexp_mantf(x);
+    if (half < 0.70710678f) half *= 2.0f, --e;
+    const double den = (double)half + 1.0;
+    double r = (double)__builtin_amdgcn_rcpf(half + 1.0f);
+    r = r * (2.0 - den * r);
+    const double s = ((double)half - 1.0) * r, t = s * s;
+    double poly = 1.0 / 13;
+    poly = __builtin_fma(poly, t, 1.0 / 11), poly = __builtin_fma(poly, t, 1.0 / 9), poly = __builtin_fma(poly, t, 1.0 / 7);
+    poly = __builtin_fma(poly, t, 1.0 / 5), poly = __builtin_fma(poly, t, 1.0 / 3);
+    return __builtin_fma(2.0 * s * t, poly, 2.0 * s) + e * 0.69314718055994530942;
 }
 
 // What is known of a row's entries together.
@@ -162,7 +160,7 @@ struct Named : Known {
         float norm = 1.0f;
         if constexpr (!kRest)
             if (all > 0.0) {
-                gain = gain / all - logf((float)all);
+                gain = gain / all - log64((float)all);
                 norm = (float)(1.0 / all);
                 all = 1.0;
             }
@@ -253,14 +251,14 @@ struct Named : Known {
         each([&](uint32_t i) { x[i] = zeros ? 0.0f : by * (x[i] * p - mass_of[i]); });
         return {bulk.max, by * share, zeros};
     }
-    // Logarithms in 32 bits: off by 2^-24 of themselves, at most 12 for 2^17 symbols
+    // Logarithms of up to 12, for 2^17 symbols, of which a loss is a small difference
     template <bool kRest>
     __device__ float loss(const DistillArgs &a, Bulk bulk) const
     {
         const Whole w = whole<kRest>(a, bulk);
-        const double log_total = logf(w.total), left = kRest && bulk.total > 0.0f ? fmax(0.0, 1.0 - all) : 0.0;
+        const double log_total = log64(w.total), left = kRest && bulk.total > 0.0f ? fmax(0.0, 1.0 - all) : 0.0;
         double sum = gain + all * (log_total - ((double)center_of(max) - w.center) * a.turn);
-        if (left > 0.0) sum += left * ((double)logf((float)left) - (((double)bulk.max - w.center) * a.turn + logf(bulk.total) - log_total));
+        if (left > 0.0) sum += left * (log64((float)left) - (((double)bulk.max - w.center) * a.turn + log64(bulk.total) - log_total));
         const bool weighted = all > 0.0;
         if (!(flags & kAny)) return 0.0f;
         if (w.spoilt) return __builtin_nanf("");

@@ -143,6 +143,25 @@ __device__ __forceinline__ V lanes_reduce(V v, Op op)
     return v;
 }
 
+// As lanes_reduce, in 64 bits.
+template <int kDpp>
+__device__ __forceinline__ double from_partner64(double v)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    return __builtin_bit_cast(double, (uint64_t)from_partner<kDpp>((uint32_t)(b >> 32)) << 32 | from_partner<kDpp>((uint32_t)b));
+}
+template <int kLanes>
+__device__ __forceinline__ double lanes_sum(double v)
+{
+    if constexpr (kLanes >= 2) v += from_partner64<0xB1>(v);
+    if constexpr (kLanes >= 4) v += from_partner64<0x4E>(v);
+    if constexpr (kLanes >= 8) v += from_partner64<0x141>(v);
+    if constexpr (kLanes >= 16) v += from_partner64<0x140>(v);
+    if constexpr (kLanes >= 32) v += __shfl_xor(v, 16, 64);
+    if constexpr (kLanes >= 64) v += __shfl_xor(v, 32, 64);
+    return v;
+}
+
 template <class V, class Op>
 __device__ __forceinline__ V wave_reduce(V v, Op op)
 {

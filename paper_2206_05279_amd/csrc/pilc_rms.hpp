@@ -86,10 +86,15 @@ struct RmsRow {
         for (int k = 0; k < kVec; ++k) t.v[k] = (W)1.0f;
         return t;
     }
-    // The row's sum in all its lanes; `room`'s halves are used in turn, so that the workgroup meets once a sum.
-    __device__ float sum(float v, float *room, int half) const
+    // The row's sum in all its lanes; `room`'s halves are used in turn, so that the workgroup meets once a sum.  In 64 bits for
+    // the sum of squares: all of a row's values are off by what it is, and codes near a border with them.
+    template <class V>
+    __device__ V sum(V v, V *room, int half) const
     {
-        v = lanes_reduce<kWithin>(v, Sum());
+        if constexpr (sizeof(V) == 8)
+            v = lanes_sum<kWithin>(v);
+        else
+            v = lanes_reduce<kWithin>(v, Sum());
         if constexpr (kWaves > 1) {
             room += half * kWaves;
             if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
@@ -135,9 +140,8 @@ k_rms_forward_rows(RmsArgs a)
 {
     using Row = RmsRow<T, W, kLanes, kEach>;
     constexpr int kVec = Row::kVec, kPer = Row::kPer;
-    __shared__ float room[2 * (Row::kWaves > 1 ? Row::kWaves : 1)];
+    __shared__ double room[2 * (Row::kWaves > 1 ? Row::kWaves : 1)];
     const Row r(a.width);
-    const float per_value = 1.0f / (float)a.width;
     Pack<W, kVec> weight[kPer];
     if (Row::kKeep)
 #pragma unroll
@@ -168,12 +172,12 @@ k_rms_forward_rows(RmsArgs a)
 #pragma unroll
             for (int q = 0; q < kPer; ++q) r.store((T *)a.sum + (uint64_t)row * a.sum_stride, q, x[q]);
         }
-        float square[2] = {0.0f, 0.0f};
+        float square[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int q = 0; q < kPer; ++q)
 #pragma unroll
-            for (int k = 0; k < kVec; ++k) square[k & 1] = __builtin_fmaf(x[q][k], x[q][k], square[k & 1]);
-        const float rstd = 1.0f / sqrtf(r.sum(square[0] + square[1], room, half) * per_value + a.eps);
+            for (int k = 0; k < kVec; ++k) square[k & 3] = __builtin_fmaf(x[q][k], x[q][k], square[k & 3]);
+        const float rstd = 1.0f / sqrtf((float)(r.sum((double)((square[0] + square[1]) + (square[2] + square[3])), room, half) / a.width) + a.eps);
         half ^= 1;
         if (r.lane == 0 && a.rstd) a.rstd[row] = rstd;
         const auto out = [&](int q, float(&v)[kVec]) {
@@ -340,12 +344,12 @@ template <class T, class W>
 __global__ __launch_bounds__(kRmsLongThreads) void k_rms_forward_long(RmsArgs a)
 {
     constexpr int kVec = 16 / sizeof(T), kWaves = kRmsLongThreads / 64;
-    __shared__ float room[kWaves];
+    __shared__ double room[kWaves];
     const W *weight = (const W *)a.weight;
     for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *x = (const T *)a.x + row * a.x_stride, *add = a.add ? (const T *)a.add + row * a.add_stride : nullptr;
         T *sum = a.sum ? (T *)a.sum + row * a.sum_stride : nullptr;
-        float square = 0.0f;
+        double square = 0.0;
         for_long<kVec>(a.width, [&](const auto &at, const auto &valid) {
             Pack<T, kVec> t[kRmsLongEach], u[kRmsLongEach];
 #pragma unroll
@@ -355,15 +359,17 @@ __global__ __launch_bounds__(kRmsLongThreads) void k_rms_forward_long(RmsArgs a)
             }
 #pragma unroll
             for (int q = 0; q < kRmsLongEach; ++q) {
+                float own = 0.0f;
 #pragma unroll
                 for (int k = 0; k < kVec; ++k) {
                     if (add) t[q].v[k] = (T)(widen(t[q].v[k]) + widen(u[q].v[k]));
-                    square = __builtin_fmaf(widen(t[q].v[k]), widen(t[q].v[k]), square);
+                    own = __builtin_fmaf(widen(t[q].v[k]), widen(t[q].v[k]), own);
                 }
+                square += own;
                 if (sum && valid[q] > 0) store_pack<kVec>(sum + at[q], valid[q], t[q]);
             }
         });
-        const float rstd = 1.0f / sqrtf(block_reduce<kWaves>(square, Sum(), room) / (float)a.width + a.eps);
+        const float rstd = 1.0f / sqrtf((float)(block_reduce<kWaves>(square, Sum(), room) / a.width) + a.eps);
         if (threadIdx.x == 0 && a.rstd) a.rstd[row] = rstd;
         // what a thread has put down as the sum it finds there itself; the sum may have taken x's or add's place
         const T *again = sum ? sum : x, *more = sum ? nullptr : add;
