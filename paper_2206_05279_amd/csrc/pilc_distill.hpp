@@ -20,6 +20,7 @@ struct DistillArgs {
     void *grad;
     uint64_t stride, grad_stride;
     uint32_t rows, num_sym, top;
+    uint64_t first;         // k_distill: the first row
     float turn;             // 1 / temperature
     uint32_t splits, span;  // see LogitsArgs
     float2 *part;           // of each run: its largest value and sum
@@ -256,9 +257,14 @@ struct Named : Known {
     __device__ float loss(const DistillArgs &a, Bulk bulk) const
     {
         const Whole w = whole<kRest>(a, bulk);
-        const double log_total = log64(w.total), left = kRest && bulk.total > 0.0f ? fmax(0.0, 1.0 - all) : 0.0;
+        const double left = kRest && bulk.total > 0.0f ? fmax(0.0, 1.0 - all) : 0.0;
+        // three lanes' logarithms at once, or one's
+        const double log_of = log64(kRest && lane % 4 == 1 ? bulk.total : kRest && lane % 4 == 2 ? (float)left : w.total);
+        const int first = kRest ? (int)(threadIdx.x & 63 & ~3u) : 0;
+        const double log_total = kRest ? __shfl(log_of, first, 64) : log_of;
+        const double log_bulk = kRest ? __shfl(log_of, first + 1, 64) : 0.0, log_left = kRest ? __shfl(log_of, first + 2, 64) : 0.0;
         double sum = gain + all * (log_total - ((double)center_of(max) - w.center) * a.turn);
-        if (left > 0.0) sum += left * (log64((float)left) - (((double)bulk.max - w.center) * a.turn + log64(bulk.total) - log_total));
+        if (left > 0.0) sum += left * (log_left - (((double)bulk.max - w.center) * a.turn + log_bulk - log_total));
         const bool weighted = all > 0.0;
         if (!(flags & kAny)) return 0.0f;
         if (w.spoilt) return __builtin_nanf("");
@@ -386,17 +392,17 @@ struct DistillRow : LogitsRow<T, kLanes, kPer> {
     }
 };
 
-// A row a workgroup or a part of it, with kGrad its gradient from the same registers.
+// A row a workgroup or a part of it, with kGrad its gradient from the same registers.  No loop over rows: what does not change from row to
+// row would be kept in registers that the row needs (8192 x 65536, 64 named: 384 us, with a loop 440).
 template <class T, int kLanes, int kPer, bool kRest, bool kGrad>
 __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<T, kLanes, kPer>::kResident)) void k_distill(DistillArgs a)
 {
     using Row = DistillRow<T, kLanes, kPer>;
     constexpr bool kMarked = kRest || kGrad;
-    __shared__ Bulk room[2 * Row::kWaves];
+    __shared__ Bulk room[Row::kWaves];
     __shared__ Moves shared_moves;
     extern __shared__ uint32_t more_room[];  // the rows' marks, then their entries
     Row r;
-    const uint64_t step = (uint64_t)gridDim.x * Row::kRows;
     const float factor = distill_factor(a);
     uint8_t *marks = kMarked ? (uint8_t *)more_room + r.row_in_block * Row::kMarks : nullptr;
     using Entries = Named<Row::kEntryLanes>;
@@ -404,8 +410,8 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
     __shared__ Known shared_known;  // where a row has several wavefronts, which would keep it in registers for the first one
     constexpr bool kApart = Row::kWaves > 1;
     const bool mine = Row::kWaves <= 1 || threadIdx.x < 64;  // of a row's wavefronts the first sees to the entries
-    int half = 0;
-    for (uint64_t item = (uint64_t)blockIdx.x * Row::kRows + r.row_in_block; item < a.rows; item += step) {
+    const uint64_t item = a.first + (uint64_t)blockIdx.x * Row::kRows + r.row_in_block;
+    if (item < a.rows) {
         const uint32_t row = (uint32_t)item;
         const float up = kGrad ? a.up[row] : 0.0f;
         if constexpr (kMarked) r.clear(marks);
@@ -430,9 +436,8 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
         r.forget(x);
         constexpr bool kKept = kGrad && Row::kKept;
         float kept[kKept ? kPer : 1][Row::kVec];
-        const Bulk bulk = r.template bulk<kKept>(x, used, own, factor, room, half, kept);
+        const Bulk bulk = r.template bulk<kKept>(x, used, own, factor, room, 0, kept);
         r.forget(x);
-        half ^= 1;
         if constexpr (kGrad) {
             Moves moves = {};
             if (mine) moves = Entries(entries, a.top, kApart ? shared_known : (const Known &)named).template moves<kRest>(a, bulk, up);
@@ -465,7 +470,6 @@ __global__ __launch_bounds__((LogitsRow<T, kLanes, kPer>::kThreads), (LogitsRow<
             const float loss = Entries(entries, a.top, kApart ? shared_known : (const Known &)named).template loss<kRest>(a, bulk);
             if (r.lane == 0) a.loss[row] = loss;
         }
-        meet<kLanes>();
     }
 }
 
@@ -636,7 +640,10 @@ static void launch_distill_rows(DistillArgs a, hipStream_t stream)
     logits_row<kGrad ? kTrainRows : kLaw>(a.num_sym * (uint32_t)sizeof(T), 0, true, [&](auto lanes, auto per) {
         using Row = DistillRow<T, decltype(lanes)::value, decltype(per)::value>;
         const size_t lds = Row::kRows * ((kRest || kGrad ? Row::kMarks : 0) + Named<Row::kEntryLanes>::bytes(a.top));
-        k_distill<T, decltype(lanes)::value, decltype(per)::value, kRest, kGrad><<<logits_blocks(a.rows, Row::kRows), Row::kThreads, lds, stream>>>(a);
+        constexpr uint64_t kMost = (uint64_t)Row::kRows << 20;  // rows a launch
+        for (a.first = 0; a.first < a.rows; a.first += kMost)
+            k_distill<T, decltype(lanes)::value, decltype(per)::value, kRest, kGrad>
+                <<<logits_blocks(std::min(a.rows - a.first, kMost), Row::kRows), Row::kThreads, lds, stream>>>(a);
     });
 }
 
