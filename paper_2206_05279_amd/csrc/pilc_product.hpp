@@ -125,7 +125,8 @@ __device__ __forceinline__ void product_wait()
 // Otherwise (rows that do not begin at multiples of 16 bytes) they come through registers.  The last block, where the depth is no multiple
 // of 128, is a step of its own.
 //
-// Measured, 8192 x 8192 x 8192: the loop without scales' rounding of clocks runs at the rate that power allows.
+// Bound by power: 8192 x 8192 x 8192 into bfloat16, 424 us or 2590 TFLOP/s; with matrices of zeros, which take less of it, the same
+// instructions reach 3100 to 3400.  Through registers 693 us where codes begin at any byte, 621 at multiples of four.
 template <int kTypeA, int kTypeB, int kTile, bool kDirect>
 __global__ __launch_bounds__(256, kTile == 256 ? 1 : 2) void k_product_groups(ProductArgs p)
 {
@@ -359,6 +360,8 @@ __global__ __launch_bounds__(256, kTile == 256 ? 1 : 2) void k_product_groups(Pr
 
 // The same tiles for sums of 32 bits: 64 of the depth a step, widened on the way from registers to LDS, which holds them as 32 chunks of
 // eight a row's 64 and both sides.  What a thread fetches is widened and put down a step later, a chunk beside every 16 rows' products.
+// Bound by the matrix unit, whose bfloat16 products take twice as long, and by power: 2047 x 1531 x 32777, rows that begin at
+// any byte, 236 us or 870 TFLOP/s; with values that hardly differ in size, which take less power, 192.
 template <int kTypeA, int kTypeB, int kTile>
 __global__ __launch_bounds__(256, kTile == 256 ? 1 : 2) void k_product_singles(ProductArgs p)
 {
@@ -489,7 +492,7 @@ __global__ __launch_bounds__(256, kTile == 256 ? 1 : 2) void k_product_singles(P
 }
 
 // Few rows: b is read once, from memory to registers, and that bounds it.  A workgroup takes 16 or 32 columns and shares their depth out
-// among its wavefronts, whose sums meet in LDS.
+// among its wavefronts, whose sums meet in LDS.  1 x 131072 x 4096 into float32 93 us, 5.8 TB/s.
 template <int kTypeA, int kTypeB, int kRowTiles, int kColTiles>
 __global__ __launch_bounds__(512) void k_product_few(ProductArgs p)
 {

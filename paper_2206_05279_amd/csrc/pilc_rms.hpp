@@ -17,7 +17,11 @@ struct RmsArgs {
 
 constexpr int kRmsLongThreads = 1024;
 // Wavefronts a SIMD that the kernels' registers are kept down to, and that are launched: all at once, each going from row to row.
-constexpr int kRmsForwardWaves = 4, kRmsBackwardWaves = 2;
+// Forward with two and with four, bfloat16, us: 32768 x 4096 92 and 103, 16384 x 8192 with a sum 194 and 201, 65536 x 1024 with a
+// sum 95 and 99, but 262144 x 128 73 and 53; with eight, which lack the registers, 164, 293, 126 and 51.
+// In 8 bits there is more to compute: 16384 x 8192 with a sum and float32 weights 212 with two and 181 with four.
+constexpr int kRmsBackwardWaves = 2;
+constexpr int rms_forward_waves(int lanes, bool in_8_bits) { return lanes < 64 || in_8_bits ? 4 : 2; }
 
 // Rows held in registers: kLanes lanes of a wavefront, or a whole workgroup of kLanes threads, hold kEach values of a row each, as
 // packs of 16 bytes, and go from row to row.  A pack that would reach over the row's end is loaded from further ahead and
@@ -134,8 +138,10 @@ __device__ __forceinline__ Raw<T> added(const Raw<T> &x, const Raw<T> &add)
     return Raw<T>::of(v);
 }
 
-template <class T, class W, int kLanes, int kEach>
-__global__ __launch_bounds__((RmsRow<T, W, kLanes, kEach>::kThreads), (RmsRow<T, W, kLanes, kEach>::waves(kRmsForwardWaves))) void
+// A row's sum, its norm and what is wanted of that, from one read.  Bound by memory: 16384 x 8192 bfloat16 with a sum and a result in
+// 8 bits 181 us, 5.2 TB/s.
+template <class T, class W, int kLanes, int kEach, int kMostWaves>
+__global__ __launch_bounds__((RmsRow<T, W, kLanes, kEach>::kThreads), (RmsRow<T, W, kLanes, kEach>::waves(kMostWaves))) void
 k_rms_forward_rows(RmsArgs a)
 {
     using Row = RmsRow<T, W, kLanes, kEach>;
@@ -220,7 +226,8 @@ k_rms_forward_rows(RmsArgs a)
 }
 
 // dx row by row as above, and what the rows a workgroup meets add to the weight's gradient, in registers; at the end the workgroup's
-// rows are added up and put down as one part.  The longest rows leave no room for that: k_rms_parts.
+// rows are added up and put down as one part.  The longest rows leave no room for that: k_rms_parts.  Bound by memory: 32768 x 4096
+// bfloat16 with the residual's gradient 191 us, 5.6 TB/s, and 5 for the parts (k_rms_join).
 template <class T, class W, int kLanes, int kEach>
 __global__ __launch_bounds__((RmsRow<T, W, kLanes, kEach>::kThreads), (RmsRow<T, W, kLanes, kEach>::waves(kRmsBackwardWaves))) void
 k_rms_backward_rows(RmsArgs a)
@@ -522,7 +529,8 @@ static uint32_t rms_blocks(uint32_t rows, int most_waves)
     return std::min(div_up(rows, Row::kRows), compute_units() * (uint32_t)(Row::waves(most_waves) * 256 / Row::kThreads));
 }
 // Workgroups of the backward pass: with the weight's gradient each puts down a part, as much as two rows in 32 bits, so that few
-// rows are shared out by four, once half the compute units have one.
+// rows are shared out by four, once half the compute units have one (bfloat16, us, with and without: 512 x 4096 11.4 13.8, 1024 x 4096
+// 12.8 15.3, 512 x 16384 20.3 21.9, 4096 x 4096 23.9 23.9).
 template <class Row>
 static uint32_t rms_backward_blocks(uint32_t rows, bool with_parts)
 {
@@ -572,8 +580,12 @@ int pilc_rms_forward(const pilc_rms_shape *shape, const void *x_dev, const void 
         using W = std::remove_pointer_t<decltype(w)>;
         if (!rms_row(a.width, [&](auto lanes, auto each) {
                 using Row = RmsRow<T, W, decltype(lanes)::value, decltype(each)::value>;
-                k_rms_forward_rows<T, W, decltype(lanes)::value, decltype(each)::value>
-                    <<<rms_blocks<Row>(a.rows, kRmsForwardWaves), Row::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+                const auto launch = [&](auto waves) {
+                    k_rms_forward_rows<T, W, decltype(lanes)::value, decltype(each)::value, decltype(waves)::value>
+                        <<<rms_blocks<Row>(a.rows, waves), Row::kThreads, 0, (hipStream_t)hip_stream>>>(a);
+                };
+                y8 ? launch(std::integral_constant<int, rms_forward_waves(decltype(lanes)::value, true)>())
+                   : launch(std::integral_constant<int, rms_forward_waves(decltype(lanes)::value, false)>());
             }))
             k_rms_forward_long<T, W><<<std::min(a.rows, 1u << 20), kRmsLongThreads, 0, (hipStream_t)hip_stream>>>(a);
     });
