@@ -478,6 +478,8 @@ int pilc_adamw_values(const uint8_t *code_dev, const uint8_t *scale_dev, uint64_
  * From a network's last states to its logits, in 8 bits: matrices whose values share scales in
  * blocks of 128, their product, the norm that answers in them, and the loss that teaches a small
  * network a large one's laws.  What is said above of streams, alignment and rounding holds here.
+ * A call writes its workspace: calls that may run at the same time, replays of captured graphs
+ * among them, need one each.
  * ------------------------------------------------------------------------------------------ */
 enum { PILC_E4M3 = 0, PILC_E5M2 = 1 }; /* types of 8-bit values: 4 bits of exponent, up to 448, no infinity; 5, up to 57344 */
 

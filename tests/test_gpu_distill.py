@@ -215,6 +215,24 @@ def test_rows_beyond_32_bits():
     assert (xt[1:32768] == 0).all()
 
 
+@pytest.mark.parametrize("rest", [False, True])
+def test_more_rows_than_a_launch_takes(rest):
+    """Rows of eight symbols go 32 to a workgroup and 2^20 workgroups to a launch: the rows of the second answer as the first's do."""
+    rows, some = (1 << 25) + 77, 1000
+    x, sym, value = inputs(some, 8, 2, rest)
+    base = torch.from_numpy(x).to(torch.bfloat16).to(DEV)
+    many = lambda t: t.repeat(-(-rows // some), 1)[:rows]  # noqa: E731
+    xt, st, vt = many(base), many(torch.from_numpy(sym).to(DEV)), many(torch.from_numpy(value).to(DEV))
+    loss, one = torch.empty(rows, device=DEV), torch.ones(rows, device=DEV)
+    pb.pilc_distill(xt, st, vt, loss, up=one, grad=xt, rest=rest, workspace=workspace(pb.pilc_distill_workspace_size(rows, 8, 2)))
+    want, want_g, err, g_err = orc.distill(up(base), sym, value.astype(float), np.ones(some), 1.0, rest)
+    close(loss[:some], want, err, torch.float32, "loss")
+    close(xt[:some], want_g, g_err, torch.bfloat16, "gradient")
+    whole = rows // some * some
+    assert (loss[:whole].view(-1, some) == loss[:some]).all() and torch.equal(loss[whole:], loss[:rows - whole])
+    assert (xt[:whole].view(-1, some, 8) == xt[:some]).all() and torch.equal(xt[whole:], xt[:rows - whole])
+
+
 @pytest.mark.parametrize("rows,n,rest", [(3000, 256, False), (40, 5000, True), (300, 40000, True), (5, 150000, True)])
 def test_same_bits_every_time_on_another_stream_and_in_a_graph(rows, n, rest):
     x, sym, value = inputs(min(rows, 40), n, 16, rest)
