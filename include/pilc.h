@@ -546,7 +546,8 @@ typedef struct {
  *               bits; NULL: not wanted
  *   rstd_dev    f32 [rows]; NULL: not wanted
  *   weight_dev  [width]; NULL: 1
- * One of sum, y, y8, rstd at least is wanted.  Errors: PILC_E_ARG, PILC_E_HIP. */
+ * One of sum, y, y8, rstd at least is wanted.  The squares are 32 bits': a row with values beyond 1e19 has rstd 0, and one of
+ * zeros with eps 0 the 0 * infinity that the formula says, which is no number.  Errors: PILC_E_ARG, PILC_E_HIP. */
 int pilc_rms_forward(const pilc_rms_shape *shape, const void *x_dev, const void *add_dev, const void *weight_dev,
                      void *sum_dev, void *y_dev, const pilc_block8 *y8, float *rstd_dev, void *hip_stream);
 

@@ -36,9 +36,10 @@ EXPORTS = [
     "pilc_logprobs_workspace_size", "pilc_logprobs", "pilc_logprobs_grad", "pilc_logprobs_train",
     "pilc_norm_workspace_size", "pilc_norm_forward", "pilc_norm_backward",
     "pilc_adamw_step", "pilc_adamw_values",
-    "pilc_block8_quantize", "pilc_block8_values", "pilc_block8_product_workspace_size", "pilc_block8_product",
     "pilc_rms_forward", "pilc_rms_workspace_size", "pilc_rms_backward", "pilc_distill_workspace_size", "pilc_distill",
 ]
+#: and those whose names have a digit in them
+EXPORTS_WITH_DIGITS = ["pilc_block8_quantize", "pilc_block8_values", "pilc_block8_product_workspace_size", "pilc_block8_product"]
 
 
 class pilc_geom(C.Structure):

@@ -1,5 +1,7 @@
 """What the entry points between states and laws refuse, before anything runs on a GPU."""
 import ctypes as C
+import os
+import re
 
 import pytest
 import torch
@@ -172,3 +174,12 @@ def test_tensors_that_the_binding_refuses():
               lambda: pb.pilc_distill(x, sym, value, loss, temperature=0.0, workspace=ws)):
         with pytest.raises(pb.PilcError):
             f()
+
+
+def test_the_library_exports_what_the_header_declares_digits_among_the_names():
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "pilc.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    names = set(re.findall(r"\b(pilc_[a-z0-9_]+)\s*\(", text))
+    assert names == set(pb.EXPORTS) | set(pb.EXPORTS_WITH_DIGITS)
+    for name in names:
+        assert hasattr(pb.lib(), name), name
